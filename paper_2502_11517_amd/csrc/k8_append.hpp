@@ -1,0 +1,208 @@
+// New rows of one layer into the cache, as 8-bit codes.
+//
+// A wave takes the rows that a call brings into one block (a run of at most 16 neighbouring slots) of one kv head, K or V: their
+// largest magnitude gives the scale, codes ahead of the run are rounded again if the scale grew, and a block begun by the run is
+// written whole.  Scales are powers of two, so x / scale is exact and a code is one rounding of its value.  Magnitudes are compared
+// as bits: what is not finite is then larger than everything finite.
+#pragma once
+#include "k8_dev.hpp"
+
+namespace k8 {
+
+struct AppendArgs {
+  Geometry g;
+  int n_rows, group;  // rows that a work-group looks at
+  const int* slot;
+  const void *k_new, *v_new;
+  uint8_t *k, *v;
+  float *ks, *vs;
+};
+
+template <int IN, int N>
+__device__ inline void load_row(const void* base, int64_t at, float (&x)[N]) {  // N neighbouring values
+  if constexpr (IN == kF32) {
+    const float* p = (const float*)base + at;
+    if constexpr (N >= 4) {
+      for (int i = 0; i < N; i += 4) {
+        const float4v w = *(const float4v*)(p + i);
+        for (int k = 0; k < 4; ++k) x[i + k] = w[k];
+      }
+    } else if constexpr (N == 2) {
+      const float2v w = *(const float2v*)p;
+      x[0] = w[0], x[1] = w[1];
+    } else {
+      x[0] = *p;
+    }
+  } else {
+    const uint16_t* p = (const uint16_t*)base + at;
+    uint32_t w[(N + 1) / 2];
+    if constexpr (N >= 8) {
+      for (int i = 0; i < N / 8; ++i) {
+        const uint4v t = *((const uint4v*)p + i);
+        for (int k = 0; k < 4; ++k) w[4 * i + k] = t[k];
+      }
+    } else if constexpr (N == 2) {
+      w[0] = *(const uint32_t*)p;
+    } else {
+      w[0] = *p;
+    }
+    for (int i = 0; i < N; ++i) {
+      const uint32_t b = (i & 1) ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
+      if constexpr (IN == kBf16) {
+        x[i] = __uint_as_float(b << 16);
+      } else {
+        union { uint16_t u; _Float16 h; } c{(uint16_t)b};
+        x[i] = (float)c.h;
+      }
+    }
+  }
+}
+
+__device__ inline uint32_t wave_max(uint32_t x) {
+  for (int d = 32; d; d >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+  return x;
+}
+
+struct RunScale {
+  float inverse;  // 2^-e of the new codes
+  float again;    // 2^(f-e) for the codes ahead of the run
+  float scale;    // what the block gets
+  bool regrown, lost;
+};
+
+template <int CODES>
+__device__ inline RunScale run_scale(uint32_t amax, int offset, float was) {
+  RunScale s{};
+  const bool bad = amax >= 0x7f800000u;
+  int e = bad ? kEMin : scale_exponent<CODES>(amax);
+  s.lost = bad;
+  if (offset > 0) {
+    if (was != was) {
+      s.lost = true;
+    } else {
+      const int f = min(max((int)(__float_as_uint(was) >> 23 & 255) - 127, kEMin), kEMax);
+      s.regrown = !bad && e > f;
+      s.again = s.regrown ? (e - f > 126 ? 0.f : pow2f(f - e)) : 1.f;
+      e = max(e, f);
+    }
+  }
+  s.inverse = pow2f(-e);
+  s.scale = s.lost ? __builtin_nanf("") : pow2f(e);
+  return s;
+}
+
+// K: a lane holds 16 dims of a token, one piece of the block's layout (two pieces if D = 128).
+template <int CODES, int D, int IN>
+__device__ inline void append_k(const AppendArgs& a, int row, int n, int offset, int head, int64_t block) {
+  constexpr int kPieces = D / 64;
+  const int lane = threadIdx.x & 63, token = lane >> 2, part = lane & 3;
+  uint8_t* codes = a.k + block * (kBlock * D);
+  const float was = offset ? a.ks[block] : 0.f;
+  float x[kPieces][16];
+  uint32_t amax = 0;
+  const bool mine = token >= offset && token < offset + n;
+  for (int j = 0; j < kPieces; ++j) {
+    for (int i = 0; i < 16; ++i) x[j][i] = 0.f;
+    if (mine) load_row<IN, 16>(a.k_new, ((int64_t)(row + token - offset) * a.g.Hkv + head) * D + (part + 4 * j) * 16, x[j]);
+    for (int i = 0; i < 16; ++i) amax = max(amax, __float_as_uint(x[j][i]) & 0x7fffffffu);
+  }
+  const RunScale s = run_scale<CODES>(wave_max(amax), offset, was);
+  const bool before = token < offset;
+  for (int j = 0; j < kPieces; ++j) {
+    uint4v* to = (uint4v*)(codes + ((part + 4 * j) * kBlock + token) * 16);
+    if (before && !s.regrown) continue;
+    if (!before && !mine && offset) continue;  // behind the run of a block that had begun
+    uint4v w;
+    if (before) {
+      w = *to;
+      for (int i = 0; i < 4; ++i) {
+        float y[4];
+        decode4<CODES>(w[i], y);
+        w[i] = encode4<CODES>(y[0] * s.again, y[1] * s.again, y[2] * s.again, y[3] * s.again);
+      }
+    } else {
+      for (int i = 0; i < 4; ++i)
+        w[i] = s.lost ? 0u : encode4<CODES>(x[j][4 * i] * s.inverse, x[j][4 * i + 1] * s.inverse, x[j][4 * i + 2] * s.inverse, x[j][4 * i + 3] * s.inverse);
+    }
+    *to = w;
+  }
+  if (lane == 0) a.ks[block] = s.scale;
+}
+
+// V: a lane holds all 16 tokens of one dim (two if D = 128), rows of the block's layout.
+template <int CODES, int D, int IN>
+__device__ inline void append_v(const AppendArgs& a, int row, int n, int offset, int head, int64_t block) {
+  constexpr int N = D / 64;
+  const int lane = threadIdx.x & 63;
+  uint4v* codes = (uint4v*)(a.v + block * (kBlock * D)) + lane * N;
+  const float was = offset ? a.vs[block] : 0.f;
+  uint4v old[N];
+  for (int j = 0; j < N; ++j) old[j] = offset ? codes[j] : uint4v{0, 0, 0, 0};
+  float x[kBlock][N];
+  uint32_t amax = 0;
+#pragma unroll
+  for (int t = 0; t < kBlock; ++t) {
+    for (int j = 0; j < N; ++j) x[t][j] = 0.f;
+    if (t >= offset && t < offset + n) load_row<IN, N>(a.v_new, ((int64_t)(row + t - offset) * a.g.Hkv + head) * D + lane * N, x[t]);
+  }
+#pragma unroll
+  for (int t = 0; t < kBlock; ++t)
+    for (int j = 0; j < N; ++j) amax = max(amax, __float_as_uint(x[t][j]) & 0x7fffffffu);
+  const RunScale s = run_scale<CODES>(wave_max(amax), offset, was);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    uint4v w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t fresh = s.lost ? 0u : encode4<CODES>(x[4 * i][j] * s.inverse, x[4 * i + 1][j] * s.inverse, x[4 * i + 2][j] * s.inverse, x[4 * i + 3][j] * s.inverse);
+      uint32_t again = old[j][i];
+      if (s.regrown) {
+        float y[4];
+        decode4<CODES>(again, y);
+        again = encode4<CODES>(y[0] * s.again, y[1] * s.again, y[2] * s.again, y[3] * s.again);
+      }
+      uint32_t before = 0, run = 0;  // bytes ahead of the run, bytes of the run
+      for (int k = 0; k < 4; ++k) {
+        const int t = 4 * i + k;
+        if (t < offset) before |= 255u << (8 * k);
+        else if (t < offset + n) run |= 255u << (8 * k);
+      }
+      w[i] = (again & before) | (fresh & run) | (old[j][i] & ~(before | run));
+    }
+    codes[j] = w;
+  }
+  if (lane == 0) a.vs[block] = s.scale;
+}
+
+template <int CODES, int D, int IN>
+__global__ __launch_bounds__(256) void k8_append(AppendArgs a) {
+  const int lane = threadIdx.x & 63, task = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = task >> 1;
+  if (head >= a.g.Hkv) return;
+  const int n_slots = a.g.n_pages << a.g.page_shift;
+  const int first = blockIdx.x * a.group, last = min(first + a.group, a.n_rows);
+  int i = first;
+  while (i < last) {
+    // lane k: the slot of row i + k - 1
+    const int at = i + lane - 1;
+    const int mine = lane <= kBlock && at >= 0 && at < a.n_rows ? a.slot[at] : -1;
+    const int prev = __builtin_amdgcn_readlane(mine, 0), slot = __builtin_amdgcn_readlane(mine, 1);
+    if (slot < 0 || slot >= n_slots) {
+      ++i;
+      continue;
+    }
+    const bool goes_on = lane >= 1 && lane <= kBlock && mine == slot + lane - 1 && (mine >> 4) == (slot >> 4);
+    const int n = __builtin_ctzll(~(__ballot(goes_on) >> 1));
+    if (!(prev >= 0 && slot == prev + 1 && (slot & 15))) {  // the run begins here
+      const int page = slot >> a.g.page_shift, b = (slot & (a.g.page_tokens - 1)) >> 4;
+      const int64_t block = ((int64_t)page * a.g.Hkv + head) * a.g.blocks_per_page + b;
+      if (task & 1)
+        append_v<CODES, D, IN>(a, i, n, slot & 15, head, block);
+      else
+        append_k<CODES, D, IN>(a, i, n, slot & 15, head, block);
+    }
+    i += n;
+  }
+}
+
+}  // namespace k8
