@@ -1,14 +1,15 @@
 // Attention over the 8-bit cache.
 //
-// With z = q . K8_j (codes), row factor c = |scale| * log2(e) * 2^-k (q is scaled by 2^k into fp16's range, and by the scale's sign),
-// block scales ks, vs and running maximum m, all scores in log2 units:
+// With z = q . K8_j (codes), row factor c = |scale| * log2(e) * 2^-k (q is scaled by 2^k into fp16's range, and by the scale's sign) and
+// block scales ks, vs = 2^ev, all scores in log2 units:
 //
-//   t_j = z * c * ks            (capped, lowered by distance)        w_j = 2^(t_j - m)      l = sum w_j
-//   O   = sum (w_j * vs * 2^-E) V8_j                                 out = O * 2^E / l      lse = ln 2 * (m + log2 l)
+//   t_j = z * c * ks            (capped, lowered by distance)        m = max (t_j + ev_j)        y_j = 2^(t_j + ev_j - m)
+//   l   = sum y_j / vs          O = sum y_j V8_j                     out = O / l                 lse = ln 2 * (m + log2 l)
 //
-// Codes are whole fp16 numbers, so K and V enter the products exactly and the scales, powers of two, outside of them; E is the largest
-// exponent of vs so far, so that what enters as fp16 (the softmax weight) stays within [0, 1].  Its rounding, 2^-12 of each weight, is
-// the only one that fp32 does not see; it is half a bit of an fp16 output.
+// Codes are whole fp16 numbers, so K and V enter the products exactly, and the scales, powers of two, stay outside of them: K's is a
+// factor of the score, V's a term of the exponent, the same for 16 tokens.  The maximum that keeps y_j within [0, 1] is that of what
+// enters the second product, row by row, so that its rounding to fp16, 2^-12 of each y_j, is small against the row's own result
+// whatever the blocks' scales; it is the only rounding that fp32 does not see, half a step of an fp16 output.
 //
 // Both products run transposed, S^T = K Q^T and O^T = V^T P^T, in 32x32x16 steps of a wave over 32 tokens x 32 stacked rows.  What row of
 // the first product a token has is free, and so is the order of dims within it; both are chosen such that
@@ -16,8 +17,8 @@
 //     the products' operands through registers alone, in whole cache lines, with no transposition;
 //   * the scores that a lane gets (16 tokens of one block, one row) are, as fp16, its operand of the second product.
 //
-// k8_attend, few rows (<= 32 stacked): every wave takes blocks of 32 tokens of its own, and the four meet once at the end.
-// Many rows: four waves of 32 rows each take the same tokens; the codes are turned into fp16 once per work-group, by way of LDS.
+// attend_few, <= 32 stacked rows: every wave takes blocks of 32 tokens of its own, and the four meet once at the end.
+// attend_many: four waves of 32 rows each take the same tokens; the codes are turned into fp16 once per work-group, by way of LDS.
 #pragma once
 #include "k8_dev.hpp"
 
@@ -36,26 +37,44 @@ struct AttendArgs {
   const int *slot_position, *row_position;
   const uint64_t* row_see;
   const float* slopes;
-  const int* n_units;
   const Unit* units;
   const Tile* tiles;
   const void* q;
   void* out;
   float* lse;
   float2v* part_ml;  // [partial row][Hkv]: m, l
-  float* part_acc;   // ... [D]: O * 2^E
+  float* part_acc;   // ... [D]: O
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kScaleSpan = 60;  // blocks whose V scale is this many powers of two below the largest take the rest as a factor
 
 __device__ inline float other_half(float x) {  // of lane ^ 32
-  return __shfl_xor(x, 32);
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// Lane i of each row of 16 lanes, for all lanes of the row.  The move stays one of its own: joined by the compiler with the subtraction that
+// uses it (v_subrev_u32 with row_newbcast), every lane got its own value on this chip.
+template <int I>
+__device__ inline int of_row(int x) {
+  int y = __builtin_amdgcn_update_dpp(0, x, 0x150 + I, 0xf, 0xf, false);
+  asm("" : "+v"(y));
+  return y;
+}
+
+template <class F, int... I>
+__device__ inline void each(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ inline void each(F f) {  // f(0) ... f(N - 1), the numbers as constants
+  each(f, std::make_integer_sequence<int, N>{});
 }
 
 // A wave's 32 stacked rows: lane n and n + 32 hold row n, each half of the dims.
 template <int D>
 struct Rows {
-  half8 q[D / 16];
   float c;      // score factor but for ks
   float slope;  // in log2 units
   int token;    // own place
@@ -69,64 +88,74 @@ __device__ inline int64_t row_address(const AttendArgs& a, int s, int head) {  /
 }
 
 template <int D>
-__device__ inline void load_rows(const AttendArgs& a, const Unit& u, int head, int first, Rows<D>& r) {
+__device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head, int first, Rows<D>& r, uint4v (&raw)[D / 16]) {
   const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
   r.real = first + n < u.n_rows;
-  const int s = u.s0 + (r.real ? first + n : 0);
+  const int s = u.s0 + (r.real ? first + n : 0);  // (a lane without a row computes the first one's, times 0)
   const uint4v* p = (const uint4v*)((const uint16_t*)a.q + row_address(a, s, head) * D);
-  uint4v w[D / 16];
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) w[k] = p[(2 * (k >> 1) + half) * 2 + (k & 1)];
+  for (int k = 0; k < D / 16; ++k) raw[k] = p[(2 * (k >> 1) + half) * 2 + (k & 1)];
   r.token = u.pos0 + ((first + n) >> a.g_shift);
   r.see = a.row_see ? a.row_see[s >> a.g_shift] : 0;
   r.position = a.row_position ? a.row_position[s >> a.g_shift] : r.token;
   r.slope = a.slopes ? a.slopes[head * a.g.G + (s & (a.g.G - 1))] * kLog2e : 0.f;
-  float x[D / 16][8];
-  uint32_t amax = 0;
+}
+
+template <int D>
+__device__ inline void finish_rows(const AttendArgs& a, Rows<D>& r, const uint4v (&raw)[D / 16], half8 (&q)[D / 16]) {
+  uint32_t amax = 0;  // largest magnitude: bits without the sign, of either type
 #pragma unroll
   for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t b = (i & 1) ? w[k][i / 2] >> 16 : w[k][i / 2] & 0xffffu;
-      union { uint16_t u; _Float16 h; } c{(uint16_t)b};
-      x[k][i] = a.dtype == kBf16 ? __uint_as_float(b << 16) : (float)c.h;
-      amax = max(amax, __float_as_uint(x[k][i]) & 0x7fffffffu);
-    }
-  amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
+    for (int i = 0; i < 4; ++i) amax = max(max(amax, raw[k][i] & 0x7fffu), raw[k][i] >> 16 & 0x7fffu);
+  amax = max(amax, __float_as_uint(other_half(__uint_as_float(amax))));
+  union { uint16_t u; _Float16 h; } c{(uint16_t)amax};
+  amax = a.dtype == kBf16 ? amax << 16 : __float_as_uint((float)c.h);
   // the largest value comes to [2^14, 2^15): bf16's 8 bits stay whole down to 2^-31 of it, fp16's 11 to 2^-28
   const int up = amax ? min(max(14 + 127 - (int)(amax >> 23), -126), 126) : 0;
-  const float f = r.real ? (a.negate ? -pow2f(up) : pow2f(up)) : 0.f;
+  const float f = !r.real ? 0.f : a.negate ? -pow2f(up) : pow2f(up);
+  if (a.dtype == kBf16) {
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k)
+    for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.q[k][i] = r.real ? (_Float16)(x[k][i] * f) : (_Float16)0.f;
+      for (int i = 0; i < 8; ++i) q[k][i] = (_Float16)(__uint_as_float((i & 1) ? raw[k][i / 2] & 0xffff0000u : raw[k][i / 2] << 16) * f);
+  } else {
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      union { uint4v w; half8 h; } x{raw[k]};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[k][i] = (_Float16)((float)x.h[i] * f);
+    }
+  }
   r.c = a.scale_log2 * pow2f(-up);
 }
 
-// The blocks of a stretch of tokens, lane k the k-th of them: index into the scales (-1: none there), the scales, the first slot / 16.
+// The blocks of a stretch of tokens, lane k the k-th of them: index into the scales (-1: none there), first slot / 16, the scales.
 struct Blocks {
   int at, slot16;
   float ks, vs;
 };
 
-__device__ inline Blocks load_blocks(const AttendArgs& a, int request, int head, int token, int hi) {
-  Blocks b{-1, 0, 0.f, 0.f};
+__device__ inline void find_blocks(const AttendArgs& a, int request, int head, int token, int hi, Blocks& b) {
+  b.at = -1, b.slot16 = 0;
   if (token < hi) {
     const int page = a.table[(int64_t)request * a.g.table_width + (token >> a.g.page_shift)];
     if (page >= 0 && page < a.g.n_pages) {
       const int in = (token & (a.g.page_tokens - 1)) >> 4;
       b.at = (page * a.g.Hkv + head) * a.g.blocks_per_page + in;
       b.slot16 = page * a.g.blocks_per_page + in;
-      b.ks = a.ks[b.at];
-      b.vs = a.vs[b.at];
     }
   }
-  return b;
+}
+
+__device__ inline void load_scales(const AttendArgs& a, Blocks& b) {
+  b.ks = b.at >= 0 ? a.ks[b.at] : 0.f;
+  b.vs = b.at >= 0 ? a.vs[b.at] : 0.f;
 }
 
 // 32 tokens: two blocks.
 struct Pair {
-  int at[2], slot16[2];
+  int at[2];
   float ks[2], vs[2];
 };
 
@@ -135,7 +164,6 @@ __device__ inline Pair pair_of(const Blocks& b, int k) {  // blocks 2k and 2k + 
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     p.at[i] = __builtin_amdgcn_readlane(b.at, 2 * k + i);
-    p.slot16[i] = __builtin_amdgcn_readlane(b.slot16, 2 * k + i);
     p.ks[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b.ks), 2 * k + i));
     p.vs[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b.vs), 2 * k + i));
   }
@@ -143,54 +171,53 @@ __device__ inline Pair pair_of(const Blocks& b, int k) {  // blocks 2k and 2k + 
 }
 
 // The codes of a pair, as this lane's pieces.  Row m = 8a + 4h + b of the first product is token 4a + b of block h.
-template <int D>
-__device__ inline void load_k(const AttendArgs& a, const Pair& p, uint4v (&k)[D / 32]) {
+__device__ inline const uint8_t* k_piece(const AttendArgs& a, int at0, int at1, int D) {
   const int lane = threadIdx.x & 63, m = lane & 31, half = lane >> 5;
-  const int at = max((m & 4) ? p.at[1] : p.at[0], 0);
-  const uint8_t* from = a.k + (int64_t)at * (kBlock * D) + half * 256 + ((m >> 3) * 4 + (m & 3)) * 16;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) k[i] = *(const uint4v*)(from + i * 512);
+  const int at = max((m & 4) ? at1 : at0, 0);
+  return a.k + (int64_t)at * (kBlock * D) + half * 256 + ((m >> 3) * 4 + (m & 3)) * 16;
 }
 
-template <int D>
-__device__ inline void load_v(const AttendArgs& a, const Pair& p, uint4v (&v)[D / 32]) {
-  const int lane = threadIdx.x & 63, half = lane >> 5;
-  const int at = max(half ? p.at[1] : p.at[0], 0);
-  const uint8_t* from = a.v + (int64_t)at * (kBlock * D) + (lane & 31) * 16;
+__device__ inline const uint8_t* v_piece(const AttendArgs& a, int at0, int at1, int D) {
+  const int lane = threadIdx.x & 63;
+  const int at = max((lane & 32) ? at1 : at0, 0);
+  return a.v + (int64_t)at * (kBlock * D) + (lane & 31) * 16;
+}
+
+template <int N>
+__device__ inline void load_pieces(const uint8_t* from, uint4v (&x)[N]) {
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) v[i] = *(const uint4v*)(from + i * 512);
-  if (p.at[0] < 0 || p.at[1] < 0) {  // what is not there must not be NaN: its weight is 0
-    const bool none = (half ? p.at[1] : p.at[0]) < 0;
+  for (int i = 0; i < N; ++i) x[i] = *(const uint4v*)(from + i * 512);
+}
+
+template <int N>
+__device__ inline void drop_absent(int at0, int at1, uint4v (&v)[N]) {  // what is not there must not be NaN: its weight is 0
+  if (at0 < 0 || at1 < 0) {
+    const bool none = ((threadIdx.x & 32) ? at1 : at0) < 0;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) v[i] = none ? uint4v{0, 0, 0, 0} : v[i];
+    for (int i = 0; i < N; ++i) v[i] = none ? uint4v{0, 0, 0, 0} : v[i];
   }
 }
 
-// Which of the lane's 16 tokens (base, base + 1, ...) its row sees, as bits.
-__device__ inline uint32_t visible(const AttendArgs& a, const Unit& u, int hi, int base, int at, int slot16, int token, uint64_t see) {
-  auto below = [](int n) { return n <= 0 ? 0u : n >= kBlock ? 0xffffu : (1u << n) - 1u; };
-  uint32_t bits = below(token + 1 - base);
-  if (a.row_see) {
-    const uint4v t = at >= 0 ? *(const uint4v*)(a.slot_tag + (int64_t)slot16 * kBlock) : uint4v{0, 0, 0, 0};
-    uint32_t tagged = 0;
-    const uint32_t one = (t[0] & 255u) * 0x01010101u;
-    if (__all(t[0] == one && t[1] == one && t[2] == one && t[3] == one)) {
-      tagged = (see >> (one & 63u)) & 1 ? 0xffffu : 0u;
-    } else {
-#pragma unroll
-      for (int i = 0; i < kBlock; ++i) tagged |= (uint32_t)((see >> ((t[i / 4] >> (8 * (i & 3))) & 63u)) & 1) << i;
-    }
-    bits &= tagged;
-  }
-  bits |= below(u.prefix - base);
-  return at >= 0 ? bits & below(hi - base) : 0u;
+// Tag and position of a pair's tokens: lane l holds those of token l & 15 of block l >> 5.
+struct Marks {
+  int tag, position;
+};
+
+__device__ inline Marks load_marks(const AttendArgs& a, const Blocks& b, int k) {
+  const int lane = threadIdx.x & 63;
+  const int s0 = __builtin_amdgcn_readlane(b.slot16, 2 * k), s1 = __builtin_amdgcn_readlane(b.slot16, 2 * k + 1);
+  const int64_t at = (int64_t)((lane & 32) ? s1 : s0) * kBlock + (lane & 15);
+  return Marks{a.row_see ? (int)a.slot_tag[at] & 63 : 0, a.row_position ? a.slot_position[at] : 0};
 }
 
-// Scores of a pair (in the first product's units) -> log2 units, capped, lowered, hidden.
-__device__ inline void finish_scores(const AttendArgs& a, const Unit& u, int hi, int t0, const Pair& p, float c, float slope, int token, int position,
-                                     uint64_t see, bool masked, float16v& s) {
+// Scores of a pair, tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
+// left so where nothing has to be done; else they come out in log2 units and f is 1.
+__device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, int at0, int at1, const Marks& marks, float slope, int token, int position,
+                                     uint64_t see, int first_token, float& f, float16v& s) {
   const int half = (threadIdx.x >> 5) & 1, base = t0 + 16 * half;
-  const float f = c * (half ? p.ks[1] : p.ks[0]);
+  const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || at0 < 0 || at1 < 0;
+  const bool masked = cut || (t0 + 32 > prefix && (a.row_see || ordered));
+  if (!(a.cap_log2 > 0.f) && !a.slopes && !masked) return;
   if (a.cap_log2 > 0.f) {
     // cap * tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap))
     const float g = f * a.cap_in;
@@ -200,33 +227,39 @@ __device__ inline void finish_scores(const AttendArgs& a, const Unit& u, int hi,
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] *= f;
   }
-  const int at = half ? p.at[1] : p.at[0], slot16 = half ? p.slot16[1] : p.slot16[0];
+  f = 1.f;
   if (a.slopes) {
     if (a.row_position) {
-      const int4* pos = (const int4*)(a.slot_position + (int64_t)slot16 * kBlock);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int4 w = pos[i];
-        s[4 * i] -= slope * fabsf((float)(position - w.x));
-        s[4 * i + 1] -= slope * fabsf((float)(position - w.y));
-        s[4 * i + 2] -= slope * fabsf((float)(position - w.z));
-        s[4 * i + 3] -= slope * fabsf((float)(position - w.w));
-      }
+      each<16>([&](auto i) { s[i.value] = fmaf(-slope, fabsf((float)(position - of_row<i.value>(marks.position))), s[i.value]); });
     } else {
+      const float far = (float)(token - base);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] -= slope * fabsf((float)(token - base - i));
+      for (int i = 0; i < 16; ++i) s[i] = fmaf(-slope, fabsf(far - (float)i), s[i]);
     }
   }
-  if (masked) {
-    const uint32_t bits = visible(a, u, hi, base, at, slot16, token, see);
+  if (!masked) return;
+  if (a.row_see && t0 >= prefix && !ordered && !cut) {  // tags alone
+    if (__all(marks.tag == of_row<0>(marks.tag))) {
+      if (!((see >> of_row<0>(marks.tag)) & 1))
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = (bits >> i) & 1 ? s[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[i] = -INFINITY;
+    } else {
+      const int up = 63 - marks.tag;
+      each<16>([&](auto i) { s[i.value] = (int64_t)(see << of_row<i.value>(up)) < 0 ? s[i.value] : -INFINITY; });
+    }
+    return;
   }
-}
-
-// Whether some row of the wave may not see some of the tokens [t0, t1).
-__device__ inline bool needs_mask(const AttendArgs& a, const Unit& u, int hi, int t0, int t1, int first_token) {
-  return t1 > hi || (t1 > u.prefix && (a.row_see || t1 - 1 > first_token));
+  auto below = [](int n) { return n <= 0 ? 0u : n >= kBlock ? 0xffffu : (1u << n) - 1u; };
+  uint32_t bits = below(token + 1 - base);
+  if (a.row_see) {
+    uint32_t tagged = 0;
+    each<16>([&](auto i) { tagged |= (uint32_t)((see >> of_row<i.value>(marks.tag)) & 1) << i.value; });
+    bits &= tagged;
+  }
+  bits |= below(prefix - base);
+  bits = (half ? at1 : at0) >= 0 ? bits & below(hi - base) : 0u;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = (bits >> i) & 1 ? s[i] : -INFINITY;
 }
 
 // Running state of a wave's rows.
@@ -234,7 +267,7 @@ template <int D>
 struct State {
   float16v o[D / 32];
   float m, l;  // l: of this lane's tokens
-  int e;       // exponent of the values in o
+  int e;       // largest exponent of V's scales so far
 };
 
 template <int D>
@@ -243,67 +276,73 @@ __device__ inline void start(State<D>& z) {
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int k = 0; k < 16; ++k) z.o[i][k] = 0.f;
-  z.m = -INFINITY, z.l = 0.f, z.e = -126;
+  z.m = -INFINITY, z.l = 0.f, z.e = kEMin;
 }
 
-// N pairs of blocks under one maximum: their scores become the second product's operands.
+// N pairs of blocks under one maximum: their scores (times f) become the second product's operands.
 template <int D, int N>
-__device__ inline void soften(State<D>& z, float16v (&s)[N], const Pair (&p)[N], half8 (&w)[N][2]) {
+__device__ inline void soften(State<D>& z, float16v (&s)[N], const float (&f)[N], const Pair (&p)[N], half8 (&w)[N][2]) {
   const int half = (threadIdx.x >> 5) & 1;
-  float m = s[0][0];
-  int e = z.e;
-  bool odd = false;
+  float m = -INFINITY, ev[N];
+  bool odd = false;  // a block that reads as NaN, or one whose scale is far below the largest
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) m = fmaxf(m, s[n][i]);
+  for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int x = (int)((__float_as_uint(p[n].vs[b]) >> 23) & 255) - 127;
-      if (x == 128) odd = true;  // the block reads as NaN
-      else if (p[n].at[b] >= 0) e = max(e, x);
+      if (p[n].at[b] >= 0) z.e = x < 128 ? max(z.e, x) : z.e;
     }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    int e[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int x = (int)((__float_as_uint(p[n].vs[b]) >> 23) & 255) - 127;
+      const bool there = p[n].at[b] >= 0;
+      odd |= there && (x == 128 || x < z.e - kScaleSpan);
+      e[b] = there && x < 128 ? max(x, z.e - kScaleSpan) : z.e;
+    }
+    ev[n] = (float)(half ? e[1] : e[0]);
+    float most = s[n][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[n][i]);
+    m = fmaxf(m, fmaf(most, f[n], ev[n]));
   }
   m = fmaxf(m, other_half(m));
   m = fmaxf(m, z.m);
   const float base = m == -INFINITY ? 0.f : m;
-  float alpha = __builtin_amdgcn_exp2f(z.m - base);
+  const float alpha = __builtin_amdgcn_exp2f(z.m - base);
+  z.m = m;
   z.l *= alpha;
-  if (e != z.e) alpha *= z.e - e < -126 ? 0.f : pow2f(z.e - e);
   if (__any(alpha != 1.f)) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int k = 0; k < 16; ++k) z.o[i][k] *= alpha;
   }
-  z.m = m, z.e = e;
-  float sum = 0.f;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const float vs = half ? p[n].vs[1] : p[n].vs[0];
-    const float f = vs * pow2f(-e);
+    const float off = ev[n] - base;
+    float sum = 0.f;
+    float16v y;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float x = __builtin_amdgcn_exp2f(s[n][i] - base);
-      sum += x;
-      float y = x * f;
-      if (odd) y = s[n][i] == -INFINITY ? 0.f : y;
-      s[n][i] = y;
+      y[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off));
+      sum += y[i];
+    }
+    z.l = fmaf(sum, __builtin_amdgcn_exp2f(-ev[n]), z.l);
+    if (odd) {
+      const float vs = half ? p[n].vs[1] : p[n].vs[0], rest = vs * __builtin_amdgcn_exp2f(-ev[n]);
+      const bool there = (half ? p[n].at[1] : p[n].at[0]) >= 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = there && s[n][i] != -INFINITY ? y[i] * rest : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) w[n][i / 8][i % 8] = (_Float16)s[n][i];
+    for (int i = 0; i < 16; i += 2) {
+      const half2v h = __builtin_convertvector((float2v{y[i], y[i + 1]}), half2v);
+      w[n][i / 8][i % 8] = h[0], w[n][i / 8][i % 8 + 1] = h[1];
+    }
   }
-  z.l += sum;
-}
-
-template <int D>
-__device__ inline float16v score(const Rows<D>& r, const half8 (&k)[D / 16]) {
-  float16v s;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[i], r.q[i], s, 0, 0, 0);
-  return s;
 }
 
 __device__ inline void store_out(const AttendArgs& a, int64_t at, float4v x) {  // four neighbouring values of the result
@@ -327,109 +366,163 @@ __device__ inline void store_out(const AttendArgs& a, int64_t at, float4v x) {  
   *(uint2v*)((uint16_t*)a.out + at) = w;
 }
 
+__device__ inline float lse_of(float m, float l) { return l == 0.f ? -INFINITY : kLn2 * (m + __builtin_amdgcn_logf(l)); }
+__device__ inline float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+// One step of a wave: N pairs whose codes are in k and v.  `ahead` is called when k may be overwritten, `behind` when v may.
+template <int CODES, int D, int N, class Ahead, class Behind>
+__device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r, const half8* q, State<D>& z, uint4v (&k)[2][D / 32], uint4v (&v)[2][D / 32],
+                            const Pair (&p)[N], const Marks (&marks)[2], const int (&t0)[2], Ahead ahead, Behind behind) {
+  float16v s[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const half8 row = q[(2 * x + y) * 64 + (threadIdx.x & 63)];
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half8<CODES>(k[n][x][2 * y], k[n][x][2 * y + 1]), row, s[n], 0, 0, 0);
+    }
+  Marks m[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) m[n] = marks[n];
+  ahead();
+  float f[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    f[n] = r.c * ((threadIdx.x & 32) ? p[n].ks[1] : p[n].ks[0]);
+    finish_scores(a, u.prefix, u.hi, t0[n], p[n].at[0], p[n].at[1], m[n], r.slope, r.token, r.position, r.see, u.pos0, f[n], s[n]);
+  }
+  half8 w[N][2];
+  soften<D, N>(z, s, f, p, w);
+  __builtin_amdgcn_sched_barrier(0);  // (V's codes are turned as they are needed: all at once they take 64 registers more)
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    drop_absent(p[n].at[0], p[n].at[1], v[n]);
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x)
+        z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half8<CODES>(v[n][x][2 * y], v[n][x][2 * y + 1]), w[n][y], z.o[x], 0, 0, 0);
+  }
+  behind();
+}
+
 template <int CODES, int D>
 __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, float* lds) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
-  const int n_pairs = (u.hi - u.lo + 31) >> 5;  // of the unit; this wave takes wave, wave + 4, ...
+  const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's: wave, wave + 4, ... of the unit's
   Rows<D> r;
   State<D> z;
   start(z);
-  Blocks b = load_blocks(a, u.request, head, u.lo + (wave + 4 * (lane >> 1)) * 32 + (lane & 1) * 16, u.hi);
-  load_rows<D>(a, u, head, 0, r);
-  const int first_token = u.pos0;
-  uint4v k[D / 32], v[D / 32];
-  Pair p = pair_of(b, 0);
-  if (wave < n_pairs) {
-    load_k<D>(a, p, k);
-    load_v<D>(a, p, v);
+  Blocks b;
+  uint4v k[2][D / 32], v[2][D / 32];
+  Marks marks[2] = {};
+  auto token = [&](int i) { return u.lo + (wave + 4 * i) * 32; };  // first of the wave's i-th pair
+  auto find = [&](int i) { find_blocks(a, u.request, head, token(i + (lane >> 1)) + (lane & 1) * 16, u.hi, b); };
+  auto load_k = [&](int i, int to) {
+    const int x = 2 * (i & 31);
+    load_pieces(k_piece(a, __builtin_amdgcn_readlane(b.at, x), __builtin_amdgcn_readlane(b.at, x + 1), D), k[to]);
+  };
+  auto load_v = [&](int i, int to) {
+    const int x = 2 * (i & 31);
+    load_pieces(v_piece(a, __builtin_amdgcn_readlane(b.at, x), __builtin_amdgcn_readlane(b.at, x + 1), D), v[to]);
+  };
+  // Q's operands lie in LDS, a copy for each wave where its output goes later: in registers they would not leave room for two pairs
+  constexpr int kPitch = D + 4;
+  half8* q = (half8*)(lds + wave * kRows * kPitch);
+  uint4v raw[D / 16];
+  find(0);
+  request_rows<D>(a, u, head, 0, r, raw);
+  if (n_pairs > 0) load_k(0, 0);
+  if (n_pairs > 1) load_k(1, 1);
+  if (n_pairs > 0) {
+    load_v(0, 0);
+    if (n_pairs > 1) load_v(1, 1);
+    load_scales(a, b);
+    marks[0] = load_marks(a, b, 0);
+    if (n_pairs > 1) marks[1] = load_marks(a, b, 1);
   }
-  for (int j = wave, i = 0; j < n_pairs; j += 4) {
-    half8 kk[D / 16];
+  {
+    half8 x[D / 16];
+    finish_rows<D>(a, r, raw, x);
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x) {
-      kk[2 * x] = codes_to_half8<CODES>(k[x][0], k[x][1]);
-      kk[2 * x + 1] = codes_to_half8<CODES>(k[x][2], k[x][3]);
-    }
-    half8 vv[D / 32][2];
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x) {
-      vv[x][0] = codes_to_half8<CODES>(v[x][0], v[x][1]);
-      vv[x][1] = codes_to_half8<CODES>(v[x][2], v[x][3]);
-    }
-    const Pair now[1] = {p};
-    const int t0 = u.lo + j * 32;
-    if (j + 4 < n_pairs) {
-      if (++i == 32) {
-        i = 0;
-        b = load_blocks(a, u.request, head, u.lo + (j + 4 + 4 * (lane >> 1)) * 32 + (lane & 1) * 16, u.hi);
-      }
-      p = pair_of(b, i);
-      load_k<D>(a, p, k);
-      load_v<D>(a, p, v);
-    }
-    float16v s[1] = {score<D>(r, kk)};
-    const bool masked = needs_mask(a, u, u.hi, t0, t0 + 32, first_token) || now[0].at[0] < 0 || now[0].at[1] < 0;
-    finish_scores(a, u, u.hi, t0, now[0], r.c, r.slope, r.token, r.position, r.see, masked, s[0]);
-    half8 w[1][2];
-    soften<D, 1>(z, s, now, w);
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x) {
-      z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vv[x][0], w[0][0], z.o[x], 0, 0, 0);
-      z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vv[x][1], w[0][1], z.o[x], 0, 0, 0);
-    }
+    for (int y = 0; y < D / 16; ++y) q[y * 64 + lane] = x[y];
+  }
+  int i = 0;
+  for (; i + 1 < n_pairs; i += 2) {
+    const Pair p[2] = {pair_of(b, i & 31), pair_of(b, (i + 1) & 31)};
+    const int t0[2] = {token(i), token(i + 1)};
+    step<CODES, D, 2>(a, u, r, q, z, k, v, p, marks, t0,
+      [&] {
+        if (i + 2 >= n_pairs) return;
+        if (((i + 2) & 31) == 0) find(i + 2), load_scales(a, b);
+        load_k(i + 2, 0);
+        marks[0] = load_marks(a, b, (i + 2) & 31);
+        if (i + 3 < n_pairs) load_k(i + 3, 1), marks[1] = load_marks(a, b, (i + 3) & 31);
+      },
+      [&] {
+        if (i + 2 < n_pairs) load_v(i + 2, 0);
+        if (i + 3 < n_pairs) load_v(i + 3, 1);
+      });
+  }
+  if (i < n_pairs) {
+    const Pair p[1] = {pair_of(b, i & 31)};
+    const int t0[2] = {token(i), 0};
+    step<CODES, D, 1>(a, u, r, q, z, k, v, p, marks, t0, [] {}, [] {});
   }
   // the four waves meet
-  constexpr int kPitch = D + 4;
   float* s_o = lds;                                       // [4][32][kPitch]
   float2v* s_ml = (float2v*)(lds + 4 * kRows * kPitch);   // [4][32]
-  float l = z.l + other_half(z.l);
+  const float l = z.l + other_half(z.l);
   if (half == 0) s_ml[wave * kRows + n] = float2v{z.m, l};
-  __syncthreads();
-  float m = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) m = fmaxf(m, s_ml[w * kRows + n][0]);
-  const float base = m == -INFINITY ? 0.f : m;
   if (r.real) {
-    const float f = __builtin_amdgcn_exp2f(z.m - base) * pow2f(z.e);
 #pragma unroll
     for (int x = 0; x < D / 32; ++x)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         *(float4v*)(s_o + (wave * kRows + n) * kPitch + 32 * x + 8 * q + 4 * half) =
-            float4v{z.o[x][4 * q] * f, z.o[x][4 * q + 1] * f, z.o[x][4 * q + 2] * f, z.o[x][4 * q + 3] * f};
+            float4v{z.o[x][4 * q], z.o[x][4 * q + 1], z.o[x][4 * q + 2], z.o[x][4 * q + 3]};
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < u.n_rows * (D / 4); i += 256) {
-    const int row = i / (D / 4), d = i % (D / 4) * 4;
-    float mm = -INFINITY, ll = 0.f;
+  for (int j = threadIdx.x; j < u.n_rows * (D / 4); j += 256) {
+    const int row = j / (D / 4), d = j % (D / 4) * 4;
+    float m = -INFINITY, all = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w * kRows + row][0]);
-    const float bb = mm == -INFINITY ? 0.f : mm;
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, s_ml[w * kRows + row][0]);
+    const float base = m == -INFINITY ? 0.f : m;
     float4v o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      ll += s_ml[w * kRows + row][1] * __builtin_amdgcn_exp2f(s_ml[w * kRows + row][0] - bb);
-      o += *(const float4v*)(s_o + (w * kRows + row) * kPitch + d);
+      const float2v ml = s_ml[w * kRows + row];
+      const float f = __builtin_amdgcn_exp2f(ml[0] - base);
+      all = fmaf(ml[1], f, all);
+      o += *(const float4v*)(s_o + (w * kRows + row) * kPitch + d) * f;
     }
     if (u.part < 0) {
       const int64_t to = row_address(a, u.s0 + row, head);
-      const float inv = ll == 0.f ? 0.f : 1.f / ll;
-      store_out(a, to * D + d, o * inv);
-      if (a.lse && d == 0) a.lse[to] = ll == 0.f ? -INFINITY : kLn2 * (mm + __builtin_amdgcn_logf(ll));
+      store_out(a, to * D + d, o * inverse_of(all));
+      if (a.lse && d == 0) a.lse[to] = lse_of(m, all);
     } else {
       const int64_t to = (int64_t)(u.part + row) * a.g.Hkv + head;
       *(float4v*)(a.part_acc + to * D + d) = o;
-      if (d == 0) a.part_ml[to] = float2v{mm, ll};
+      if (d == 0) a.part_ml[to] = float2v{m, all};
     }
   }
 }
 
-// LDS of the shared tiles: two buffers of 64 tokens, K and V as the products' operands, a lane's 16 bytes next to its neighbour's.
+// LDS of the shared tiles: two buffers of 64 tokens, K and V as the products' operands (a lane's 16 bytes next to its neighbour's), behind
+// them the tokens' tags and positions.
 template <int D>
-constexpr int kTileHalfs = 2 * 64 * D;  // K and V
+constexpr int kTileBytes = 2 * 64 * D * 2;
+constexpr int kMarkBytes = 2 * 64 * 4;
 
 template <int CODES, int D>
-__device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head, half8* lds) {
+__device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head, uint8_t* lds) {
   constexpr int kPieces = D / 64;               // pieces of K, and of V, that a wave brings of a tile
   constexpr int kK = 64 * 2 * (D / 16);         // half8's of K in a tile; as many of V behind
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
@@ -439,29 +532,24 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   State<D> z;
   start(z);
   const bool works = wave * kRows < u.n_rows;
-  Blocks b = load_blocks(a, u.request, head, u.lo + lane * 16, u.hi), ahead = b;
-  load_rows<D>(a, u, head, wave * kRows, r);
+  Blocks b, ahead;
   const int first_token = u.pos0 + (wave * kRows >> a.g_shift);
   const int last_token = u.pos0 + ((min(wave * kRows + kRows, u.n_rows) - 1) >> a.g_shift);
   uint4v k[kPieces], v[kPieces];
+  Marks marks{};
+  const bool marked = a.row_see || a.row_position;
   auto request = [&](int tile) {
-    if (tile && (tile & 15) == 0) ahead = load_blocks(a, u.request, head, u.lo + tile * 64 + lane * 16, u.hi);
-    const Pair p = pair_of(ahead, 2 * (tile & 15) + sub);
-    const int m = lane & 31;
-    const int at = max((m & 4) ? p.at[1] : p.at[0], 0), atv = half ? p.at[1] : p.at[0];
-    const uint8_t* from = a.k + (int64_t)at * (kBlock * D) + half * 256 + ((m >> 3) * 4 + (m & 3)) * 16;
-    const uint8_t* fromv = a.v + (int64_t)max(atv, 0) * (kBlock * D) + (lane & 31) * 16;
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      k[i] = *(const uint4v*)(from + (piece0 + i) * 512);
-      v[i] = *(const uint4v*)(fromv + (piece0 + i) * 512);
-    }
-    if (p.at[0] < 0 || p.at[1] < 0)
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) v[i] = atv < 0 ? uint4v{0, 0, 0, 0} : v[i];
+    if (tile && (tile & 15) == 0) find_blocks(a, u.request, head, u.lo + tile * 64 + lane * 16, u.hi, ahead);
+    const int x = 2 * (tile & 15) + sub;
+    const int at0 = __builtin_amdgcn_readlane(ahead.at, 2 * x), at1 = __builtin_amdgcn_readlane(ahead.at, 2 * x + 1);
+    load_pieces(k_piece(a, at0, at1, D) + piece0 * 512, k);
+    load_pieces(v_piece(a, at0, at1, D) + piece0 * 512, v);
+    if (marked) marks = load_marks(a, ahead, x);
   };
   auto publish = [&](int tile) {
-    half8* to = lds + (tile & 1) * 2 * kK;
+    const int x = 2 * (tile & 15) + sub;
+    drop_absent(__builtin_amdgcn_readlane(ahead.at, 2 * x), __builtin_amdgcn_readlane(ahead.at, 2 * x + 1), v);
+    half8* to = (half8*)(lds + (tile & 1) * kTileBytes<D>);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int step = (sub * (D / 32) + piece0 + i) * 2;
@@ -470,39 +558,61 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
       to[kK + step * 64 + lane] = codes_to_half8<CODES>(v[i][0], v[i][1]);
       to[kK + (step + 1) * 64 + lane] = codes_to_half8<CODES>(v[i][2], v[i][3]);
     }
+    if (marked && !(wave & 1) && !(lane & 16)) {
+      int* m = (int*)(lds + 2 * kTileBytes<D> + (tile & 1) * kMarkBytes) + sub * 32 + half * 16 + (lane & 15);
+      m[0] = marks.tag, m[64] = marks.position;
+    }
   };
+  find_blocks(a, u.request, head, u.lo + lane * 16, u.hi, b);
+  ahead = b;
+  uint4v raw[D / 16];
+  half8 q[D / 16];
+  request_rows<D>(a, u, head, wave * kRows, r, raw);
+  if (n_tiles > 0) request(0);
+  load_scales(a, b);
+  finish_rows<D>(a, r, raw, q);
   if (n_tiles > 0) {
-    request(0);
     publish(0);
     if (n_tiles > 1) request(1);
   }
   __syncthreads();
   for (int j = 0; j < n_tiles; ++j) {
-    if (j && (j & 15) == 0) b = load_blocks(a, u.request, head, u.lo + j * 64 + lane * 16, u.hi);
+    if (j && (j & 15) == 0) {
+      find_blocks(a, u.request, head, u.lo + j * 64 + lane * 16, u.hi, b);
+      load_scales(a, b);
+    }
     const int t0 = u.lo + j * 64;
     if (works && (t0 <= last_token || t0 < u.prefix)) {
-      const half8* from = lds + (j & 1) * 2 * kK;
+      const half8* from = (const half8*)(lds + (j & 1) * kTileBytes<D>);
       const Pair p[2] = {pair_of(b, 2 * (j & 15)), pair_of(b, 2 * (j & 15) + 1)};
       float16v s[2];
 #pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[(x * (D / 16) + i) * 64 + lane], q[i], s[x], 0, 0, 0);
+      float f[2];
+#pragma unroll
       for (int x = 0; x < 2; ++x) {
-        half8 kk[D / 16];
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) kk[i] = from[(x * (D / 16) + i) * 64 + lane];
-        s[x] = score<D>(r, kk);
+        Marks m{};
+        if (marked) {
+          const int* from_m = (const int*)(lds + 2 * kTileBytes<D> + (j & 1) * kMarkBytes) + x * 32 + half * 16 + (lane & 15);
+          m.tag = from_m[0], m.position = from_m[64];
+        }
+        f[x] = r.c * (half ? p[x].ks[1] : p[x].ks[0]);
+        finish_scores(a, u.prefix, u.hi, t0 + 32 * x, p[x].at[0], p[x].at[1], m, r.slope, r.token, r.position, r.see, first_token, f[x], s[x]);
       }
-      const bool gone = p[0].at[0] < 0 || p[0].at[1] < 0 || p[1].at[0] < 0 || p[1].at[1] < 0;
-      const bool masked = gone || needs_mask(a, u, u.hi, t0, t0 + 64, first_token);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) finish_scores(a, u, u.hi, t0 + 32 * x, p[x], r.c, r.slope, r.token, r.position, r.see, masked, s[x]);
       half8 w[2][2];
-      soften<D, 2>(z, s, p, w);
+      soften<D, 2>(z, s, f, p, w);
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i)
+        for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int y = 0; y < 2; ++y)
+          for (int i = 0; i < D / 32; ++i)
             z.o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[kK + ((x * (D / 32) + i) * 2 + y) * 64 + lane], w[x][y], z.o[i], 0, 0, 0);
     }
     if (j + 1 < n_tiles) {
@@ -515,24 +625,22 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   const float l = z.l + other_half(z.l);
   if (!r.real) return;
   const int row = wave * kRows + n;
-  const float up = pow2f(z.e);
   if (u.part < 0) {
     const int64_t to = row_address(a, u.s0 + row, head);
-    const float f = l == 0.f ? 0.f : up / l;
+    const float f = inverse_of(l);
 #pragma unroll
     for (int x = 0; x < D / 32; ++x)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         store_out(a, to * D + 32 * x + 8 * q + 4 * half, float4v{z.o[x][4 * q] * f, z.o[x][4 * q + 1] * f, z.o[x][4 * q + 2] * f, z.o[x][4 * q + 3] * f});
-    if (a.lse && half == 0) a.lse[to] = l == 0.f ? -INFINITY : kLn2 * (z.m + __builtin_amdgcn_logf(l));
+    if (a.lse && half == 0) a.lse[to] = lse_of(z.m, l);
   } else {
     const int64_t to = (int64_t)(u.part + row) * a.g.Hkv + head;
 #pragma unroll
     for (int x = 0; x < D / 32; ++x)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        *(float4v*)(a.part_acc + to * D + 32 * x + 8 * q + 4 * half) =
-            float4v{z.o[x][4 * q] * up, z.o[x][4 * q + 1] * up, z.o[x][4 * q + 2] * up, z.o[x][4 * q + 3] * up};
+        *(float4v*)(a.part_acc + to * D + 32 * x + 8 * q + 4 * half) = float4v{z.o[x][4 * q], z.o[x][4 * q + 1], z.o[x][4 * q + 2], z.o[x][4 * q + 3]};
     if (half == 0) a.part_ml[to] = float2v{z.m, l};
   }
 }
@@ -540,57 +648,66 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
 template <int CODES, int D, bool MANY>
 __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   constexpr int kFewBytes = 4 * kRows * (D + 4) * 4 + 4 * kRows * 8;
-  constexpr int kManyBytes = 2 * kTileHalfs<D> * 2;
+  constexpr int kManyBytes = 2 * kTileBytes<D> + 2 * kMarkBytes;
   __shared__ __attribute__((aligned(16))) uint8_t lds[MANY && kManyBytes > kFewBytes ? kManyBytes : kFewBytes];
-  const int i = blockIdx.x / a.g.Hkv, head = blockIdx.x % a.g.Hkv;
-  if (i >= a.n_units[0]) return;
-  const Unit u = a.units[i];
+  const int head = blockIdx.x % a.g.Hkv;
+  const Unit u = a.units[blockIdx.x / a.g.Hkv];
+  if (u.n_rows == 0) return;
   if (MANY && u.n_rows > kRows)
-    attend_many<CODES, D>(a, u, head, (half8*)lds);
+    attend_many<CODES, D>(a, u, head, lds);
   else
     attend_few<CODES, D>(a, u, head, (float*)lds);
 }
 
-// Joins the partial rows of the tiles whose tokens are split.  Work-group (tile, head, z) takes every gridDim.z-th row; 32 lanes hold a row's
-// parts four dims apiece (D = 128), and the 256 / (D / 4) groups of lanes take a share of the parts each.
+// Joins the partial rows of the tiles whose tokens are split.  D / 4 lanes hold a row, four dims apiece; the 1024 / D such groups of a
+// work-group take a row each where there are few parts, else share a row's parts, two or all of them.
 template <int D>
 __global__ __launch_bounds__(256) void k8_merge(AttendArgs a) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
   __shared__ float4v s_o[kGroups][kLanes];
   __shared__ float s_l[kGroups];
   const int t = blockIdx.x / a.g.Hkv, head = blockIdx.x % a.g.Hkv;
-  if (t >= a.n_units[1]) return;
   const Tile tile = a.tiles[t];
   if (tile.n_parts < 2) return;
   const int group = threadIdx.x / kLanes, d = threadIdx.x % kLanes;
-  for (int row = blockIdx.y; row < tile.n_rows; row += gridDim.y) {
-    const float2v* ml = a.part_ml + ((int64_t)(tile.part + row) * a.g.Hkv + head);
-    const float* acc = a.part_acc + ((int64_t)(tile.part + row) * a.g.Hkv + head) * D;
-    const int64_t step = (int64_t)tile.n_rows * a.g.Hkv;
+  const int share = tile.n_parts <= 8 ? 1 : tile.n_parts <= 32 ? kGroups / 2 : kGroups;  // groups to a row
+  const int rows = kGroups / share;                                                      // rows at a time
+  const int64_t step = (int64_t)tile.n_rows * a.g.Hkv;
+  for (int row0 = blockIdx.y * rows; row0 < tile.n_rows; row0 += gridDim.y * rows) {
+    const int row = row0 + group / share;
+    const bool real = row < tile.n_rows;
+    const int64_t at = (int64_t)(tile.part + (real ? row : 0)) * a.g.Hkv + head;
+    const float2v* ml = a.part_ml + at;
+    const float* acc = a.part_acc + at * D + 4 * d;
     float m = -INFINITY;
-    for (int k = threadIdx.x & 63; k < tile.n_parts; k += 64) m = fmaxf(m, ml[k * step][0]);
-    for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    if (tile.n_parts <= 8) {
+      for (int k = 0; k < tile.n_parts; ++k) m = fmaxf(m, ml[k * step][0]);
+    } else {
+      for (int k = d; k < tile.n_parts; k += kLanes) m = fmaxf(m, ml[k * step][0]);
+      for (int x = kLanes / 2; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    }
     const float base = m == -INFINITY ? 0.f : m;
     float4v o{0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
 #pragma unroll 4
-    for (int k = group; k < tile.n_parts; k += kGroups) {
+    for (int k = group % share; k < tile.n_parts; k += share) {
       const float2v x = ml[k * step];
       const float f = __builtin_amdgcn_exp2f(x[0] - base);
-      l += x[1] * f;
-      o += *(const float4v*)(acc + k * step * D + 4 * d) * f;
+      l = fmaf(x[1], f, l);
+      o += *(const float4v*)(acc + k * step * D) * f;
     }
-    s_o[group][d] = o;
-    if (d == 0) s_l[group] = l;
-    __syncthreads();
-    if (group == 0) {
-      for (int x = 1; x < kGroups; ++x) o += s_o[x][d], l += s_l[x];
-      const int64_t to = row_address(a, tile.s0 + row, head);
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      store_out(a, to * D + 4 * d, o * inv);
-      if (a.lse && d == 0) a.lse[to] = l == 0.f ? -INFINITY : kLn2 * (m + __builtin_amdgcn_logf(l));
+    if (share > 1) {
+      __syncthreads();
+      s_o[group][d] = o;
+      if (d == 0) s_l[group] = l;
+      __syncthreads();
+      if (group % share) continue;
+      for (int x = 1; x < share; ++x) o += s_o[group + x][d], l += s_l[group + x];
     }
-    __syncthreads();
+    if (!real) continue;
+    const int64_t to = row_address(a, tile.s0 + row, head);
+    store_out(a, to * D + 4 * d, o * inverse_of(l));
+    if (a.lse && d == 0) a.lse[to] = lse_of(m, l);
   }
 }
 

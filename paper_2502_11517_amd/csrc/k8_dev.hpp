@@ -4,6 +4,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <utility>
+
 namespace k8 {
 
 constexpr int kBlock = 16;           // tokens under one scale

@@ -15,7 +15,6 @@ struct PlanArgs {
   int capacity;   // units that the chip takes at once
   int max_units, max_tiles, max_part_rows;
   const int *length, *row_offsets, *prefix_len, *slot;
-  int* n_units;   // workspace: number of units, number of tiles
   Unit* units;
   Tile* tiles;
   int* w_tiles;   // workspace, n_requests + 1: tiles of the requests up to and including this one
@@ -111,10 +110,9 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
     n_units += all;
     n_part_rows += all_rows;
   }
-  if (tid == 0) {
-    a.n_units[0] = min(n_units, a.max_units);
-    a.n_units[1] = n_tiles;
-  }
+  // what the launches of k8_attend and k8_merge go over beyond that is empty
+  for (int j = min(n_units, a.max_units) + tid; j < a.max_units; j += NT) a.units[j] = Unit{};
+  for (int j = n_tiles + tid; j < a.max_tiles; j += NT) a.tiles[j] = Tile{};
 }
 
 }  // namespace k8

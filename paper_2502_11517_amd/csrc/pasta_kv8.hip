@@ -28,7 +28,7 @@ struct pasta_kv8 {
   pasta_kv8_config cfg{};
   k8::Geometry g{};
   // workspace
-  int *kept = nullptr, *old_pages = nullptr, *take = nullptr, *top = nullptr, *n_units = nullptr, *tiles_upto = nullptr;
+  int *kept = nullptr, *old_pages = nullptr, *take = nullptr, *top = nullptr, *tiles_upto = nullptr;
   k8::Unit* units = nullptr;
   k8::Tile* tiles = nullptr;
   k8::float2v* part_ml = nullptr;
@@ -88,7 +88,6 @@ uint64_t lay_out(const pasta_kv8_config& c, pasta_kv8* h) {
   take(h->old_pages, c.max_requests);
   take(h->take, c.max_requests);
   take(h->top, 1);
-  take(h->n_units, 2);
   take(h->tiles_upto, c.max_requests + 1);
   take(h->units, b.units);
   take(h->tiles, b.tiles);
@@ -226,7 +225,7 @@ extern "C" int32_t pasta_kv8_plan(pasta_kv8* h, const pasta_kv8_plan_args* a) {
   k.g = h->g, k.n_requests = a->n_requests, k.n_rows = a->n_rows, k.wide = h->plan_wide, k.capacity = (int)h->plan.capacity;
   k.max_units = (int)h->plan.units, k.max_tiles = (int)h->plan.tiles, k.max_part_rows = (int)h->plan.part_rows;
   k.length = a->length, k.row_offsets = a->row_offsets, k.prefix_len = a->prefix_len, k.slot = a->slot;
-  k.n_units = h->n_units, k.units = h->units, k.tiles = h->tiles, k.w_tiles = h->tiles_upto;
+  k.units = h->units, k.tiles = h->tiles, k.w_tiles = h->tiles_upto;
   hipStream_t s = (hipStream_t)c.hip_stream;
   if (h->plan.tiles <= 64 && a->n_requests < 64)
     k8::k8_plan<64><<<1, 64, 0, s>>>(k);
@@ -273,7 +272,7 @@ extern "C" int32_t pasta_kv8_attend(pasta_kv8* h, const pasta_kv8_attend_args* a
   k.ks = c.k_scale + at, k.vs = c.v_scale + at;
   k.table = c.page_table, k.slot_tag = c.slot_tag, k.slot_position = c.slot_position;
   k.row_position = a->row_position, k.row_see = a->row_see, k.slopes = a->slopes;
-  k.n_units = h->n_units, k.units = h->units, k.tiles = h->tiles;
+  k.units = h->units, k.tiles = h->tiles;
   k.q = a->q, k.out = a->out, k.lse = a->lse, k.part_ml = h->part_ml, k.part_acc = h->part_acc;
   hipStream_t s = (hipStream_t)c.hip_stream;
   const int64_t groups = h->plan.units * c.n_kv_heads;
@@ -284,7 +283,7 @@ extern "C" int32_t pasta_kv8_attend(pasta_kv8* h, const pasta_kv8_attend_args* a
     c.head_dim == 128 ? launch_attend<k8::kInt8, 128>(k, many, groups, s) : launch_attend<k8::kInt8, 64>(k, many, groups, s);
   if ((int64_t)c.pages_per_request * c.page_tokens > k8::kChunkTokens) {  // no tile is split otherwise
     const int64_t tiles = h->plan.tiles * c.n_kv_heads;
-    int64_t split = (1024 + tiles - 1) / tiles;
+    int64_t split = (2048 + tiles - 1) / tiles;  // work-groups to a tile: rows, one by one where there are so few tiles
     if (split > h->plan.merge_rows) split = h->plan.merge_rows;
     const dim3 grid((unsigned)tiles, (unsigned)split);
     if (c.head_dim == 128)
