@@ -33,6 +33,9 @@ struct AttendArgs {
   const uint8_t *k, *v;
   const float *ks, *vs;
   const int* table;
+  // Arrays that the call does without are replaced by others that are as long, so that their loads need no branches (each of which would
+  // wait for everything under way); the flags say whether what comes of them counts.
+  bool tagged, placed, lowered;  // row_see, row_position, slopes are given
   const uint8_t* slot_tag;
   const int *slot_position, *row_position;
   const uint64_t* row_see;
@@ -87,7 +90,7 @@ __device__ inline int64_t row_address(const AttendArgs& a, int s, int head) {  /
   return (int64_t)(s >> a.g_shift) * a.Hq + head * a.g.G + (s & (a.g.G - 1));
 }
 
-template <int D>
+template <int D, bool MARKS>
 __device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head, int first, Rows<D>& r, uint4v (&raw)[D / 16]) {
   const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
   r.real = first + n < u.n_rows;
@@ -96,9 +99,13 @@ __device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) raw[k] = p[(2 * (k >> 1) + half) * 2 + (k & 1)];
   r.token = u.pos0 + ((first + n) >> a.g_shift);
-  r.see = a.row_see ? a.row_see[s >> a.g_shift] : 0;
-  r.position = a.row_position ? a.row_position[s >> a.g_shift] : r.token;
-  r.slope = a.slopes ? a.slopes[head * a.g.G + (s & (a.g.G - 1))] * kLog2e : 0.f;
+  r.slope = a.slopes[head * a.g.G + (s & (a.g.G - 1))];
+  if constexpr (MARKS) {
+    r.see = a.row_see[s >> a.g_shift];
+    r.position = a.row_position[s >> a.g_shift];
+  } else {
+    r.see = 0, r.position = 0;
+  }
 }
 
 template <int D>
@@ -128,6 +135,7 @@ __device__ inline void finish_rows(const AttendArgs& a, Rows<D>& r, const uint4v
     }
   }
   r.c = a.scale_log2 * pow2f(-up);
+  r.slope *= kLog2e;
 }
 
 // The blocks of a stretch of tokens, lane k the k-th of them: index into the scales (-1: none there), first slot / 16, the scales.
@@ -136,21 +144,25 @@ struct Blocks {
   float ks, vs;
 };
 
+__device__ inline int load_page(const AttendArgs& a, int request, int token, int hi) {
+  const int t = max(min(token, hi - 1), 0);
+  return a.table[(int64_t)request * a.g.table_width + (t >> a.g.page_shift)];
+}
+
+__device__ inline void on_page(const AttendArgs& a, int page, int head, int token, int hi, Blocks& b) {
+  const bool there = token < hi && page >= 0 && page < a.g.n_pages;
+  const int in = (token & (a.g.page_tokens - 1)) >> 4;
+  b.at = there ? (page * a.g.Hkv + head) * a.g.blocks_per_page + in : -1;
+  b.slot16 = there ? page * a.g.blocks_per_page + in : 0;
+}
+
 __device__ inline void find_blocks(const AttendArgs& a, int request, int head, int token, int hi, Blocks& b) {
-  b.at = -1, b.slot16 = 0;
-  if (token < hi) {
-    const int page = a.table[(int64_t)request * a.g.table_width + (token >> a.g.page_shift)];
-    if (page >= 0 && page < a.g.n_pages) {
-      const int in = (token & (a.g.page_tokens - 1)) >> 4;
-      b.at = (page * a.g.Hkv + head) * a.g.blocks_per_page + in;
-      b.slot16 = page * a.g.blocks_per_page + in;
-    }
-  }
+  on_page(a, load_page(a, request, token, hi), head, token, hi, b);
 }
 
 __device__ inline void load_scales(const AttendArgs& a, Blocks& b) {
-  b.ks = b.at >= 0 ? a.ks[b.at] : 0.f;
-  b.vs = b.at >= 0 ? a.vs[b.at] : 0.f;
+  b.ks = a.ks[max(b.at, 0)];  // (those of an absent block are not looked at, or multiply scores that are hidden)
+  b.vs = a.vs[max(b.at, 0)];
 }
 
 // 32 tokens: two blocks.
@@ -207,17 +219,18 @@ __device__ inline Marks load_marks(const AttendArgs& a, const Blocks& b, int k) 
   const int lane = threadIdx.x & 63;
   const int s0 = __builtin_amdgcn_readlane(b.slot16, 2 * k), s1 = __builtin_amdgcn_readlane(b.slot16, 2 * k + 1);
   const int64_t at = (int64_t)((lane & 32) ? s1 : s0) * kBlock + (lane & 15);
-  return Marks{a.row_see ? (int)a.slot_tag[at] & 63 : 0, a.row_position ? a.slot_position[at] : 0};
+  return Marks{(int)a.slot_tag[at], a.slot_position[at]};
 }
 
 // Scores of a pair, tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
 // left so where nothing has to be done; else they come out in log2 units and f is 1.
+template <bool MARKS>
 __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, int at0, int at1, const Marks& marks, float slope, int token, int position,
                                      uint64_t see, int first_token, float& f, float16v& s) {
   const int half = (threadIdx.x >> 5) & 1, base = t0 + 16 * half;
   const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || at0 < 0 || at1 < 0;
-  const bool masked = cut || (t0 + 32 > prefix && (a.row_see || ordered));
-  if (!(a.cap_log2 > 0.f) && !a.slopes && !masked) return;
+  const bool masked = cut || (t0 + 32 > prefix && ((MARKS && a.tagged) || ordered));
+  if (!(a.cap_log2 > 0.f) && !a.lowered && !masked) return;
   if (a.cap_log2 > 0.f) {
     // cap * tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap))
     const float g = f * a.cap_in;
@@ -228,8 +241,8 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     for (int i = 0; i < 16; ++i) s[i] *= f;
   }
   f = 1.f;
-  if (a.slopes) {
-    if (a.row_position) {
+  if (a.lowered) {
+    if (MARKS && a.placed) {
       each<16>([&](auto i) { s[i.value] = fmaf(-slope, fabsf((float)(position - of_row<i.value>(marks.position))), s[i.value]); });
     } else {
       const float far = (float)(token - base);
@@ -238,22 +251,24 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     }
   }
   if (!masked) return;
-  if (a.row_see && t0 >= prefix && !ordered && !cut) {  // tags alone
-    if (__all(marks.tag == of_row<0>(marks.tag))) {
-      if (!((see >> of_row<0>(marks.tag)) & 1))
+  if (MARKS && a.tagged && t0 >= prefix && !ordered && !cut) {  // tags alone
+    const int first = of_row<0>(marks.tag);
+    if (__all(marks.tag == first)) {
+      if (!((see >> (first & 63)) & 1))
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = -INFINITY;
     } else {
-      const int up = 63 - marks.tag;
+      const int up = 63 - (marks.tag & 63);
       each<16>([&](auto i) { s[i.value] = (int64_t)(see << of_row<i.value>(up)) < 0 ? s[i.value] : -INFINITY; });
     }
     return;
   }
   auto below = [](int n) { return n <= 0 ? 0u : n >= kBlock ? 0xffffu : (1u << n) - 1u; };
   uint32_t bits = below(token + 1 - base);
-  if (a.row_see) {
+  if (MARKS && a.tagged) {
     uint32_t tagged = 0;
-    each<16>([&](auto i) { tagged |= (uint32_t)((see >> of_row<i.value>(marks.tag)) & 1) << i.value; });
+    const int tag = marks.tag & 63;
+    each<16>([&](auto i) { tagged |= (uint32_t)((see >> of_row<i.value>(tag)) & 1) << i.value; });
     bits &= tagged;
   }
   bits |= below(prefix - base);
@@ -370,7 +385,7 @@ __device__ inline float lse_of(float m, float l) { return l == 0.f ? -INFINITY :
 __device__ inline float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // One step of a wave: N pairs whose codes are in k and v.  `ahead` is called when k may be overwritten, `behind` when v may.
-template <int CODES, int D, int N, class Ahead, class Behind>
+template <int CODES, int D, bool MARKS, int N, class Ahead, class Behind>
 __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r, const half8* q, State<D>& z, uint4v (&k)[2][D / 32], uint4v (&v)[2][D / 32],
                             const Pair (&p)[N], const Marks (&marks)[2], const int (&t0)[2], Ahead ahead, Behind behind) {
   float16v s[N];
@@ -395,7 +410,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     f[n] = r.c * ((threadIdx.x & 32) ? p[n].ks[1] : p[n].ks[0]);
-    finish_scores(a, u.prefix, u.hi, t0[n], p[n].at[0], p[n].at[1], m[n], r.slope, r.token, r.position, r.see, u.pos0, f[n], s[n]);
+    finish_scores<MARKS>(a, u.prefix, u.hi, t0[n], p[n].at[0], p[n].at[1], m[n], r.slope, r.token, r.position, r.see, u.pos0, f[n], s[n]);
   }
   half8 w[N][2];
   soften<D, N>(z, s, f, p, w);
@@ -412,7 +427,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
   behind();
 }
 
-template <int CODES, int D>
+template <int CODES, int D, bool MARKS>
 __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, float* lds) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
   const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's: wave, wave + 4, ... of the unit's
@@ -436,17 +451,18 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
   constexpr int kPitch = D + 4;
   half8* q = (half8*)(lds + wave * kRows * kPitch);
   uint4v raw[D / 16];
-  find(0);
-  request_rows<D>(a, u, head, 0, r, raw);
-  if (n_pairs > 0) load_k(0, 0);
-  if (n_pairs > 1) load_k(1, 1);
-  if (n_pairs > 0) {
-    load_v(0, 0);
-    if (n_pairs > 1) load_v(1, 1);
-    load_scales(a, b);
-    marks[0] = load_marks(a, b, 0);
-    if (n_pairs > 1) marks[1] = load_marks(a, b, 1);
-  }
+  // (the page is the first thing asked for, and everything else asked for before anything is waited for: loads come back in their order)
+  const int page = load_page(a, u.request, token(lane >> 1) + (lane & 1) * 16, u.hi);
+  __builtin_amdgcn_sched_barrier(0);
+  request_rows<D, MARKS>(a, u, head, 0, r, raw);
+  __builtin_amdgcn_sched_barrier(0);
+  on_page(a, page, head, token(lane >> 1) + (lane & 1) * 16, u.hi, b);
+  // (where the wave has fewer than two pairs, block 0 is read in their place)
+  load_scales(a, b);
+  if constexpr (MARKS) marks[0] = load_marks(a, b, 0), marks[1] = load_marks(a, b, 1);
+  load_k(0, 0), load_k(1, 1);
+  load_v(0, 0), load_v(1, 1);
+  __builtin_amdgcn_sched_barrier(0);
   {
     half8 x[D / 16];
     finish_rows<D>(a, r, raw, x);
@@ -457,23 +473,21 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
   for (; i + 1 < n_pairs; i += 2) {
     const Pair p[2] = {pair_of(b, i & 31), pair_of(b, (i + 1) & 31)};
     const int t0[2] = {token(i), token(i + 1)};
-    step<CODES, D, 2>(a, u, r, q, z, k, v, p, marks, t0,
+    step<CODES, D, MARKS, 2>(a, u, r, q, z, k, v, p, marks, t0,
       [&] {
         if (i + 2 >= n_pairs) return;
         if (((i + 2) & 31) == 0) find(i + 2), load_scales(a, b);
-        load_k(i + 2, 0);
-        marks[0] = load_marks(a, b, (i + 2) & 31);
-        if (i + 3 < n_pairs) load_k(i + 3, 1), marks[1] = load_marks(a, b, (i + 3) & 31);
+        if constexpr (MARKS) marks[0] = load_marks(a, b, (i + 2) & 31), marks[1] = load_marks(a, b, (i + 3) & 31);
+        load_k(i + 2, 0), load_k(i + 3, 1);
       },
       [&] {
-        if (i + 2 < n_pairs) load_v(i + 2, 0);
-        if (i + 3 < n_pairs) load_v(i + 3, 1);
+        if (i + 2 < n_pairs) load_v(i + 2, 0), load_v(i + 3, 1);
       });
   }
   if (i < n_pairs) {
     const Pair p[1] = {pair_of(b, i & 31)};
     const int t0[2] = {token(i), 0};
-    step<CODES, D, 1>(a, u, r, q, z, k, v, p, marks, t0, [] {}, [] {});
+    step<CODES, D, MARKS, 1>(a, u, r, q, z, k, v, p, marks, t0, [] {}, [] {});
   }
   // the four waves meet
   float* s_o = lds;                                       // [4][32][kPitch]
@@ -521,7 +535,7 @@ template <int D>
 constexpr int kTileBytes = 2 * 64 * D * 2;
 constexpr int kMarkBytes = 2 * 64 * 4;
 
-template <int CODES, int D>
+template <int CODES, int D, bool MARKS>
 __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head, uint8_t* lds) {
   constexpr int kPieces = D / 64;               // pieces of K, and of V, that a wave brings of a tile
   constexpr int kK = 64 * 2 * (D / 16);         // half8's of K in a tile; as many of V behind
@@ -537,14 +551,13 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   const int last_token = u.pos0 + ((min(wave * kRows + kRows, u.n_rows) - 1) >> a.g_shift);
   uint4v k[kPieces], v[kPieces];
   Marks marks{};
-  const bool marked = a.row_see || a.row_position;
   auto request = [&](int tile) {
     if (tile && (tile & 15) == 0) find_blocks(a, u.request, head, u.lo + tile * 64 + lane * 16, u.hi, ahead);
     const int x = 2 * (tile & 15) + sub;
     const int at0 = __builtin_amdgcn_readlane(ahead.at, 2 * x), at1 = __builtin_amdgcn_readlane(ahead.at, 2 * x + 1);
     load_pieces(k_piece(a, at0, at1, D) + piece0 * 512, k);
     load_pieces(v_piece(a, at0, at1, D) + piece0 * 512, v);
-    if (marked) marks = load_marks(a, ahead, x);
+    if constexpr (MARKS) marks = load_marks(a, ahead, x);
   };
   auto publish = [&](int tile) {
     const int x = 2 * (tile & 15) + sub;
@@ -558,7 +571,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
       to[kK + step * 64 + lane] = codes_to_half8<CODES>(v[i][0], v[i][1]);
       to[kK + (step + 1) * 64 + lane] = codes_to_half8<CODES>(v[i][2], v[i][3]);
     }
-    if (marked && !(wave & 1) && !(lane & 16)) {
+    if (MARKS && !(wave & 1) && !(lane & 16)) {
       int* m = (int*)(lds + 2 * kTileBytes<D> + (tile & 1) * kMarkBytes) + sub * 32 + half * 16 + (lane & 15);
       m[0] = marks.tag, m[64] = marks.position;
     }
@@ -567,7 +580,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   ahead = b;
   uint4v raw[D / 16];
   half8 q[D / 16];
-  request_rows<D>(a, u, head, wave * kRows, r, raw);
+  request_rows<D, MARKS>(a, u, head, wave * kRows, r, raw);
   if (n_tiles > 0) request(0);
   load_scales(a, b);
   finish_rows<D>(a, r, raw, q);
@@ -598,12 +611,12 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         Marks m{};
-        if (marked) {
+        if constexpr (MARKS) {
           const int* from_m = (const int*)(lds + 2 * kTileBytes<D> + (j & 1) * kMarkBytes) + x * 32 + half * 16 + (lane & 15);
           m.tag = from_m[0], m.position = from_m[64];
         }
         f[x] = r.c * (half ? p[x].ks[1] : p[x].ks[0]);
-        finish_scores(a, u.prefix, u.hi, t0 + 32 * x, p[x].at[0], p[x].at[1], m, r.slope, r.token, r.position, r.see, first_token, f[x], s[x]);
+        finish_scores<MARKS>(a, u.prefix, u.hi, t0 + 32 * x, p[x].at[0], p[x].at[1], m, r.slope, r.token, r.position, r.see, first_token, f[x], s[x]);
       }
       half8 w[2][2];
       soften<D, 2>(z, s, f, p, w);
@@ -645,18 +658,19 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   }
 }
 
-template <int CODES, int D, bool MANY>
+template <int CODES, int D, bool MANY, bool MARKS>
 __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   constexpr int kFewBytes = 4 * kRows * (D + 4) * 4 + 4 * kRows * 8;
   constexpr int kManyBytes = 2 * kTileBytes<D> + 2 * kMarkBytes;
   __shared__ __attribute__((aligned(16))) uint8_t lds[MANY && kManyBytes > kFewBytes ? kManyBytes : kFewBytes];
   const int head = blockIdx.x % a.g.Hkv;
   const Unit u = a.units[blockIdx.x / a.g.Hkv];
+  asm volatile("" ::"s"(u.request), "s"(u.s0), "s"(u.pos0), "s"(u.lo), "s"(u.hi), "s"(u.prefix), "s"(u.part));  // (one load, ahead of the branch)
   if (u.n_rows == 0) return;
   if (MANY && u.n_rows > kRows)
-    attend_many<CODES, D>(a, u, head, lds);
+    attend_many<CODES, D, MARKS>(a, u, head, lds);
   else
-    attend_few<CODES, D>(a, u, head, (float*)lds);
+    attend_few<CODES, D, MARKS>(a, u, head, (float*)lds);
 }
 
 // Joins the partial rows of the tiles whose tokens are split.  D / 4 lanes hold a row, four dims apiece; the 1024 / D such groups of a

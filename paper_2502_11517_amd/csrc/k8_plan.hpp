@@ -49,7 +49,7 @@ __device__ inline Unit tile_of(const PlanArgs& a, int j) {
   const RequestTiles q = request_tiles(a, r);
   const int t = j - (a.w_tiles[r] - q.n_tiles);
   const int first = t * q.tile_rows, stacked = q.n * a.g.G;
-  u.request = min(r, a.n_requests - 1);
+  u.request = max(min(r, a.n_requests - 1), 0);
   u.s0 = q.row0 * a.g.G + first;
   u.n_rows = min(stacked - first, q.tile_rows);
   u.pos0 = q.length - q.n + first / a.g.G;

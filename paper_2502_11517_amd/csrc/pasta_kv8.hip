@@ -240,10 +240,11 @@ namespace {
 
 template <int CODES, int D>
 void launch_attend(const k8::AttendArgs& k, bool many, int64_t groups, hipStream_t s) {
+  const bool marks = k.tagged || k.placed;
   if (many)
-    k8::k8_attend<CODES, D, true><<<(unsigned)groups, 256, 0, s>>>(k);
+    marks ? k8::k8_attend<CODES, D, true, true><<<(unsigned)groups, 256, 0, s>>>(k) : k8::k8_attend<CODES, D, true, false><<<(unsigned)groups, 256, 0, s>>>(k);
   else
-    k8::k8_attend<CODES, D, false><<<(unsigned)groups, 256, 0, s>>>(k);
+    marks ? k8::k8_attend<CODES, D, false, true><<<(unsigned)groups, 256, 0, s>>>(k) : k8::k8_attend<CODES, D, false, false><<<(unsigned)groups, 256, 0, s>>>(k);
 }
 
 }  // namespace
@@ -272,6 +273,11 @@ extern "C" int32_t pasta_kv8_attend(pasta_kv8* h, const pasta_kv8_attend_args* a
   k.ks = c.k_scale + at, k.vs = c.v_scale + at;
   k.table = c.page_table, k.slot_tag = c.slot_tag, k.slot_position = c.slot_position;
   k.row_position = a->row_position, k.row_see = a->row_see, k.slopes = a->slopes;
+  k.tagged = a->row_see, k.placed = a->row_position, k.lowered = a->slopes;
+  // stand-ins: a slot has at least 64 bytes of codes, a row of q at least 128, and q has at least 128 a head
+  if (!k.tagged) k.row_see = (const uint64_t*)a->q, k.slot_tag = (const uint8_t*)c.k_codes;
+  if (!k.placed) k.row_position = (const int*)a->q, k.slot_position = (const int*)c.k_codes;
+  if (!k.lowered) k.slopes = (const float*)a->q;
   k.units = h->units, k.tiles = h->tiles;
   k.q = a->q, k.out = a->out, k.lse = a->lse, k.part_ml = h->part_ml, k.part_acc = h->part_acc;
   hipStream_t s = (hipStream_t)c.hip_stream;
