@@ -138,10 +138,12 @@ __device__ inline void finish_rows(const AttendArgs& a, Rows<D>& r, const uint4v
   r.slope *= kLog2e;
 }
 
-// The blocks of a stretch of tokens, lane k the k-th of them: index into the scales (-1: none there), first slot / 16, the scales.
+// The blocks of a stretch of tokens, lane k the k-th of them: index into the scales (-1: none there), first slot / 16, K's scale, the exponent of
+// V's as it enters the scores, and, for the wave, which are absent and which need more than that exponent.
 struct Blocks {
   int at, slot16;
-  float ks, vs;
+  float ks, vs, ev;
+  uint64_t absent, odd;
 };
 
 __device__ inline int load_page(const AttendArgs& a, int request, int token, int hi) {
@@ -161,24 +163,41 @@ __device__ inline void find_blocks(const AttendArgs& a, int request, int head, i
 }
 
 __device__ inline void load_scales(const AttendArgs& a, Blocks& b) {
-  b.ks = a.ks[max(b.at, 0)];  // (those of an absent block are not looked at, or multiply scores that are hidden)
+  b.ks = a.ks[max(b.at, 0)];
   b.vs = a.vs[max(b.at, 0)];
 }
 
-// 32 tokens: two blocks.
+// `most`: the largest exponent of V's scales so far; these blocks' are added to it.
+__device__ inline void finish_scales(Blocks& b, int& most) {
+  const int x = (int)((__float_as_uint(b.vs) >> 23) & 255) - 127;
+  const bool there = b.at >= 0, nan = x == 128;
+  int e = there && !nan ? x : kEMin;
+  for (int d = 32; d; d >>= 1) e = max(e, __shfl_xor(e, d));
+  most = max(most, __builtin_amdgcn_readfirstlane(e));
+  e = there && !nan ? max(x, most - kScaleSpan) : most;
+  b.ev = (float)e;
+  b.absent = __ballot(!there);
+  b.odd = __ballot(there && (nan || x < most - kScaleSpan));
+}
+
+// 32 tokens: two blocks, of which the lane has to do with the one that its half of the wave holds scores of.
 struct Pair {
-  int at[2];
-  float ks[2], vs[2];
+  float ks, ev;
+  float vs;       // only if odd
+  bool cut, odd;  // one of the two is absent; one of the two is odd
+  bool there;     // the lane's
 };
 
+__device__ inline float of_lane(float x, int from) { return __uint_as_float(__builtin_amdgcn_ds_bpermute(from * 4, __float_as_uint(x))); }
+
 __device__ inline Pair pair_of(const Blocks& b, int k) {  // blocks 2k and 2k + 1 of the wave's lanes; k the same for all lanes
+  const int mine = 2 * k + ((threadIdx.x >> 5) & 1);
   Pair p;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    p.at[i] = __builtin_amdgcn_readlane(b.at, 2 * k + i);
-    p.ks[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b.ks), 2 * k + i));
-    p.vs[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(b.vs), 2 * k + i));
-  }
+  p.ks = of_lane(b.ks, mine), p.ev = of_lane(b.ev, mine);
+  p.cut = (b.absent >> (2 * k)) & 3, p.odd = (b.odd >> (2 * k)) & 3;
+  p.there = !((b.absent >> mine) & 1);
+  p.vs = 0.f;
+  if (p.odd) p.vs = of_lane(b.vs, mine);
   return p;
 }
 
@@ -202,11 +221,10 @@ __device__ inline void load_pieces(const uint8_t* from, uint4v (&x)[N]) {
 }
 
 template <int N>
-__device__ inline void drop_absent(int at0, int at1, uint4v (&v)[N]) {  // what is not there must not be NaN: its weight is 0
-  if (at0 < 0 || at1 < 0) {
-    const bool none = ((threadIdx.x & 32) ? at1 : at0) < 0;
+__device__ inline void drop_absent(bool cut, bool there, uint4v (&v)[N]) {  // what is not there must not be NaN: its weight is 0
+  if (cut) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = none ? uint4v{0, 0, 0, 0} : v[i];
+    for (int i = 0; i < N; ++i) v[i] = there ? v[i] : uint4v{0, 0, 0, 0};
   }
 }
 
@@ -225,10 +243,10 @@ __device__ inline Marks load_marks(const AttendArgs& a, const Blocks& b, int k) 
 // Scores of a pair, tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
 // left so where nothing has to be done; else they come out in log2 units and f is 1.
 template <bool MARKS>
-__device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, int at0, int at1, const Marks& marks, float slope, int token, int position,
+__device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, const Pair& p, const Marks& marks, float slope, int token, int position,
                                      uint64_t see, int first_token, float& f, float16v& s) {
   const int half = (threadIdx.x >> 5) & 1, base = t0 + 16 * half;
-  const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || at0 < 0 || at1 < 0;
+  const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || p.cut;
   const bool masked = cut || (t0 + 32 > prefix && ((MARKS && a.tagged) || ordered));
   if (!(a.cap_log2 > 0.f) && !a.lowered && !masked) return;
   if (a.cap_log2 > 0.f) {
@@ -272,7 +290,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     bits &= tagged;
   }
   bits |= below(prefix - base);
-  bits = (half ? at1 : at0) >= 0 ? bits & below(hi - base) : 0u;
+  bits = p.there ? bits & below(hi - base) : 0u;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = (bits >> i) & 1 ? s[i] : -INFINITY;
 }
@@ -282,7 +300,7 @@ template <int D>
 struct State {
   float16v o[D / 32];
   float m, l;  // l: of this lane's tokens
-  int e;       // largest exponent of V's scales so far
+  int most;    // largest exponent of V's scales so far
 };
 
 template <int D>
@@ -291,37 +309,29 @@ __device__ inline void start(State<D>& z) {
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int k = 0; k < 16; ++k) z.o[i][k] = 0.f;
-  z.m = -INFINITY, z.l = 0.f, z.e = kEMin;
+  z.m = -INFINITY, z.l = 0.f, z.most = kEMin;
+}
+
+__device__ inline void to_half(const float16v& y, half8 (&w)[2]) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    const half2v h = __builtin_convertvector((float2v{y[i], y[i + 1]}), half2v);
+    w[i / 8][i % 8] = h[0], w[i / 8][i % 8 + 1] = h[1];
+  }
 }
 
 // N pairs of blocks under one maximum: their scores (times f) become the second product's operands.
 template <int D, int N>
-__device__ inline void soften(State<D>& z, float16v (&s)[N], const float (&f)[N], const Pair (&p)[N], half8 (&w)[N][2]) {
-  const int half = (threadIdx.x >> 5) & 1;
-  float m = -INFINITY, ev[N];
+__device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (&f)[N], const Pair (&p)[N], half8 (&w)[N][2]) {
+  float m = -INFINITY;
   bool odd = false;  // a block that reads as NaN, or one whose scale is far below the largest
 #pragma unroll
-  for (int n = 0; n < N; ++n)
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int x = (int)((__float_as_uint(p[n].vs[b]) >> 23) & 255) - 127;
-      if (p[n].at[b] >= 0) z.e = x < 128 ? max(z.e, x) : z.e;
-    }
-#pragma unroll
   for (int n = 0; n < N; ++n) {
-    int e[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int x = (int)((__float_as_uint(p[n].vs[b]) >> 23) & 255) - 127;
-      const bool there = p[n].at[b] >= 0;
-      odd |= there && (x == 128 || x < z.e - kScaleSpan);
-      e[b] = there && x < 128 ? max(x, z.e - kScaleSpan) : z.e;
-    }
-    ev[n] = (float)(half ? e[1] : e[0]);
     float most = s[n][0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) most = fmaxf(most, s[n][i]);
-    m = fmaxf(m, fmaf(most, f[n], ev[n]));
+    m = fmaxf(m, fmaf(most, f[n], p[n].ev));
+    odd |= p[n].odd;
   }
   m = fmaxf(m, other_half(m));
   m = fmaxf(m, z.m);
@@ -335,9 +345,26 @@ __device__ inline void soften(State<D>& z, float16v (&s)[N], const float (&f)[N]
 #pragma unroll
       for (int k = 0; k < 16; ++k) z.o[i][k] *= alpha;
   }
+  if (__builtin_expect(odd, 0)) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float inverse = __builtin_amdgcn_exp2f(-p[n].ev), rest = p[n].odd ? p[n].vs * inverse : 1.f;
+      float sum = 0.f;
+      float16v y;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], p[n].ev - base));
+        sum += x;
+        y[i] = !p[n].there || s[n][i] == -INFINITY ? 0.f : x * rest;
+      }
+      z.l = fmaf(sum, inverse, z.l);
+      to_half(y, w[n]);
+    }
+    return;
+  }
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const float off = ev[n] - base;
+    const float off = p[n].ev - base;
     float sum = 0.f;
     float16v y;
 #pragma unroll
@@ -345,18 +372,8 @@ __device__ inline void soften(State<D>& z, float16v (&s)[N], const float (&f)[N]
       y[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off));
       sum += y[i];
     }
-    z.l = fmaf(sum, __builtin_amdgcn_exp2f(-ev[n]), z.l);
-    if (odd) {
-      const float vs = half ? p[n].vs[1] : p[n].vs[0], rest = vs * __builtin_amdgcn_exp2f(-ev[n]);
-      const bool there = (half ? p[n].at[1] : p[n].at[0]) >= 0;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = there && s[n][i] != -INFINITY ? y[i] * rest : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const half2v h = __builtin_convertvector((float2v{y[i], y[i + 1]}), half2v);
-      w[n][i / 8][i % 8] = h[0], w[n][i / 8][i % 8 + 1] = h[1];
-    }
+    z.l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z.l);
+    to_half(y, w[n]);
   }
 }
 
@@ -409,15 +426,15 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
   float f[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    f[n] = r.c * ((threadIdx.x & 32) ? p[n].ks[1] : p[n].ks[0]);
-    finish_scores<MARKS>(a, u.prefix, u.hi, t0[n], p[n].at[0], p[n].at[1], m[n], r.slope, r.token, r.position, r.see, u.pos0, f[n], s[n]);
+    f[n] = r.c * p[n].ks;
+    finish_scores<MARKS>(a, u.prefix, u.hi, t0[n], p[n], m[n], r.slope, r.token, r.position, r.see, u.pos0, f[n], s[n]);
   }
   half8 w[N][2];
   soften<D, N>(z, s, f, p, w);
   __builtin_amdgcn_sched_barrier(0);  // (V's codes are turned as they are needed: all at once they take 64 registers more)
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    drop_absent(p[n].at[0], p[n].at[1], v[n]);
+    drop_absent(p[n].cut, p[n].there, v[n]);
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -469,6 +486,7 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
 #pragma unroll
     for (int y = 0; y < D / 16; ++y) q[y * 64 + lane] = x[y];
   }
+  finish_scales(b, z.most);
   int i = 0;
   for (; i + 1 < n_pairs; i += 2) {
     const Pair p[2] = {pair_of(b, i & 31), pair_of(b, (i + 1) & 31)};
@@ -476,7 +494,7 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
     step<CODES, D, MARKS, 2>(a, u, r, q, z, k, v, p, marks, t0,
       [&] {
         if (i + 2 >= n_pairs) return;
-        if (((i + 2) & 31) == 0) find(i + 2), load_scales(a, b);
+        if (((i + 2) & 31) == 0) find(i + 2), load_scales(a, b), finish_scales(b, z.most);
         if constexpr (MARKS) marks[0] = load_marks(a, b, (i + 2) & 31), marks[1] = load_marks(a, b, (i + 3) & 31);
         load_k(i + 2, 0), load_k(i + 3, 1);
       },
@@ -560,8 +578,9 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
     if constexpr (MARKS) marks = load_marks(a, ahead, x);
   };
   auto publish = [&](int tile) {
-    const int x = 2 * (tile & 15) + sub;
-    drop_absent(__builtin_amdgcn_readlane(ahead.at, 2 * x), __builtin_amdgcn_readlane(ahead.at, 2 * x + 1), v);
+    const int x = 2 * (2 * (tile & 15) + sub);
+    const uint64_t gone = __ballot(ahead.at < 0) >> x;
+    drop_absent(gone & 3, !((gone >> half) & 1), v);
     half8* to = (half8*)(lds + (tile & 1) * kTileBytes<D>);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
@@ -584,6 +603,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   if (n_tiles > 0) request(0);
   load_scales(a, b);
   finish_rows<D>(a, r, raw, q);
+  finish_scales(b, z.most);
   if (n_tiles > 0) {
     publish(0);
     if (n_tiles > 1) request(1);
@@ -593,6 +613,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
     if (j && (j & 15) == 0) {
       find_blocks(a, u.request, head, u.lo + j * 64 + lane * 16, u.hi, b);
       load_scales(a, b);
+      finish_scales(b, z.most);
     }
     const int t0 = u.lo + j * 64;
     if (works && (t0 <= last_token || t0 < u.prefix)) {
@@ -615,8 +636,8 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
           const int* from_m = (const int*)(lds + 2 * kTileBytes<D> + (j & 1) * kMarkBytes) + x * 32 + half * 16 + (lane & 15);
           m.tag = from_m[0], m.position = from_m[64];
         }
-        f[x] = r.c * (half ? p[x].ks[1] : p[x].ks[0]);
-        finish_scores<MARKS>(a, u.prefix, u.hi, t0 + 32 * x, p[x].at[0], p[x].at[1], m, r.slope, r.token, r.position, r.see, first_token, f[x], s[x]);
+        f[x] = r.c * p[x].ks;
+        finish_scores<MARKS>(a, u.prefix, u.hi, t0 + 32 * x, p[x], m, r.slope, r.token, r.position, r.see, first_token, f[x], s[x]);
       }
       half8 w[2][2];
       soften<D, 2>(z, s, f, p, w);
