@@ -50,7 +50,7 @@ struct AttendArgs {
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kScaleSpan = 60;  // blocks whose V scale is this many powers of two below the largest take the rest as a factor
+constexpr int kScaleSpan = 60;  // V of blocks whose scale is more powers of two than this below the largest counts as 0
 
 __device__ inline float other_half(float x) {  // of lane ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -139,11 +139,11 @@ __device__ inline void finish_rows(const AttendArgs& a, Rows<D>& r, const uint4v
 }
 
 // The blocks of a stretch of tokens, lane k the k-th of them: index into the scales (-1: none there), first slot / 16, K's scale, the exponent of
-// V's as it enters the scores, and, for the wave, which are absent and which need more than that exponent.
+// V's as it enters the scores; and, for the wave, which blocks are absent, whose V reads as NaN, and whose V is too small to count.
 struct Blocks {
   int at, slot16;
   float ks, vs, ev;
-  uint64_t absent, odd;
+  uint64_t absent, nan, far;
 };
 
 __device__ inline int load_page(const AttendArgs& a, int request, int token, int hi) {
@@ -174,18 +174,17 @@ __device__ inline void finish_scales(Blocks& b, int& most) {
   int e = there && !nan ? x : kEMin;
   for (int d = 32; d; d >>= 1) e = max(e, __shfl_xor(e, d));
   most = max(most, __builtin_amdgcn_readfirstlane(e));
-  e = there && !nan ? max(x, most - kScaleSpan) : most;
-  b.ev = (float)e;
+  b.ev = (float)(there && !nan ? max(x, most - kScaleSpan) : most);
   b.absent = __ballot(!there);
-  b.odd = __ballot(there && (nan || x < most - kScaleSpan));
+  b.nan = __ballot(there && nan);
+  b.far = __ballot(there && x < most - kScaleSpan);
 }
 
-// 32 tokens: two blocks, of which the lane has to do with the one that its half of the wave holds scores of.
+// 32 tokens: two blocks, of which the lane has to do with the one that its half of the wave holds scores of.  Of what is rare, bit h says it of
+// block h.
 struct Pair {
   float ks, ev;
-  float vs;       // only if odd
-  bool cut, odd;  // one of the two is absent; one of the two is odd
-  bool there;     // the lane's
+  int absent, nan, far;
 };
 
 __device__ inline float of_lane(float x, int from) { return __uint_as_float(__builtin_amdgcn_ds_bpermute(from * 4, __float_as_uint(x))); }
@@ -194,12 +193,11 @@ __device__ inline Pair pair_of(const Blocks& b, int k) {  // blocks 2k and 2k + 
   const int mine = 2 * k + ((threadIdx.x >> 5) & 1);
   Pair p;
   p.ks = of_lane(b.ks, mine), p.ev = of_lane(b.ev, mine);
-  p.cut = (b.absent >> (2 * k)) & 3, p.odd = (b.odd >> (2 * k)) & 3;
-  p.there = !((b.absent >> mine) & 1);
-  p.vs = 0.f;
-  if (p.odd) p.vs = of_lane(b.vs, mine);
+  p.absent = (int)(b.absent >> (2 * k)) & 3, p.nan = (int)(b.nan >> (2 * k)) & 3, p.far = (int)(b.far >> (2 * k)) & 3;
   return p;
 }
+
+__device__ inline bool of_half(int bits) { return (bits >> ((threadIdx.x >> 5) & 1)) & 1; }
 
 // The codes of a pair, as this lane's pieces.  Row m = 8a + 4h + b of the first product is token 4a + b of block h.
 __device__ inline const uint8_t* k_piece(const AttendArgs& a, int at0, int at1, int D) {
@@ -221,10 +219,11 @@ __device__ inline void load_pieces(const uint8_t* from, uint4v (&x)[N]) {
 }
 
 template <int N>
-__device__ inline void drop_absent(bool cut, bool there, uint4v (&v)[N]) {  // what is not there must not be NaN: its weight is 0
-  if (cut) {
+__device__ inline void drop_absent(int absent, uint4v (&v)[N]) {  // what is not there must not be NaN: its weight is 0
+  if (absent) {
+    const bool none = of_half(absent);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = there ? v[i] : uint4v{0, 0, 0, 0};
+    for (int i = 0; i < N; ++i) v[i] = none ? uint4v{0, 0, 0, 0} : v[i];
   }
 }
 
@@ -246,7 +245,7 @@ template <bool MARKS>
 __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, const Pair& p, const Marks& marks, float slope, int token, int position,
                                      uint64_t see, int first_token, float& f, float16v& s) {
   const int half = (threadIdx.x >> 5) & 1, base = t0 + 16 * half;
-  const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || p.cut;
+  const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || p.absent;
   const bool masked = cut || (t0 + 32 > prefix && ((MARKS && a.tagged) || ordered));
   if (!(a.cap_log2 > 0.f) && !a.lowered && !masked) return;
   if (a.cap_log2 > 0.f) {
@@ -290,7 +289,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     bits &= tagged;
   }
   bits |= below(prefix - base);
-  bits = p.there ? bits & below(hi - base) : 0u;
+  bits = of_half(p.absent) ? 0u : bits & below(hi - base);
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = (bits >> i) & 1 ? s[i] : -INFINITY;
 }
@@ -300,6 +299,7 @@ template <int D>
 struct State {
   float16v o[D / 32];
   float m, l;  // l: of this lane's tokens
+  float bad;   // NaN: the row sees a block whose V reads as NaN
   int most;    // largest exponent of V's scales so far
 };
 
@@ -309,7 +309,7 @@ __device__ inline void start(State<D>& z) {
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int k = 0; k < 16; ++k) z.o[i][k] = 0.f;
-  z.m = -INFINITY, z.l = 0.f, z.most = kEMin;
+  z.m = -INFINITY, z.l = 0.f, z.bad = 0.f, z.most = kEMin;
 }
 
 __device__ inline void to_half(const float16v& y, half8 (&w)[2]) {
@@ -320,18 +320,28 @@ __device__ inline void to_half(const float16v& y, half8 (&w)[2]) {
   }
 }
 
-// N pairs of blocks under one maximum: their scores (times f) become the second product's operands.
-template <int D, int N>
-__device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (&f)[N], const Pair (&p)[N], half8 (&w)[N][2]) {
+// N pairs of blocks under one maximum: their scores (times f) become the second product's operands.  `between` is called where the exponentials are
+// taken.
+template <int D, int N, class Between>
+__device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (&f)[N], const Pair (&p)[N], half8 (&w)[N][2], Between between) {
   float m = -INFINITY;
-  bool odd = false;  // a block that reads as NaN, or one whose scale is far below the largest
+  int rare = 0;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     float most = s[n][0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) most = fmaxf(most, s[n][i]);
     m = fmaxf(m, fmaf(most, f[n], p[n].ev));
-    odd |= p[n].odd;
+    rare |= p[n].nan | p[n].far;
+  }
+  if (__builtin_expect(rare, 0)) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      bool sees = false;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sees |= s[n][i] != -INFINITY;
+      if (of_half(p[n].nan) && sees) z.bad = __builtin_nanf("");
+    }
   }
   m = fmaxf(m, other_half(m));
   m = fmaxf(m, z.m);
@@ -345,23 +355,7 @@ __device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (
 #pragma unroll
       for (int k = 0; k < 16; ++k) z.o[i][k] *= alpha;
   }
-  if (__builtin_expect(odd, 0)) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const float inverse = __builtin_amdgcn_exp2f(-p[n].ev), rest = p[n].odd ? p[n].vs * inverse : 1.f;
-      float sum = 0.f;
-      float16v y;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], p[n].ev - base));
-        sum += x;
-        y[i] = !p[n].there || s[n][i] == -INFINITY ? 0.f : x * rest;
-      }
-      z.l = fmaf(sum, inverse, z.l);
-      to_half(y, w[n]);
-    }
-    return;
-  }
+  between();
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const float off = p[n].ev - base;
@@ -374,6 +368,11 @@ __device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (
     }
     z.l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z.l);
     to_half(y, w[n]);
+    if (__builtin_expect(p[n].far, 0)) {
+      const bool none = of_half(p[n].far);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[n][i] = none ? half8{} : w[n][i];
+    }
   }
 }
 
@@ -396,6 +395,17 @@ __device__ inline void store_out(const AttendArgs& a, int64_t at, float4v x) {  
     }
   }
   *(uint2v*)((uint16_t*)a.out + at) = w;
+}
+
+template <int D>
+__device__ inline void poison(State<D>& z) {
+  const float bad = z.bad + other_half(z.bad);
+  if (__any(bad != 0.f)) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) z.o[i][k] += bad;
+  }
 }
 
 __device__ inline float lse_of(float m, float l) { return l == 0.f ? -INFINITY : kLn2 * (m + __builtin_amdgcn_logf(l)); }
@@ -430,11 +440,11 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
     finish_scores<MARKS>(a, u.prefix, u.hi, t0[n], p[n], m[n], r.slope, r.token, r.position, r.see, u.pos0, f[n], s[n]);
   }
   half8 w[N][2];
-  soften<D, N>(z, s, f, p, w);
+  soften<D, N>(z, s, f, p, w, [] {});
   __builtin_amdgcn_sched_barrier(0);  // (V's codes are turned as they are needed: all at once they take 64 registers more)
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    drop_absent(p[n].cut, p[n].there, v[n]);
+    drop_absent(p[n].absent, v[n]);
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -511,6 +521,7 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
   float* s_o = lds;                                       // [4][32][kPitch]
   float2v* s_ml = (float2v*)(lds + 4 * kRows * kPitch);   // [4][32]
   const float l = z.l + other_half(z.l);
+  poison(z);
   if (half == 0) s_ml[wave * kRows + n] = float2v{z.m, l};
   if (r.real) {
 #pragma unroll
@@ -547,116 +558,146 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
   }
 }
 
-// LDS of the shared tiles: two buffers of 64 tokens, K and V as the products' operands (a lane's 16 bytes next to its neighbour's), behind
-// them the tokens' tags and positions.
+// LDS of the shared tokens: rings of four pairs of blocks (32 tokens) for K and for V, as the products' operands (a lane's 16 bytes next to its
+// neighbour's), and for the tokens' tags and positions.
 template <int D>
-constexpr int kTileBytes = 2 * 64 * D * 2;
-constexpr int kMarkBytes = 2 * 64 * 4;
+constexpr int kPairBytes = 32 * D * 2;  // K or V
+constexpr int kMarkBytes = 2 * 32 * 4;
 
+// The scores of pair i + 1 are taken between the exponentials of pair i, so that within a wave the matrix pipe and the vector pipe work at the same
+// time; pairs, not twice as many tokens, because two sets of scores, O and Q are what the registers hold.  One barrier for two pairs, 2j and 2j + 1:
+// in between the rings hold K up to 2j + 2 and V up to 2j + 1, and K of 2j + 3, 2j + 4 and V of 2j + 2, 2j + 3 are put where older ones were.
 template <int CODES, int D, bool MARKS>
 __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head, uint8_t* lds) {
-  constexpr int kPieces = D / 64;               // pieces of K, and of V, that a wave brings of a tile
-  constexpr int kK = 64 * 2 * (D / 16);         // half8's of K in a tile; as many of V behind
+  constexpr int kPieces = D / 64;  // pieces of a pair's K, and of its V, that a wave brings
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
-  const int n_tiles = (u.hi - u.lo + 63) >> 6;
-  const int sub = wave >> 1, piece0 = (wave & 1) * kPieces;  // this wave's share: pieces piece0 .. of 32-token half `sub`
+  const int n_pairs = (u.hi - u.lo + 31) >> 5;
+  const int odd = wave >> 1, piece0 = (wave & 1) * kPieces;  // this wave's share: pieces piece0 .. of every second pair
   Rows<D> r;
   State<D> z;
   start(z);
   const bool works = wave * kRows < u.n_rows;
-  Blocks b, ahead;
   const int first_token = u.pos0 + (wave * kRows >> a.g_shift);
-  const int last_token = u.pos0 + ((min(wave * kRows + kRows, u.n_rows) - 1) >> a.g_shift);
+  Blocks b, ahead_k, ahead_v;  // of the pair under computation, and of those asked for: 32 pairs, from a multiple of 32 on
+  int group_k = 0, group_v = 0;
   uint4v k[kPieces], v[kPieces];
   Marks marks{};
-  auto request = [&](int tile) {
-    if (tile && (tile & 15) == 0) find_blocks(a, u.request, head, u.lo + tile * 64 + lane * 16, u.hi, ahead);
-    const int x = 2 * (tile & 15) + sub;
-    const int at0 = __builtin_amdgcn_readlane(ahead.at, 2 * x), at1 = __builtin_amdgcn_readlane(ahead.at, 2 * x + 1);
-    load_pieces(k_piece(a, at0, at1, D) + piece0 * 512, k);
-    load_pieces(v_piece(a, at0, at1, D) + piece0 * 512, v);
-    if constexpr (MARKS) marks = load_marks(a, ahead, x);
+  auto find = [&](int i, Blocks& to) { find_blocks(a, u.request, head, u.lo + (i & ~31) * 32 + lane * 16, u.hi, to); };
+  auto request_k = [&](int i) {
+    if (i >> 5 != group_k) group_k = i >> 5, find(i, ahead_k);
+    const int x = 2 * (i & 31);
+    load_pieces(k_piece(a, __builtin_amdgcn_readlane(ahead_k.at, x), __builtin_amdgcn_readlane(ahead_k.at, x + 1), D) + piece0 * 512, k);
+    if constexpr (MARKS) marks = load_marks(a, ahead_k, i & 31);
   };
-  auto publish = [&](int tile) {
-    const int x = 2 * (2 * (tile & 15) + sub);
-    const uint64_t gone = __ballot(ahead.at < 0) >> x;
-    drop_absent(gone & 3, !((gone >> half) & 1), v);
-    half8* to = (half8*)(lds + (tile & 1) * kTileBytes<D>);
+  auto request_v = [&](int i) {
+    if (i >> 5 != group_v) group_v = i >> 5, find(i, ahead_v);
+    const int x = 2 * (i & 31);
+    load_pieces(v_piece(a, __builtin_amdgcn_readlane(ahead_v.at, x), __builtin_amdgcn_readlane(ahead_v.at, x + 1), D) + piece0 * 512, v);
+  };
+  auto publish_k = [&](int i) {
+    half8* to = (half8*)(lds + (i & 3) * kPairBytes<D>) + piece0 * 2 * 64 + lane;
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int step = (sub * (D / 32) + piece0 + i) * 2;
-      to[step * 64 + lane] = codes_to_half8<CODES>(k[i][0], k[i][1]);
-      to[(step + 1) * 64 + lane] = codes_to_half8<CODES>(k[i][2], k[i][3]);
-      to[kK + step * 64 + lane] = codes_to_half8<CODES>(v[i][0], v[i][1]);
-      to[kK + (step + 1) * 64 + lane] = codes_to_half8<CODES>(v[i][2], v[i][3]);
+    for (int x = 0; x < kPieces; ++x) {
+      to[(2 * x) * 64] = codes_to_half8<CODES>(k[x][0], k[x][1]);
+      to[(2 * x + 1) * 64] = codes_to_half8<CODES>(k[x][2], k[x][3]);
     }
     if (MARKS && !(wave & 1) && !(lane & 16)) {
-      int* m = (int*)(lds + 2 * kTileBytes<D> + (tile & 1) * kMarkBytes) + sub * 32 + half * 16 + (lane & 15);
-      m[0] = marks.tag, m[64] = marks.position;
+      int* m = (int*)(lds + 8 * kPairBytes<D> + (i & 3) * kMarkBytes) + half * 16 + (lane & 15);
+      m[0] = marks.tag, m[32] = marks.position;
     }
   };
-  find_blocks(a, u.request, head, u.lo + lane * 16, u.hi, b);
-  ahead = b;
-  uint4v raw[D / 16];
+  auto publish_v = [&](int i) {
+    drop_absent((int)(__ballot(ahead_v.at < 0) >> (2 * (i & 31))) & 3, v);
+    half8* to = (half8*)(lds + (4 + (i & 3)) * kPairBytes<D>) + piece0 * 2 * 64 + lane;
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      to[(2 * x) * 64] = codes_to_half8<CODES>(v[x][0], v[x][1]);
+      to[(2 * x + 1) * 64] = codes_to_half8<CODES>(v[x][2], v[x][3]);
+    }
+  };
   half8 q[D / 16];
-  request_rows<D, MARKS>(a, u, head, wave * kRows, r, raw);
-  if (n_tiles > 0) request(0);
-  load_scales(a, b);
-  finish_rows<D>(a, r, raw, q);
-  finish_scales(b, z.most);
-  if (n_tiles > 0) {
-    publish(0);
-    if (n_tiles > 1) request(1);
+  {
+    uint4v raw[D / 16];
+    const int page = load_page(a, u.request, u.lo + lane * 16, u.hi);
+    __builtin_amdgcn_sched_barrier(0);
+    request_rows<D, MARKS>(a, u, head, wave * kRows, r, raw);
+    __builtin_amdgcn_sched_barrier(0);
+    on_page(a, page, head, u.lo + lane * 16, u.hi, b);
+    ahead_k = ahead_v = b;
+    load_scales(a, b);
+    request_k(odd);
+    request_v(odd);
+    __builtin_amdgcn_sched_barrier(0);
+    finish_rows<D>(a, r, raw, q);
   }
+  finish_scales(b, z.most);
+  publish_k(odd);
+  publish_v(odd);
+  if (!odd) request_k(2), publish_k(2);
+  request_k(3 + odd);
+  request_v(2 + odd);
   __syncthreads();
-  for (int j = 0; j < n_tiles; ++j) {
-    if (j && (j & 15) == 0) {
-      find_blocks(a, u.request, head, u.lo + j * 64 + lane * 16, u.hi, b);
-      load_scales(a, b);
-      finish_scales(b, z.most);
+  Pair p[1];
+  float f[1];
+  float16v s[1], t[1];  // scores of even and of odd pairs
+  half8 w[1][2];
+  auto products = [&](int i, float16v& to) {
+    const half8* from = (const half8*)(lds + (i & 3) * kPairBytes<D>) + lane;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) to[x] = 0.f;
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) to = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[x * 64], q[x], to, 0, 0, 0);
+  };
+  auto finish = [&](int i, float16v& of) {
+    p[0] = pair_of(b, i & 31);
+    Marks m{};
+    if constexpr (MARKS) {
+      const int* from = (const int*)(lds + 8 * kPairBytes<D> + (i & 3) * kMarkBytes) + half * 16 + (lane & 15);
+      m.tag = from[0], m.position = from[32];
     }
-    const int t0 = u.lo + j * 64;
-    if (works && (t0 <= last_token || t0 < u.prefix)) {
-      const half8* from = (const half8*)(lds + (j & 1) * kTileBytes<D>);
-      const Pair p[2] = {pair_of(b, 2 * (j & 15)), pair_of(b, 2 * (j & 15) + 1)};
-      float16v s[2];
+    f[0] = r.c * p[0].ks;
+    finish_scores<MARKS>(a, u.prefix, u.hi, u.lo + i * 32, p[0], m, r.slope, r.token, r.position, r.see, first_token, f[0], of);
+  };
+  auto add_values = [&](int i) {
+    const half8* from = (const half8*)(lds + (4 + (i & 3)) * kPairBytes<D>) + lane;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+    for (int y = 0; y < 2; ++y)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[(x * (D / 16) + i) * 64 + lane], q[i], s[x], 0, 0, 0);
-      float f[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        Marks m{};
-        if constexpr (MARKS) {
-          const int* from_m = (const int*)(lds + 2 * kTileBytes<D> + (j & 1) * kMarkBytes) + x * 32 + half * 16 + (lane & 15);
-          m.tag = from_m[0], m.position = from_m[64];
-        }
-        f[x] = r.c * p[x].ks;
-        finish_scores<MARKS>(a, u.prefix, u.hi, t0 + 32 * x, p[x], m, r.slope, r.token, r.position, r.see, first_token, f[x], s[x]);
+      for (int x = 0; x < D / 32; ++x) z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[(2 * x + y) * 64], w[0][y], z.o[x], 0, 0, 0);
+  };
+  auto interleave = [&] {};
+  if (works && n_pairs > 0) {
+    products(0, s[0]);
+    finish(0, s[0]);
+  }
+  for (int i = 0; i < n_pairs; i += 2) {
+    // (behind the last pair comes one of absent blocks, and where its successor would be the ring holds an older one: products for nobody)
+    if (works) {
+      soften<D, 1>(z, s, f, p, w, [&] { products(i + 1, t[0]); });
+      add_values(i);
+      interleave();
+      finish(i + 1, t[0]);
+      soften<D, 1>(z, t, f, p, w, [&] { products(i + 2, s[0]); });
+      add_values(i + 1);
+      interleave();
+    }
+    if (i + 2 < n_pairs) {
+      publish_k(i + 3 + odd);
+      publish_v(i + 2 + odd);
+      request_k(i + 5 + odd);
+      request_v(i + 4 + odd);
+      if (((i + 2) & 31) == 0) {
+        find(i + 2, b);
+        load_scales(a, b);
+        finish_scales(b, z.most);
       }
-      half8 w[2][2];
-      soften<D, 2>(z, s, f, p, w);
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int i = 0; i < D / 32; ++i)
-            z.o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[kK + ((x * (D / 32) + i) * 2 + y) * 64 + lane], w[x][y], z.o[i], 0, 0, 0);
+      if (works) finish(i + 2, s[0]);
+      __syncthreads();
     }
-    if (j + 1 < n_tiles) {
-      publish(j + 1);
-      if (j + 2 < n_tiles) request(j + 2);
-    }
-    __syncthreads();
   }
   if (!works) return;
   const float l = z.l + other_half(z.l);
+  poison(z);
   if (!r.real) return;
   const int row = wave * kRows + n;
   if (u.part < 0) {
@@ -682,7 +723,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
 template <int CODES, int D, bool MANY, bool MARKS>
 __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   constexpr int kFewBytes = 4 * kRows * (D + 4) * 4 + 4 * kRows * 8;
-  constexpr int kManyBytes = 2 * kTileBytes<D> + 2 * kMarkBytes;
+  constexpr int kManyBytes = 8 * kPairBytes<D> + 4 * kMarkBytes;
   __shared__ __attribute__((aligned(16))) uint8_t lds[MANY && kManyBytes > kFewBytes ? kManyBytes : kFewBytes];
   const int head = blockIdx.x % a.g.Hkv;
   const Unit u = a.units[blockIdx.x / a.g.Hkv];
