@@ -20,6 +20,8 @@
 // attend_few, <= 32 stacked rows: every wave takes blocks of 32 tokens of its own, and the four meet once at the end.
 // attend_many: four waves of 32 rows each take the same tokens; the codes are turned into fp16 once per work-group, by way of LDS.
 #pragma once
+#include <float.h>
+
 #include "k8_dev.hpp"
 
 namespace k8 {
@@ -50,6 +52,8 @@ struct AttendArgs {
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 8.f;   // the base of the scores follows their maximum when that is 2^8 ahead: O is rescaled rarely, and weights up to 256
+                                // lose nothing in fp16
 constexpr int kScaleSpan = 60;  // V of blocks whose scale is more powers of two than this below the largest counts as 0
 
 __device__ inline float other_half(float x) {  // of lane ^ 32
@@ -239,11 +243,70 @@ __device__ inline Marks load_marks(const AttendArgs& a, const Blocks& b, int k) 
   return Marks{(int)a.slot_tag[at], a.slot_position[at]};
 }
 
+// What the tokens of a pair are to the wave's rows: how far, and who sees them.
+struct Unmarked {
+  template <class F>
+  __device__ void distances(F) const {}
+  template <class F>
+  __device__ void sights(F) const {}
+  __device__ bool alike(bool&) const { return false; }
+};
+
+// attend_few: from the tokens' marks in the wave's own lanes.
+struct MarkedHere {
+  Marks marks;
+  int position;
+  uint64_t see;
+  template <class F>
+  __device__ void distances(F f) const {
+    each<16>([&](auto i) { f(i.value, (float)(position - of_row<i.value>(marks.position))); });
+  }
+  template <class F>
+  __device__ void sights(F f) const {
+    const int up = 63 - (marks.tag & 63);
+    each<16>([&](auto i) { f(i.value, (int64_t)(see << of_row<i.value>(up)) < 0); });
+  }
+  __device__ bool alike(bool& sees) const {  // one tag for all of the lane's tokens, for every lane
+    const int first = of_row<0>(marks.tag);
+    sees = (see >> (first & 63)) & 1;
+    return __all(marks.tag == first);
+  }
+};
+
+// attend_many: from LDS, where positions lie as distances from one row of the work-group, and tags as the rows that see them: bit n of a token's
+// word is row n of the wave.  A lane holds the word of token l & 15 of block l >> 5, so that two words are the lanes that see token i.
+struct MarkedThere {
+  const float* position;
+  float own;
+  uint32_t rows;
+  template <class F>
+  __device__ void distances(F f) const {
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float4v x = *(const float4v*)(position + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f(i + k, own - x[k]);
+    }
+  }
+  template <class F>
+  __device__ void sights(F f) const {
+    each<16>([&](auto i) {
+      const uint64_t lanes = (uint64_t)__builtin_amdgcn_readlane(rows, 32 + i.value) << 32 | (uint32_t)__builtin_amdgcn_readlane(rows, i.value);
+      f(i.value, __builtin_amdgcn_inverse_ballot_w64(lanes));
+    });
+  }
+  __device__ bool alike(bool& sees) const {
+    const int first = of_row<0>(rows);
+    sees = (first >> (threadIdx.x & 31)) & 1;
+    return __all((int)rows == first);
+  }
+};
+
 // Scores of a pair, tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
 // left so where nothing has to be done; else they come out in log2 units and f is 1.
-template <bool MARKS>
-__device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, const Pair& p, const Marks& marks, float slope, int token, int position,
-                                     uint64_t see, int first_token, float& f, float16v& s) {
+template <bool MARKS, class Source>
+__device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, const Pair& p, const Source& source, float slope, int token,
+                                     int first_token, float& f, float16v& s) {
   const int half = (threadIdx.x >> 5) & 1, base = t0 + 16 * half;
   const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || p.absent;
   const bool masked = cut || (t0 + 32 > prefix && ((MARKS && a.tagged) || ordered));
@@ -260,7 +323,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
   f = 1.f;
   if (a.lowered) {
     if (MARKS && a.placed) {
-      each<16>([&](auto i) { s[i.value] = fmaf(-slope, fabsf((float)(position - of_row<i.value>(marks.position))), s[i.value]); });
+      source.distances([&](int i, float far) { s[i] = fmaf(-slope, fabsf(far), s[i]); });
     } else {
       const float far = (float)(token - base);
 #pragma unroll
@@ -269,14 +332,13 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
   }
   if (!masked) return;
   if (MARKS && a.tagged && t0 >= prefix && !ordered && !cut) {  // tags alone
-    const int first = of_row<0>(marks.tag);
-    if (__all(marks.tag == first)) {
-      if (!((see >> (first & 63)) & 1))
+    bool sees;
+    if (source.alike(sees)) {
+      if (!sees)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = -INFINITY;
     } else {
-      const int up = 63 - (marks.tag & 63);
-      each<16>([&](auto i) { s[i.value] = (int64_t)(see << of_row<i.value>(up)) < 0 ? s[i.value] : -INFINITY; });
+      source.sights([&](int i, bool seen) { s[i] = seen ? s[i] : -INFINITY; });
     }
     return;
   }
@@ -284,8 +346,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
   uint32_t bits = below(token + 1 - base);
   if (MARKS && a.tagged) {
     uint32_t tagged = 0;
-    const int tag = marks.tag & 63;
-    each<16>([&](auto i) { tagged |= (uint32_t)((see >> of_row<i.value>(tag)) & 1) << i.value; });
+    source.sights([&](int i, bool seen) { tagged |= seen ? 1u << i : 0u; });
     bits &= tagged;
   }
   bits |= below(prefix - base);
@@ -298,7 +359,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
 template <int D>
 struct State {
   float16v o[D / 32];
-  float m, l;  // l: of this lane's tokens
+  float m, l;  // the scores' base, at most kSlack below their maximum; l: of this lane's tokens
   float bad;   // NaN: the row sees a block whose V reads as NaN
   int most;    // largest exponent of V's scales so far
 };
@@ -309,7 +370,7 @@ __device__ inline void start(State<D>& z) {
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int k = 0; k < 16; ++k) z.o[i][k] = 0.f;
-  z.m = -INFINITY, z.l = 0.f, z.bad = 0.f, z.most = kEMin;
+  z.m = -FLT_MAX, z.l = 0.f, z.bad = 0.f, z.most = kEMin;
 }
 
 __device__ inline void to_half(const float16v& y, half8 (&w)[2]) {
@@ -320,11 +381,11 @@ __device__ inline void to_half(const float16v& y, half8 (&w)[2]) {
   }
 }
 
-// N pairs of blocks under one maximum: their scores (times f) become the second product's operands.  `between` is called where the exponentials are
-// taken.
+// N pairs of blocks: their scores (times f) become the second product's operands.  `between` is called where the exponentials are taken; from there
+// on there is no branch.
 template <int D, int N, class Between>
 __device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (&f)[N], const Pair (&p)[N], half8 (&w)[N][2], Between between) {
-  float m = -INFINITY;
+  float m = -FLT_MAX;
   int rare = 0;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -334,45 +395,43 @@ __device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (
     m = fmaxf(m, fmaf(most, f[n], p[n].ev));
     rare |= p[n].nan | p[n].far;
   }
-  if (__builtin_expect(rare, 0)) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      bool sees = false;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sees |= s[n][i] != -INFINITY;
-      if (of_half(p[n].nan) && sees) z.bad = __builtin_nanf("");
-    }
-  }
   m = fmaxf(m, other_half(m));
-  m = fmaxf(m, z.m);
-  const float base = m == -INFINITY ? 0.f : m;
-  const float alpha = __builtin_amdgcn_exp2f(z.m - base);
-  z.m = m;
-  z.l *= alpha;
-  if (__any(alpha != 1.f)) {
+  if (__any(m > z.m + kSlack)) {
+    m = fmaxf(m, z.m);
+    const float alpha = __builtin_amdgcn_exp2f(z.m - m);
+    z.m = m;
+    z.l *= alpha;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int k = 0; k < 16; ++k) z.o[i][k] *= alpha;
   }
+  float off[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) off[n] = p[n].ev - z.m;
+  if (__builtin_expect(rare, 0)) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      bool sees = false;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sees |= s[n][i] != -INFINITY, sum += __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off[n]));
+      if (of_half(p[n].nan) && sees) z.bad = __builtin_nanf("");
+      if (of_half(p[n].far)) z.l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z.l), off[n] = -INFINITY;
+    }
+  }
   between();
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const float off = p[n].ev - base;
     float sum = 0.f;
     float16v y;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      y[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off));
+      y[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off[n]));
       sum += y[i];
     }
     z.l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z.l);
     to_half(y, w[n]);
-    if (__builtin_expect(p[n].far, 0)) {
-      const bool none = of_half(p[n].far);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) w[n][i] = none ? half8{} : w[n][i];
-    }
   }
 }
 
@@ -437,7 +496,10 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     f[n] = r.c * p[n].ks;
-    finish_scores<MARKS>(a, u.prefix, u.hi, t0[n], p[n], m[n], r.slope, r.token, r.position, r.see, u.pos0, f[n], s[n]);
+    if constexpr (MARKS)
+      finish_scores<true>(a, u.prefix, u.hi, t0[n], p[n], MarkedHere{m[n], r.position, r.see}, r.slope, r.token, u.pos0, f[n], s[n]);
+    else
+      finish_scores<false>(a, u.prefix, u.hi, t0[n], p[n], Unmarked{}, r.slope, r.token, u.pos0, f[n], s[n]);
   }
   half8 w[N][2];
   soften<D, N>(z, s, f, p, w, [] {});
@@ -534,15 +596,14 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
   __syncthreads();
   for (int j = threadIdx.x; j < u.n_rows * (D / 4); j += 256) {
     const int row = j / (D / 4), d = j % (D / 4) * 4;
-    float m = -INFINITY, all = 0.f;
+    float m = -FLT_MAX, all = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) m = fmaxf(m, s_ml[w * kRows + row][0]);
-    const float base = m == -INFINITY ? 0.f : m;
     float4v o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float2v ml = s_ml[w * kRows + row];
-      const float f = __builtin_amdgcn_exp2f(ml[0] - base);
+      const float f = __builtin_amdgcn_exp2f(ml[0] - m);
       all = fmaf(ml[1], f, all);
       o += *(const float4v*)(s_o + (w * kRows + row) * kPitch + d) * f;
     }
@@ -558,11 +619,25 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
   }
 }
 
+// The order that the compiler is asked for: one product, reads of operands, vector instructions with exponentials among them.
+template <int READS, int EXPONENTIALS>
+__device__ inline void between_products() {
+  __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+  __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  __builtin_amdgcn_sched_group_barrier(0x002, 2 * EXPONENTIALS / 2, 0);
+  __builtin_amdgcn_sched_group_barrier(0x400, EXPONENTIALS, 0);
+  __builtin_amdgcn_sched_group_barrier(0x002, 3 * EXPONENTIALS / 2, 0);
+}
+
 // LDS of the shared tokens: rings of four pairs of blocks (32 tokens) for K and for V, as the products' operands (a lane's 16 bytes next to its
-// neighbour's), and for the tokens' tags and positions.
+// neighbour's); a ring for the tokens' positions (less the first row's) and for the rows that see them, a word per wave; and, per tag, those rows.
 template <int D>
 constexpr int kPairBytes = 32 * D * 2;  // K or V
-constexpr int kMarkBytes = 2 * 32 * 4;
+struct ManyMarks {
+  float position[4][32];
+  uint4v rows[4][32];
+  uint4v tag_rows[64];
+};
 
 // The scores of pair i + 1 are taken between the exponentials of pair i, so that within a wave the matrix pipe and the vector pipe work at the same
 // time; pairs, not twice as many tokens, because two sets of scores, O and Q are what the registers hold.  One barrier for two pairs, 2j and 2j + 1:
@@ -570,9 +645,11 @@ constexpr int kMarkBytes = 2 * 32 * 4;
 template <int CODES, int D, bool MARKS>
 __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head, uint8_t* lds) {
   constexpr int kPieces = D / 64;  // pieces of a pair's K, and of its V, that a wave brings
+  constexpr int kEarly = D / 32;   // operands of K that are read ahead of the maximum
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
   const int n_pairs = (u.hi - u.lo + 31) >> 5;
   const int odd = wave >> 1, piece0 = (wave & 1) * kPieces;  // this wave's share: pieces piece0 .. of every second pair
+  ManyMarks& there = *(ManyMarks*)(lds + 8 * kPairBytes<D>);
   Rows<D> r;
   State<D> z;
   start(z);
@@ -582,6 +659,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   int group_k = 0, group_v = 0;
   uint4v k[kPieces], v[kPieces];
   Marks marks{};
+  const int origin = MARKS ? a.row_position[u.s0 >> a.g_shift] : 0;
   auto find = [&](int i, Blocks& to) { find_blocks(a, u.request, head, u.lo + (i & ~31) * 32 + lane * 16, u.hi, to); };
   auto request_k = [&](int i) {
     if (i >> 5 != group_k) group_k = i >> 5, find(i, ahead_k);
@@ -602,17 +680,21 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
       to[(2 * x + 1) * 64] = codes_to_half8<CODES>(k[x][2], k[x][3]);
     }
     if (MARKS && !(wave & 1) && !(lane & 16)) {
-      int* m = (int*)(lds + 8 * kPairBytes<D> + (i & 3) * kMarkBytes) + half * 16 + (lane & 15);
-      m[0] = marks.tag, m[32] = marks.position;
+      const int t = half * 16 + (lane & 15);
+      if (a.placed) there.position[i & 3][t] = (float)(marks.position - origin);
+      if (a.tagged) there.rows[i & 3][t] = there.tag_rows[marks.tag & 63];
     }
   };
   auto publish_v = [&](int i) {
-    drop_absent((int)(__ballot(ahead_v.at < 0) >> (2 * (i & 31))) & 3, v);
+    const bool none = of_half((int)(__ballot(ahead_v.at < 0) >> (2 * (i & 31))) & 3);
     half8* to = (half8*)(lds + (4 + (i & 3)) * kPairBytes<D>) + piece0 * 2 * 64 + lane;
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) {
-      to[(2 * x) * 64] = codes_to_half8<CODES>(v[x][0], v[x][1]);
-      to[(2 * x + 1) * 64] = codes_to_half8<CODES>(v[x][2], v[x][3]);
+      uint4v c;  // what is not there must not be NaN: its weight is 0
+#pragma unroll
+      for (int y = 0; y < 4; ++y) c[y] = none ? 0u : v[x][y];
+      to[(2 * x) * 64] = codes_to_half8<CODES>(c[0], c[1]);
+      to[(2 * x + 1) * 64] = codes_to_half8<CODES>(c[2], c[3]);
     }
   };
   half8 q[D / 16];
@@ -630,6 +712,15 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
     __builtin_amdgcn_sched_barrier(0);
     finish_rows<D>(a, r, raw, q);
   }
+  if (MARKS && a.tagged && u.hi > u.prefix) {
+    uint32_t rows = 0;  // lane t: the wave's rows that see tag t
+    for (int t = 0; t < 64; ++t) {
+      const uint32_t now = (uint32_t)__ballot((r.see >> t) & 1);
+      rows = lane == t ? now : rows;
+    }
+    ((uint32_t*)there.tag_rows)[lane * 4 + wave] = rows;
+    __syncthreads();
+  }
   finish_scales(b, z.most);
   publish_k(odd);
   publish_v(odd);
@@ -640,23 +731,27 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   Pair p[1];
   float f[1];
   float16v s[1], t[1];  // scores of even and of odd pairs
-  half8 w[1][2];
+  half8 w[1][2], early[kEarly];
+  auto k_ring = [&](int i) { return (const half8*)(lds + (i & 3) * kPairBytes<D>) + lane; };
+  auto look_ahead = [&](int i) {
+#pragma unroll
+    for (int x = 0; x < kEarly; ++x) early[x] = k_ring(i)[x * 64];
+  };
   auto products = [&](int i, float16v& to) {
-    const half8* from = (const half8*)(lds + (i & 3) * kPairBytes<D>) + lane;
 #pragma unroll
     for (int x = 0; x < 16; ++x) to[x] = 0.f;
 #pragma unroll
-    for (int x = 0; x < D / 16; ++x) to = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[x * 64], q[x], to, 0, 0, 0);
+    for (int x = 0; x < D / 16; ++x) to = __builtin_amdgcn_mfma_f32_32x32x16_f16(x < kEarly ? early[x] : k_ring(i)[x * 64], q[x], to, 0, 0, 0);
   };
   auto finish = [&](int i, float16v& of) {
     p[0] = pair_of(b, i & 31);
-    Marks m{};
-    if constexpr (MARKS) {
-      const int* from = (const int*)(lds + 8 * kPairBytes<D> + (i & 3) * kMarkBytes) + half * 16 + (lane & 15);
-      m.tag = from[0], m.position = from[32];
-    }
     f[0] = r.c * p[0].ks;
-    finish_scores<MARKS>(a, u.prefix, u.hi, u.lo + i * 32, p[0], m, r.slope, r.token, r.position, r.see, first_token, f[0], of);
+    if constexpr (MARKS) {
+      const MarkedThere source{there.position[i & 3] + half * 16, (float)(r.position - origin), there.rows[i & 3][half * 16 + (lane & 15)][wave]};
+      finish_scores<true>(a, u.prefix, u.hi, u.lo + i * 32, p[0], source, r.slope, r.token, first_token, f[0], of);
+    } else {
+      finish_scores<false>(a, u.prefix, u.hi, u.lo + i * 32, p[0], Unmarked{}, r.slope, r.token, first_token, f[0], of);
+    }
   };
   auto add_values = [&](int i) {
     const half8* from = (const half8*)(lds + (4 + (i & 3)) * kPairBytes<D>) + lane;
@@ -664,22 +759,24 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
     for (int y = 0; y < 2; ++y)
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[(2 * x + y) * 64], w[0][y], z.o[x], 0, 0, 0);
+    // per product of the scores: a piece of the exponentials, and the reads of the operands that come next
+    each<D / 16>([](auto x) { between_products<(x.value < kEarly ? 1 : 2), 256 / D>(); });
   };
-  auto interleave = [&] {};
   if (works && n_pairs > 0) {
+    look_ahead(0);
     products(0, s[0]);
     finish(0, s[0]);
   }
   for (int i = 0; i < n_pairs; i += 2) {
     // (behind the last pair comes one of absent blocks, and where its successor would be the ring holds an older one: products for nobody)
     if (works) {
+      look_ahead(i + 1);
       soften<D, 1>(z, s, f, p, w, [&] { products(i + 1, t[0]); });
       add_values(i);
-      interleave();
       finish(i + 1, t[0]);
+      look_ahead(i + 2);
       soften<D, 1>(z, t, f, p, w, [&] { products(i + 2, s[0]); });
       add_values(i + 1);
-      interleave();
     }
     if (i + 2 < n_pairs) {
       publish_k(i + 3 + odd);
@@ -723,7 +820,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
 template <int CODES, int D, bool MANY, bool MARKS>
 __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   constexpr int kFewBytes = 4 * kRows * (D + 4) * 4 + 4 * kRows * 8;
-  constexpr int kManyBytes = 8 * kPairBytes<D> + 4 * kMarkBytes;
+  constexpr int kManyBytes = 8 * kPairBytes<D> + sizeof(ManyMarks);
   __shared__ __attribute__((aligned(16))) uint8_t lds[MANY && kManyBytes > kFewBytes ? kManyBytes : kFewBytes];
   const int head = blockIdx.x % a.g.Hkv;
   const Unit u = a.units[blockIdx.x / a.g.Hkv];
@@ -755,20 +852,19 @@ __global__ __launch_bounds__(256) void k8_merge(AttendArgs a) {
     const int64_t at = (int64_t)(tile.part + (real ? row : 0)) * a.g.Hkv + head;
     const float2v* ml = a.part_ml + at;
     const float* acc = a.part_acc + at * D + 4 * d;
-    float m = -INFINITY;
+    float m = -FLT_MAX;
     if (tile.n_parts <= 8) {
       for (int k = 0; k < tile.n_parts; ++k) m = fmaxf(m, ml[k * step][0]);
     } else {
       for (int k = d; k < tile.n_parts; k += kLanes) m = fmaxf(m, ml[k * step][0]);
       for (int x = kLanes / 2; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
     }
-    const float base = m == -INFINITY ? 0.f : m;
     float4v o{0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
 #pragma unroll 4
     for (int k = group % share; k < tile.n_parts; k += share) {
       const float2v x = ml[k * step];
-      const float f = __builtin_amdgcn_exp2f(x[0] - base);
+      const float f = __builtin_amdgcn_exp2f(x[0] - m);
       l = fmaf(x[1], f, l);
       o += *(const float4v*)(acc + k * step * D) * f;
     }
