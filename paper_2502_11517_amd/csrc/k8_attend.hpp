@@ -619,16 +619,6 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
   }
 }
 
-// The order that the compiler is asked for: one product, reads of operands, vector instructions with exponentials among them.
-template <int READS, int EXPONENTIALS>
-__device__ inline void between_products() {
-  __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-  __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-  __builtin_amdgcn_sched_group_barrier(0x002, 2 * EXPONENTIALS / 2, 0);
-  __builtin_amdgcn_sched_group_barrier(0x400, EXPONENTIALS, 0);
-  __builtin_amdgcn_sched_group_barrier(0x002, 3 * EXPONENTIALS / 2, 0);
-}
-
 // LDS of the shared tokens: rings of four pairs of blocks (32 tokens) for K and for V, as the products' operands (a lane's 16 bytes next to its
 // neighbour's); a ring for the tokens' positions (less the first row's) and for the rows that see them, a word per wave; and, per tag, those rows.
 template <int D>
@@ -738,6 +728,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
     for (int x = 0; x < kEarly; ++x) early[x] = k_ring(i)[x * 64];
   };
   auto products = [&](int i, float16v& to) {
+    __builtin_amdgcn_s_setprio(1);  // (the wave that feeds the matrix pipe goes ahead of its neighbour: 3 %)
 #pragma unroll
     for (int x = 0; x < 16; ++x) to[x] = 0.f;
 #pragma unroll
@@ -759,8 +750,6 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
     for (int y = 0; y < 2; ++y)
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[(2 * x + y) * 64], w[0][y], z.o[x], 0, 0, 0);
-    // per product of the scores: a piece of the exponentials, and the reads of the operands that come next
-    each<D / 16>([](auto x) { between_products<(x.value < kEarly ? 1 : 2), 256 / D>(); });
   };
   if (works && n_pairs > 0) {
     look_ahead(0);
@@ -773,10 +762,12 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
       look_ahead(i + 1);
       soften<D, 1>(z, s, f, p, w, [&] { products(i + 1, t[0]); });
       add_values(i);
+      __builtin_amdgcn_s_setprio(0);
       finish(i + 1, t[0]);
       look_ahead(i + 2);
       soften<D, 1>(z, t, f, p, w, [&] { products(i + 2, s[0]); });
       add_values(i + 1);
+      __builtin_amdgcn_s_setprio(0);
     }
     if (i + 2 < n_pairs) {
       publish_k(i + 3 + odd);
