@@ -164,7 +164,8 @@ int32_t pasta_kv8_append(pasta_kv8 *h, const pasta_kv8_append_args *a);
  * the step's own rows, which are a request's last n (length_out of pasta_kv8_slots).
  * slot (optional): a request whose first row has no slot was refused; its rows get
  * the result of a row that sees nothing.
- * Needs the workspace.  Errors: E_INVAL, E_CAPACITY, E_DEVICE, E_STATE.          */
+* Needs page_table and the workspace.  Errors: E_INVAL, E_CAPACITY, E_DEVICE,
+ * E_STATE.                                                                       */
 typedef struct {
   uint32_t struct_size, flags;    /* flags: 0 */
   int32_t n_requests, n_rows;

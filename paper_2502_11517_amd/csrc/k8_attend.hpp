@@ -42,7 +42,9 @@ struct AttendArgs {
   const int *slot_position, *row_position;
   const uint64_t* row_see;
   const float* slopes;
+  int block_shift;  // page_tokens / 16 = 1 << block_shift
   const Unit* units;
+  const int* unit_blocks;  // [unit][kUnitBlocks]
   const Tile* tiles;
   const void* q;
   void* out;
@@ -150,20 +152,15 @@ struct Blocks {
   uint64_t absent, nan, far;
 };
 
-__device__ inline int load_page(const AttendArgs& a, int request, int token, int hi) {
-  const int t = max(min(token, hi - 1), 0);
-  return a.table[(int64_t)request * a.g.table_width + (t >> a.g.page_shift)];
-}
-
-__device__ inline void on_page(const AttendArgs& a, int page, int head, int token, int hi, Blocks& b) {
-  const bool there = token < hi && page >= 0 && page < a.g.n_pages;
-  const int in = (token & (a.g.page_tokens - 1)) >> 4;
-  b.at = there ? (page * a.g.Hkv + head) * a.g.blocks_per_page + in : -1;
-  b.slot16 = there ? page * a.g.blocks_per_page + in : 0;
+// Block `number` of the layer's slots (slot / 16; negative: absent) for a kv head.
+__device__ inline void on_block(const AttendArgs& a, int number, int head, Blocks& b) {
+  const int page = number >> a.block_shift, in = number & (a.g.blocks_per_page - 1);
+  b.at = number >= 0 ? (page * a.g.Hkv + head) * a.g.blocks_per_page + in : -1;
+  b.slot16 = max(number, 0);
 }
 
 __device__ inline void find_blocks(const AttendArgs& a, int request, int head, int token, int hi, Blocks& b) {
-  on_page(a, load_page(a, request, token, hi), head, token, hi, b);
+  on_block(a, block_of(a.g, a.table, request, token, hi), head, b);
 }
 
 __device__ inline void load_scales(const AttendArgs& a, Blocks& b) {
@@ -191,12 +188,14 @@ struct Pair {
   int absent, nan, far;
 };
 
-__device__ inline float of_lane(float x, int from) { return __uint_as_float(__builtin_amdgcn_ds_bpermute(from * 4, __float_as_uint(x))); }
+__device__ inline float of_lanes(float x, int low, int high) {  // of one lane for the lower half of the wave, of another for the upper half
+  const float l = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), low)), h = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), high));
+  return (threadIdx.x & 32) ? h : l;
+}
 
 __device__ inline Pair pair_of(const Blocks& b, int k) {  // blocks 2k and 2k + 1 of the wave's lanes; k the same for all lanes
-  const int mine = 2 * k + ((threadIdx.x >> 5) & 1);
   Pair p;
-  p.ks = of_lane(b.ks, mine), p.ev = of_lane(b.ev, mine);
+  p.ks = of_lanes(b.ks, 2 * k, 2 * k + 1), p.ev = of_lanes(b.ev, 2 * k, 2 * k + 1);
   p.absent = (int)(b.absent >> (2 * k)) & 3, p.nan = (int)(b.nan >> (2 * k)) & 3, p.far = (int)(b.far >> (2 * k)) & 3;
   return p;
 }
@@ -517,7 +516,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
 }
 
 template <int CODES, int D, bool MARKS>
-__device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, float* lds) {
+__device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
   const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's: wave, wave + 4, ... of the unit's
   Rows<D> r;
@@ -540,12 +539,13 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int head, 
   constexpr int kPitch = D + 4;
   half8* q = (half8*)(lds + wave * kRows * kPitch);
   uint4v raw[D / 16];
-  // (the page is the first thing asked for, and everything else asked for before anything is waited for: loads come back in their order)
-  const int page = load_page(a, u.request, token(lane >> 1) + (lane & 1) * 16, u.hi);
-  __builtin_amdgcn_sched_barrier(0);
   request_rows<D, MARKS>(a, u, head, 0, r, raw);
   __builtin_amdgcn_sched_barrier(0);
-  on_page(a, page, head, token(lane >> 1) + (lane & 1) * 16, u.hi, b);
+  // (everything is asked for before anything is waited for: loads come back in their order)
+  if (u.hi - u.lo <= kUnitBlocks * kBlock)
+    on_block(a, 2 * (wave + 4 * (lane >> 1)) + (lane & 1) < kUnitBlocks ? listed : -1, head, b);
+  else
+    find(0);
   // (where the wave has fewer than two pairs, block 0 is read in their place)
   load_scales(a, b);
   if constexpr (MARKS) marks[0] = load_marks(a, b, 0), marks[1] = load_marks(a, b, 1);
@@ -632,70 +632,82 @@ struct ManyMarks {
 // The scores of pair i + 1 are taken between the exponentials of pair i, so that within a wave the matrix pipe and the vector pipe work at the same
 // time; pairs, not twice as many tokens, because two sets of scores, O and Q are what the registers hold.  One barrier for two pairs, 2j and 2j + 1:
 // in between the rings hold K up to 2j + 2 and V up to 2j + 1, and K of 2j + 3, 2j + 4 and V of 2j + 2, 2j + 3 are put where older ones were.
+// A wave brings one block of every second pair, 1 KB of neighbouring codes at a time.
 template <int CODES, int D, bool MARKS>
-__device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head, uint8_t* lds) {
-  constexpr int kPieces = D / 64;  // pieces of a pair's K, and of its V, that a wave brings
+__device__ inline void attend_many(const AttendArgs& a, const Unit& u, int listed, int head, uint8_t* lds) {
+  constexpr int kPieces = D / 64;  // 1 KB pieces of a block's K, and of its V
   constexpr int kEarly = D / 32;   // operands of K that are read ahead of the maximum
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
   const int n_pairs = (u.hi - u.lo + 31) >> 5;
-  const int odd = wave >> 1, piece0 = (wave & 1) * kPieces;  // this wave's share: pieces piece0 .. of every second pair
+  const int odd = wave >> 1, side = wave & 1;  // this wave's share: block `side` of every second pair
   ManyMarks& there = *(ManyMarks*)(lds + 8 * kPairBytes<D>);
   Rows<D> r;
   State<D> z;
   start(z);
   const bool works = wave * kRows < u.n_rows;
   const int first_token = u.pos0 + (wave * kRows >> a.g_shift);
-  Blocks b, ahead_k, ahead_v;  // of the pair under computation, and of those asked for: 32 pairs, from a multiple of 32 on
-  int group_k = 0, group_v = 0;
+  Blocks b, ahead;  // of the pair under computation, and of those asked for: 32 pairs, from a multiple of 32 on
+  int group = 0;
   uint4v k[kPieces], v[kPieces];
-  Marks marks{};
+  bool v_absent = false;
+  int tag = 0, position = 0;
   const int origin = MARKS ? a.row_position[u.s0 >> a.g_shift] : 0;
   auto find = [&](int i, Blocks& to) { find_blocks(a, u.request, head, u.lo + (i & ~31) * 32 + lane * 16, u.hi, to); };
+  // V of pair i and K of the one behind it: a piece of K is 4 runs of 16 dims x 16 tokens, one of V 64 dims x 16 tokens
+  auto block = [&](int i) {
+    if (i >> 5 != group) group = i >> 5, find(i, ahead);
+    return 2 * (i & 31) + side;
+  };
   auto request_k = [&](int i) {
-    if (i >> 5 != group_k) group_k = i >> 5, find(i, ahead_k);
-    const int x = 2 * (i & 31);
-    load_pieces(k_piece(a, __builtin_amdgcn_readlane(ahead_k.at, x), __builtin_amdgcn_readlane(ahead_k.at, x + 1), D) + piece0 * 512, k);
-    if constexpr (MARKS) marks = load_marks(a, ahead_k, i & 31);
+    const int x = block(i), at = __builtin_amdgcn_readlane(ahead.at, x);
+    const uint8_t* from = a.k + (int64_t)max(at, 0) * (kBlock * D);
+#pragma unroll
+    for (int y = 0; y < kPieces; ++y) k[y] = *(const uint4v*)(from + y * 1024 + lane * 16);
+    if constexpr (MARKS) {
+      const int64_t slot = (int64_t)__builtin_amdgcn_readlane(ahead.slot16, x) * kBlock + (lane & 15);
+      tag = a.slot_tag[slot], position = a.slot_position[slot];
+    }
   };
   auto request_v = [&](int i) {
-    if (i >> 5 != group_v) group_v = i >> 5, find(i, ahead_v);
-    const int x = 2 * (i & 31);
-    load_pieces(v_piece(a, __builtin_amdgcn_readlane(ahead_v.at, x), __builtin_amdgcn_readlane(ahead_v.at, x + 1), D) + piece0 * 512, v);
-  };
-  auto publish_k = [&](int i) {
-    half8* to = (half8*)(lds + (i & 3) * kPairBytes<D>) + piece0 * 2 * 64 + lane;
+    const int at = __builtin_amdgcn_readlane(ahead.at, block(i));
+    const uint8_t* from = a.v + (int64_t)max(at, 0) * (kBlock * D);
 #pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-      to[(2 * x) * 64] = codes_to_half8<CODES>(k[x][0], k[x][1]);
-      to[(2 * x + 1) * 64] = codes_to_half8<CODES>(k[x][2], k[x][3]);
+    for (int y = 0; y < kPieces; ++y) v[y] = *(const uint4v*)(from + y * 1024 + lane * 16);
+    v_absent = at < 0;
+  };
+  // K: run c = lane / 16 of a piece, token t = lane % 16, is lane m + 32 (c & 1) of operands 2 (c / 2) and the next, m = 8 (t / 4) + 4 side + t % 4
+  const int k_place = (lane >> 5) * 128 + ((lane >> 2) & 3) * 8 + side * 4 + (lane & 3) + ((lane >> 4) & 1) * 32;
+  const int v_place = (lane >> 5) * 128 + side * 32 + (lane & 31);
+  auto publish_k = [&](int i) {
+    half8* to = (half8*)(lds + (i & 3) * kPairBytes<D>) + k_place;
+#pragma unroll
+    for (int y = 0; y < kPieces; ++y) {
+      to[y * 256] = codes_to_half8<CODES>(k[y][0], k[y][1]);
+      to[y * 256 + 64] = codes_to_half8<CODES>(k[y][2], k[y][3]);
     }
-    if (MARKS && !(wave & 1) && !(lane & 16)) {
-      const int t = half * 16 + (lane & 15);
-      if (a.placed) there.position[i & 3][t] = (float)(marks.position - origin);
-      if (a.tagged) there.rows[i & 3][t] = there.tag_rows[marks.tag & 63];
+    if (MARKS && lane < 16) {
+      if (a.placed) there.position[i & 3][side * 16 + lane] = (float)(position - origin);
+      if (a.tagged) there.rows[i & 3][side * 16 + lane] = there.tag_rows[tag & 63];
     }
   };
   auto publish_v = [&](int i) {
-    const bool none = of_half((int)(__ballot(ahead_v.at < 0) >> (2 * (i & 31))) & 3);
-    half8* to = (half8*)(lds + (4 + (i & 3)) * kPairBytes<D>) + piece0 * 2 * 64 + lane;
+    half8* to = (half8*)(lds + (4 + (i & 3)) * kPairBytes<D>) + v_place;
 #pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
+    for (int y = 0; y < kPieces; ++y) {
       uint4v c;  // what is not there must not be NaN: its weight is 0
 #pragma unroll
-      for (int y = 0; y < 4; ++y) c[y] = none ? 0u : v[x][y];
-      to[(2 * x) * 64] = codes_to_half8<CODES>(c[0], c[1]);
-      to[(2 * x + 1) * 64] = codes_to_half8<CODES>(c[2], c[3]);
+      for (int x = 0; x < 4; ++x) c[x] = v_absent ? 0u : v[y][x];
+      to[y * 256] = codes_to_half8<CODES>(c[0], c[1]);
+      to[y * 256 + 64] = codes_to_half8<CODES>(c[2], c[3]);
     }
   };
   half8 q[D / 16];
   {
     uint4v raw[D / 16];
-    const int page = load_page(a, u.request, u.lo + lane * 16, u.hi);
-    __builtin_amdgcn_sched_barrier(0);
     request_rows<D, MARKS>(a, u, head, wave * kRows, r, raw);
     __builtin_amdgcn_sched_barrier(0);
-    on_page(a, page, head, u.lo + lane * 16, u.hi, b);
-    ahead_k = ahead_v = b;
+    on_block(a, u.lo + lane * 16 < u.hi ? listed : -1, head, b);
+    ahead = b;
     load_scales(a, b);
     request_k(odd);
     request_v(odd);
@@ -715,8 +727,8 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
   publish_k(odd);
   publish_v(odd);
   if (!odd) request_k(2), publish_k(2);
-  request_k(3 + odd);
   request_v(2 + odd);
+  request_k(3 + odd);
   __syncthreads();
   Pair p[1];
   float f[1];
@@ -751,13 +763,18 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[(2 * x + y) * 64], w[0][y], z.o[x], 0, 0, 0);
   };
+  // (in the last round what is put into the rings, and the products of the pair behind the last, are for nobody: their blocks are absent, or older ones)
+  auto publish = [&](int i) {
+    publish_v(i + 2 + odd);
+    publish_k(i + 3 + odd);
+  };
   if (works && n_pairs > 0) {
     look_ahead(0);
     products(0, s[0]);
     finish(0, s[0]);
   }
+  __syncthreads();  // (pair 4 goes where pair 0 is)
   for (int i = 0; i < n_pairs; i += 2) {
-    // (behind the last pair comes one of absent blocks, and where its successor would be the ring holds an older one: products for nobody)
     if (works) {
       look_ahead(i + 1);
       soften<D, 1>(z, s, f, p, w, [&] { products(i + 1, t[0]); });
@@ -767,13 +784,14 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int head,
       look_ahead(i + 2);
       soften<D, 1>(z, t, f, p, w, [&] { products(i + 2, s[0]); });
       add_values(i + 1);
+      publish(i);
       __builtin_amdgcn_s_setprio(0);
+    } else {
+      publish(i);
     }
     if (i + 2 < n_pairs) {
-      publish_k(i + 3 + odd);
-      publish_v(i + 2 + odd);
-      request_k(i + 5 + odd);
       request_v(i + 4 + odd);
+      request_k(i + 5 + odd);
       if (((i + 2) & 31) == 0) {
         find(i + 2, b);
         load_scales(a, b);
@@ -813,14 +831,17 @@ __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   constexpr int kFewBytes = 4 * kRows * (D + 4) * 4 + 4 * kRows * 8;
   constexpr int kManyBytes = 8 * kPairBytes<D> + sizeof(ManyMarks);
   __shared__ __attribute__((aligned(16))) uint8_t lds[MANY && kManyBytes > kFewBytes ? kManyBytes : kFewBytes];
-  const int head = blockIdx.x % a.g.Hkv;
-  const Unit u = a.units[blockIdx.x / a.g.Hkv];
+  const int head = blockIdx.x % a.g.Hkv, unit = blockIdx.x / a.g.Hkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Unit u = a.units[unit];
+  // the lane's block, asked for together with the unit: in attend_few pairs are dealt out to the four waves
+  const int dealt = a.unit_blocks[unit * kUnitBlocks + min(2 * (wave + 4 * (lane >> 1)) + (lane & 1), kUnitBlocks - 1)];
+  const int listed = MANY ? a.unit_blocks[unit * kUnitBlocks + lane] : 0;
   asm volatile("" ::"s"(u.request), "s"(u.s0), "s"(u.pos0), "s"(u.lo), "s"(u.hi), "s"(u.prefix), "s"(u.part));  // (one load, ahead of the branch)
   if (u.n_rows == 0) return;
   if (MANY && u.n_rows > kRows)
-    attend_many<CODES, D, MARKS>(a, u, head, lds);
+    attend_many<CODES, D, MARKS>(a, u, listed, head, lds);
   else
-    attend_few<CODES, D, MARKS>(a, u, head, (float*)lds);
+    attend_few<CODES, D, MARKS>(a, u, dealt, head, (float*)lds);
 }
 
 // Joins the partial rows of the tiles whose tokens are split.  D / 4 lanes hold a row, four dims apiece; the 1024 / D such groups of a

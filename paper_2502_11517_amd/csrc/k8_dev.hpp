@@ -13,6 +13,7 @@ constexpr int kEMin = -100, kEMax = 119;
 constexpr int kRows = 32;            // stacked rows (query row x head of the kv head's group) of one wave
 constexpr int kWideRows = 128;       // ... of one work-group whose four waves share tiles
 constexpr int kChunkTokens = 128;    // tokens a work-group takes at least
+constexpr int kUnitBlocks = 64;      // blocks of a unit that are listed with it
 enum { kE4m3 = 0, kInt8 = 1 };
 enum { kF32 = 0, kBf16 = 1, kF16 = 2 };
 
@@ -149,6 +150,13 @@ __device__ inline int count_le(const T* v, int n, int x) {
     if (v[m] <= x) lo = m + 1; else hi = m;
   }
   return lo;
+}
+
+// The block that holds a token of a request, by its page table.
+__device__ inline int block_of(const Geometry& g, const int* table, int request, int token, int hi) {
+  const int t = max(min(token, hi - 1), 0);
+  const int page = table[(int64_t)request * g.table_width + (t >> g.page_shift)];
+  return token < hi && page >= 0 && page < g.n_pages ? page * g.blocks_per_page + ((token & (g.page_tokens - 1)) >> 4) : -1;
 }
 
 }  // namespace k8

@@ -2,7 +2,8 @@
 //
 // Rows come in tiles of 32 (a work-group whose waves split the tokens) or, in requests with more stacked rows than that, of 128 (four
 // waves of 32 rows over the same tokens).  Tokens are split so that about as many work-groups run as the chip holds; a tile whose
-// tokens are split leaves partial rows, which k8_merge joins.
+// tokens are split leaves partial rows, which k8_merge joins.  One work-group; what it takes is the way through its dependent reads and sums,
+// so a step's tiles, where they fit, stay in LDS and are looked at once.
 #pragma once
 #include "k8_dev.hpp"
 
@@ -13,98 +14,170 @@ struct PlanArgs {
   int n_requests, n_rows;
   int wide;       // requests with more than 32 stacked rows take tiles of 128
   int capacity;   // units that the chip takes at once
+  int whole;      // tokens up to which a tile is not split
   int max_units, max_tiles, max_part_rows;
-  const int *length, *row_offsets, *prefix_len, *slot;
+  const int *length, *row_offsets, *prefix_len, *slot, *table;
   Unit* units;
+  int* unit_blocks;  // [max_units][kUnitBlocks]
   Tile* tiles;
   int* w_tiles;   // workspace, n_requests + 1: tiles of the requests up to and including this one
 };
 
 struct RequestTiles {
-  int row0, n, length, tile_rows, n_tiles;
+  int row0, n, length, prefix, tile_rows, n_tiles;
 };
 
 // Request r, or (r == n_requests) the rows behind the last request, which see nothing.
 __device__ inline RequestTiles request_tiles(const PlanArgs& a, int r) {
   RequestTiles q;
-  const int end = min(max(a.row_offsets[a.n_requests], 0), a.n_rows);
+  const int here = max(min(r, a.n_requests - 1), 0);
+  const int first = a.row_offsets[min(r, a.n_requests)], next = a.row_offsets[min(r + 1, a.n_requests)], all = a.row_offsets[a.n_requests];
+  const int length = a.length[here], prefix = a.prefix_len ? a.prefix_len[here] : 0;
+  const int end = min(max(all, 0), a.n_rows);
   if (r == a.n_requests) {
     q.row0 = end, q.n = a.n_rows - end, q.length = 0;
   } else {
-    q.row0 = min(max(a.row_offsets[r], 0), end);
-    q.n = min(max(a.row_offsets[r + 1], q.row0), end) - q.row0;
-    q.length = min(max(a.length[r], 0), a.g.table_width << a.g.page_shift);
+    q.row0 = min(max(first, 0), end);
+    q.n = min(max(next, q.row0), end) - q.row0;
+    q.length = min(max(length, 0), a.g.table_width << a.g.page_shift);
     if (a.slot && q.n > 0 && a.slot[q.row0] < 0) q.length = 0;
   }
+  q.prefix = min(max(prefix, 0), q.length);
   const int64_t stacked = (int64_t)q.n * a.g.G;
   q.tile_rows = a.wide && stacked > kRows ? kWideRows : kRows;
   q.n_tiles = (int)((stacked + q.tile_rows - 1) / q.tile_rows);
   return q;
 }
 
-__device__ inline Unit tile_of(const PlanArgs& a, int j) {
-  const int r = count_le(a.w_tiles, a.n_requests + 1, j);
+// Tile t of request r, unsplit.
+__device__ inline Unit tile_of(const PlanArgs& a, int r, const RequestTiles& q, int t) {
   Unit u{};
-  if (r > a.n_requests) return u;
-  const RequestTiles q = request_tiles(a, r);
-  const int t = j - (a.w_tiles[r] - q.n_tiles);
   const int first = t * q.tile_rows, stacked = q.n * a.g.G;
   u.request = max(min(r, a.n_requests - 1), 0);
   u.s0 = q.row0 * a.g.G + first;
   u.n_rows = min(stacked - first, q.tile_rows);
   u.pos0 = q.length - q.n + first / a.g.G;
-  if (q.length == 0) return u;
-  u.prefix = a.prefix_len ? min(max(a.prefix_len[r], 0), q.length) : 0;
+  u.prefix = q.prefix;
   const int last = q.length - q.n + (first + u.n_rows - 1) / a.g.G;
   u.hi = min(q.length, max(max(last + 1, 0), u.prefix));
   return u;
 }
 
+__device__ inline int chunks_of(int tokens) { return min((tokens + kChunkTokens - 1) / kChunkTokens, 1 << 20); }
+
+__device__ inline Unit part_of(Unit u, int k, int parts, int chunk, int row_at) {
+  const int hi = u.hi;
+  u.lo = k * chunk, u.hi = min(hi, (k + 1) * chunk), u.part = parts > 1 ? row_at + k * u.n_rows : -1;
+  return u;
+}
+
+// The first blocks of a unit, so that attention needs no page table on its way to them.
+__device__ inline void list_blocks(const PlanArgs& a, const Unit& u, int unit, int k) {
+  const int token = u.lo + k * kBlock;
+  a.unit_blocks[unit * kUnitBlocks + k] = token < u.hi ? block_of(a.g, a.table, u.request, token, u.hi) : -1;
+}
+
+// Fewer requests than NT and at most NT tiles: a thread to a request, then a thread to a tile.  Every work-group finds out the same and
+// writes down the unit of its own number, so that the whole plan is one launch whose way is no longer than one page's.
 template <int NT>
 __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
+  __shared__ int s_tmp[NT / 64 + 1], s_upto[NT], s_chunks[NT];
+  __shared__ RequestTiles s_request[NT];
+  __shared__ Unit s_unit;
+  const int tid = threadIdx.x, unit = blockIdx.x;
+  int mine = 0, n_tiles, work;
+  if (tid <= a.n_requests) {
+    s_request[tid] = request_tiles(a, tid);
+    mine = s_request[tid].n_tiles;
+  }
+  const int upto = group_scan<NT>(mine, s_tmp, n_tiles);
+  s_upto[tid] = upto;
+  if (tid == 0) s_unit = Unit{};
+  __syncthreads();
+  n_tiles = min(n_tiles, a.max_tiles);
+  Unit u{};
+  if (tid < n_tiles) {
+    const int r = min(count_le(s_upto, a.n_requests + 1, tid), a.n_requests);
+    const RequestTiles q = s_request[r];
+    u = tile_of(a, r, q, tid - (s_upto[r] - q.n_tiles));
+  }
+  const int own = tid < n_tiles ? chunks_of(u.hi) : 0;
+  s_chunks[tid] = own;
+  group_scan<NT>(own, s_tmp, work);
+  // Chunks of this many times 128 tokens.  With one remainder per tile that makes at most `capacity` units while there are few tiles; from
+  // half as many tiles on, chunks are twice the mean load.
+  const int room = max(max(a.capacity - n_tiles, a.capacity / 2), 1);
+  int chunk = max(1, (work + room - 1) / room);
+  if (n_tiles > 1 && n_tiles < a.capacity) {
+    // the least that does: 64 candidates from the one without remainders on, looked at by a lane each
+    const int least = max(1, (work + a.capacity - 1) / a.capacity);
+    if (tid < 64) {
+      const int c = least + tid;
+      int units = 0;
+      for (int j = 0; j < n_tiles; ++j) units += max(1, (s_chunks[j] + c - 1) / c);
+      const uint64_t fits = __ballot(units <= a.capacity);
+      if (tid == 0) s_tmp[NT / 64] = fits ? least + __builtin_ctzll(fits) : chunk;
+    }
+    __syncthreads();
+    chunk = min(chunk, s_tmp[NT / 64]);
+  }
+  chunk = max(chunk * kChunkTokens, a.whole);
+  const int parts = tid < n_tiles ? max(1, (u.hi + chunk - 1) / chunk) : 0;
+  int all;
+  const int at = group_scan<NT>(parts, s_tmp, all) - parts;
+  const int rows = parts > 1 ? parts * u.n_rows : 0;
+  const int row_at = group_scan<NT>(rows, s_tmp, all) - rows;
+  const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;  // (the host's bounds hold: see pasta_kv8.hip)
+  if (unit >= at && unit < at + parts && fits) s_unit = part_of(u, unit - at, parts, chunk, row_at);
+  if (unit == 0 && tid < a.max_tiles) a.tiles[tid] = Tile{u.s0, u.n_rows, row_at, tid < n_tiles && fits ? parts : 0};
+  __syncthreads();
+  if (tid == 0) a.units[unit] = s_unit;
+  if (tid < kUnitBlocks && s_unit.n_rows) list_blocks(a, s_unit, unit, tid);
+}
+
+// Any number of them, one work-group, NT at a time; the units' blocks follow in a launch of their own.
+template <int NT>
+__global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
   __shared__ int s_tmp[NT / 64];
   const int tid = threadIdx.x;
-  int n_tiles = 0;
+  int n_tiles = 0, work = 0;
   for (int r0 = 0; r0 <= a.n_requests; r0 += NT) {
     const int r = r0 + tid;
     int mine = 0, all;
     if (r <= a.n_requests) mine = request_tiles(a, r).n_tiles;
-    const int upto = n_tiles + group_scan<NT>(mine, s_tmp, all);
-    if (r <= a.n_requests) a.w_tiles[r] = upto;
+    const int now = n_tiles + group_scan<NT>(mine, s_tmp, all);
+    if (r <= a.n_requests) a.w_tiles[r] = now;
     n_tiles += all;
   }
   __syncthreads();
   n_tiles = min(n_tiles, a.max_tiles);
-  int work = 0;  // (in chunks of the least length: below 2^31 / 128 for a table's tokens, times the tiles)
+  auto tile = [&](int j) {
+    const int r = min(count_le(a.w_tiles, a.n_requests + 1, j), a.n_requests);
+    const RequestTiles q = request_tiles(a, r);
+    return tile_of(a, r, q, j - (a.w_tiles[r] - q.n_tiles));
+  };
   for (int j0 = 0; j0 < n_tiles; j0 += NT) {
     int all;
-    const int j = j0 + tid;
-    group_scan<NT>(j < n_tiles ? min((tile_of(a, j).hi + kChunkTokens - 1) / kChunkTokens, 1 << 20) : 0, s_tmp, all);
+    group_scan<NT>(j0 + tid < n_tiles ? chunks_of(tile(j0 + tid).hi) : 0, s_tmp, all);
     work += all;
   }
-  // Chunks of this many times 128 tokens: with one remainder per tile at most `capacity` units, while there are few tiles; from half as
-  // many tiles on, chunks of twice the mean load.
   const int room = max(max(a.capacity - n_tiles, a.capacity / 2), 1);
-  const int chunk = max(1, (work + room - 1) / room) * kChunkTokens;
+  const int chunk = max(max(1, (work + room - 1) / room) * kChunkTokens, a.whole);
   int n_units = 0, n_part_rows = 0;
   for (int j0 = 0; j0 < n_tiles; j0 += NT) {
     const int j = j0 + tid;
     Unit u{};
     int parts = 0, all, all_rows;
     if (j < n_tiles) {
-      u = tile_of(a, j);
+      u = tile(j);
       parts = max(1, (u.hi + chunk - 1) / chunk);
     }
     const int at = n_units + group_scan<NT>(parts, s_tmp, all) - parts;
     const int rows = parts > 1 ? parts * u.n_rows : 0;
     const int row_at = n_part_rows + group_scan<NT>(rows, s_tmp, all_rows) - rows;
     if (j < n_tiles) {
-      const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;  // (the host's bounds hold: see pasta_kv8_plan)
-      const int hi = u.hi;
-      for (int k = 0; k < parts && fits; ++k) {
-        u.lo = k * chunk, u.hi = min(hi, (k + 1) * chunk), u.part = parts > 1 ? row_at + k * u.n_rows : -1;
-        a.units[at + k] = u;
-      }
+      const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;
+      for (int k = 0; k < parts && fits; ++k) a.units[at + k] = part_of(u, k, parts, chunk, row_at);
       a.tiles[j] = Tile{u.s0, u.n_rows, row_at, fits ? parts : 0};
     }
     n_units += all;
@@ -113,6 +186,13 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
   // what the launches of k8_attend and k8_merge go over beyond that is empty
   for (int j = min(n_units, a.max_units) + tid; j < a.max_units; j += NT) a.units[j] = Unit{};
   for (int j = n_tiles + tid; j < a.max_tiles; j += NT) a.tiles[j] = Tile{};
+}
+
+__global__ __launch_bounds__(256) void k8_unit_blocks(PlanArgs a) {
+  const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (unit >= a.max_units) return;
+  const Unit u = a.units[unit];
+  if (u.n_rows) list_blocks(a, u, unit, threadIdx.x & 63);
 }
 
 }  // namespace k8

@@ -15,6 +15,7 @@
 namespace {
 
 constexpr uint64_t kMagic = 0x3876'6b61'7473'6170ull;
+constexpr int kWholeTokens = 384;  // of a tile that is not split
 constexpr int kUnitsAtOnce = 512;  // work-groups of the attention: two per CU
 
 struct Bounds {
@@ -30,6 +31,7 @@ struct pasta_kv8 {
   // workspace
   int *kept = nullptr, *old_pages = nullptr, *take = nullptr, *top = nullptr, *tiles_upto = nullptr;
   k8::Unit* units = nullptr;
+  int* unit_blocks = nullptr;
   k8::Tile* tiles = nullptr;
   k8::float2v* part_ml = nullptr;
   float* part_acc = nullptr;
@@ -90,6 +92,7 @@ uint64_t lay_out(const pasta_kv8_config& c, pasta_kv8* h) {
   take(h->top, 1);
   take(h->tiles_upto, c.max_requests + 1);
   take(h->units, b.units);
+  take(h->unit_blocks, b.units * k8::kUnitBlocks);
   take(h->tiles, b.tiles);
   take(h->part_ml, b.part_rows * c.n_kv_heads);
   take(h->part_acc, b.part_rows * c.n_kv_heads * c.head_dim);
@@ -213,7 +216,7 @@ extern "C" int32_t pasta_kv8_plan(pasta_kv8* h, const pasta_kv8_plan_args* a) {
   const pasta_kv8_config& c = h->cfg;
   if (a->n_requests < 0 || a->n_rows < 0 || a->max_request_rows < 0) return PASTA_E_INVAL;
   if (a->n_requests > c.max_requests || a->n_rows > c.max_rows) return PASTA_E_CAPACITY;
-  if (!a->row_offsets || !c.workspace || (a->n_requests && !a->length)) return PASTA_E_INVAL;
+  if (!a->row_offsets || !c.workspace || !c.page_table || (a->n_requests && !a->length)) return PASTA_E_INVAL;
   if (!aligned(a->length, 4) || !aligned(a->row_offsets, 4) || !aligned(a->prefix_len, 4) || !aligned(a->slot, 4)) return PASTA_E_INVAL;
   h->planned = true;
   h->plan_rows = a->n_rows;
@@ -224,13 +227,17 @@ extern "C" int32_t pasta_kv8_plan(pasta_kv8* h, const pasta_kv8_plan_args* a) {
   k8::PlanArgs k{};
   k.g = h->g, k.n_requests = a->n_requests, k.n_rows = a->n_rows, k.wide = h->plan_wide, k.capacity = (int)h->plan.capacity;
   k.max_units = (int)h->plan.units, k.max_tiles = (int)h->plan.tiles, k.max_part_rows = (int)h->plan.part_rows;
-  k.length = a->length, k.row_offsets = a->row_offsets, k.prefix_len = a->prefix_len, k.slot = a->slot;
-  k.units = h->units, k.tiles = h->tiles, k.w_tiles = h->tiles_upto;
+  k.length = a->n_requests ? a->length : a->row_offsets;  // (read, not used, without a request)
+  k.row_offsets = a->row_offsets, k.prefix_len = a->prefix_len, k.slot = a->slot;
+  k.table = c.page_table, k.whole = kWholeTokens;
+  k.units = h->units, k.unit_blocks = h->unit_blocks, k.tiles = h->tiles, k.w_tiles = h->tiles_upto;
   hipStream_t s = (hipStream_t)c.hip_stream;
-  if (h->plan.tiles <= 64 && a->n_requests < 64)
-    k8::k8_plan<64><<<1, 64, 0, s>>>(k);
-  else
-    k8::k8_plan<1024><<<1, 1024, 0, s>>>(k);
+  if (h->plan.tiles <= 256 && a->n_requests < 256) {
+    k8::k8_plan<256><<<(unsigned)h->plan.units, 256, 0, s>>>(k);
+  } else {
+    k8::k8_plan_long<1024><<<1, 1024, 0, s>>>(k);
+    k8::k8_unit_blocks<<<(unsigned)((h->plan.units + 3) / 4), 256, 0, s>>>(k);
+  }
   const int32_t rc = launched();
   if (rc != PASTA_OK) h->planned = false;
   return rc;
@@ -278,7 +285,8 @@ extern "C" int32_t pasta_kv8_attend(pasta_kv8* h, const pasta_kv8_attend_args* a
   if (!k.tagged) k.row_see = (const uint64_t*)a->q, k.slot_tag = (const uint8_t*)c.k_codes;
   if (!k.placed) k.row_position = (const int*)a->q, k.slot_position = (const int*)c.k_codes;
   if (!k.lowered) k.slopes = (const float*)a->q;
-  k.units = h->units, k.tiles = h->tiles;
+  k.units = h->units, k.unit_blocks = h->unit_blocks, k.tiles = h->tiles;
+  while ((1 << k.block_shift) < k.g.blocks_per_page) k.block_shift++;
   k.q = a->q, k.out = a->out, k.lse = a->lse, k.part_ml = h->part_ml, k.part_acc = h->part_acc;
   hipStream_t s = (hipStream_t)c.hip_stream;
   const int64_t groups = h->plan.units * c.n_kv_heads;
@@ -287,7 +295,7 @@ extern "C" int32_t pasta_kv8_attend(pasta_kv8* h, const pasta_kv8_attend_args* a
     c.head_dim == 128 ? launch_attend<k8::kE4m3, 128>(k, many, groups, s) : launch_attend<k8::kE4m3, 64>(k, many, groups, s);
   else
     c.head_dim == 128 ? launch_attend<k8::kInt8, 128>(k, many, groups, s) : launch_attend<k8::kInt8, 64>(k, many, groups, s);
-  if ((int64_t)c.pages_per_request * c.page_tokens > k8::kChunkTokens) {  // no tile is split otherwise
+  if ((int64_t)c.pages_per_request * c.page_tokens > kWholeTokens) {  // no tile is split otherwise
     const int64_t tiles = h->plan.tiles * c.n_kv_heads;
     int64_t split = (2048 + tiles - 1) / tiles;  // work-groups to a tile: rows, one by one where there are so few tiles
     if (split > h->plan.merge_rows) split = h->plan.merge_rows;
