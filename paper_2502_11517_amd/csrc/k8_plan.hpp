@@ -65,9 +65,11 @@ __device__ inline Unit tile_of(const PlanArgs& a, int r, const RequestTiles& q, 
 
 __device__ inline int chunks_of(int tokens) { return min((tokens + kChunkTokens - 1) / kChunkTokens, 1 << 20); }
 
+__device__ inline int parts_of(const PlanArgs& a, int tokens, int chunk) { return tokens <= max(chunk, a.whole) ? 1 : (tokens + chunk - 1) / chunk; }
+
 __device__ inline Unit part_of(Unit u, int k, int parts, int chunk, int row_at) {
   const int hi = u.hi;
-  u.lo = k * chunk, u.hi = min(hi, (k + 1) * chunk), u.part = parts > 1 ? row_at + k * u.n_rows : -1;
+  u.lo = k * chunk, u.hi = parts > 1 ? min(hi, (k + 1) * chunk) : hi, u.part = parts > 1 ? row_at + k * u.n_rows : -1;
   return u;
 }
 
@@ -121,8 +123,8 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
     __syncthreads();
     chunk = min(chunk, s_tmp[NT / 64]);
   }
-  chunk = max(chunk * kChunkTokens, a.whole);
-  const int parts = tid < n_tiles ? max(1, (u.hi + chunk - 1) / chunk) : 0;
+  chunk *= kChunkTokens;
+  const int parts = tid < n_tiles ? parts_of(a, u.hi, chunk) : 0;
   int all;
   const int at = group_scan<NT>(parts, s_tmp, all) - parts;
   const int rows = parts > 1 ? parts * u.n_rows : 0;
@@ -162,7 +164,7 @@ __global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
     work += all;
   }
   const int room = max(max(a.capacity - n_tiles, a.capacity / 2), 1);
-  const int chunk = max(max(1, (work + room - 1) / room) * kChunkTokens, a.whole);
+  const int chunk = max(1, (work + room - 1) / room) * kChunkTokens;
   int n_units = 0, n_part_rows = 0;
   for (int j0 = 0; j0 < n_tiles; j0 += NT) {
     const int j = j0 + tid;
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
     int parts = 0, all, all_rows;
     if (j < n_tiles) {
       u = tile(j);
-      parts = max(1, (u.hi + chunk - 1) / chunk);
+      parts = parts_of(a, u.hi, chunk);
     }
     const int at = n_units + group_scan<NT>(parts, s_tmp, all) - parts;
     const int rows = parts > 1 ? parts * u.n_rows : 0;
