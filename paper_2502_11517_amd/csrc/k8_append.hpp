@@ -58,12 +58,24 @@ __device__ inline void load_row(const void* base, int64_t at, float (&x)[N]) {  
   }
 }
 
-__device__ inline uint32_t wave_max(uint32_t x) {
-  for (int d = 32; d; d >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
-  return x;
+// Bits of the largest magnitude of N values that load_row gave.
+template <int N>
+__device__ inline uint32_t magnitude(const float (&x)[N], uint32_t amax) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) amax = max(amax, __float_as_uint(x[i]) & 0x7fffffffu);
+  return amax;
+}
+
+// Past kEMax a value can be beyond Q times the scale, and is Q then.
+template <int CODES, int N>
+__device__ inline void hold(float (&x)[N], float inverse) {
+  constexpr float kTop = CODES == kE4m3 ? 448.f : 127.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = fminf(fmaxf(x[i], -kTop / inverse), kTop / inverse);
 }
 
 struct RunScale {
+  bool held;      // the exponent is kEMax
   float inverse;  // 2^-e of the new codes
   float again;    // 2^(f-e) for the codes ahead of the run
   float scale;    // what the block gets
@@ -86,6 +98,7 @@ __device__ inline RunScale run_scale(uint32_t amax, int offset, float was) {
       e = max(e, f);
     }
   }
+  s.held = e == kEMax;
   s.inverse = pow2f(-e);
   s.scale = s.lost ? __builtin_nanf("") : pow2f(e);
   return s;
@@ -104,9 +117,11 @@ __device__ inline void append_k(const AppendArgs& a, int row, int n, int offset,
   for (int j = 0; j < kPieces; ++j) {
     for (int i = 0; i < 16; ++i) x[j][i] = 0.f;
     if (mine) load_row<IN, 16>(a.k_new, ((int64_t)(row + token - offset) * a.g.Hkv + head) * D + (part + 4 * j) * 16, x[j]);
-    for (int i = 0; i < 16; ++i) amax = max(amax, __float_as_uint(x[j][i]) & 0x7fffffffu);
+    amax = magnitude(x[j], amax);
   }
   const RunScale s = run_scale<CODES>(wave_max(amax), offset, was);
+  if (s.held)
+    for (int j = 0; j < kPieces; ++j) hold<CODES>(x[j], s.inverse);
   const bool before = token < offset;
   for (int j = 0; j < kPieces; ++j) {
     uint4v* to = (uint4v*)(codes + ((part + 4 * j) * kBlock + token) * 16);
@@ -146,9 +161,11 @@ __device__ inline void append_v(const AppendArgs& a, int row, int n, int offset,
     if (t >= offset && t < offset + n) load_row<IN, N>(a.v_new, ((int64_t)(row + t - offset) * a.g.Hkv + head) * D + lane * N, x[t]);
   }
 #pragma unroll
-  for (int t = 0; t < kBlock; ++t)
-    for (int j = 0; j < N; ++j) amax = max(amax, __float_as_uint(x[t][j]) & 0x7fffffffu);
+  for (int t = 0; t < kBlock; ++t) amax = magnitude(x[t], amax);
   const RunScale s = run_scale<CODES>(wave_max(amax), offset, was);
+  if (s.held)
+#pragma unroll
+    for (int t = 0; t < kBlock; ++t) hold<CODES>(x[t], s.inverse);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     uint4v w;

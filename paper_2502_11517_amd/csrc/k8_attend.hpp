@@ -172,9 +172,7 @@ __device__ inline void load_scales(const AttendArgs& a, Blocks& b) {
 __device__ inline void finish_scales(Blocks& b, int& most) {
   const int x = (int)((__float_as_uint(b.vs) >> 23) & 255) - 127;
   const bool there = b.at >= 0, nan = x == 128;
-  int e = there && !nan ? x : kEMin;
-  for (int d = 32; d; d >>= 1) e = max(e, __shfl_xor(e, d));
-  most = max(most, __builtin_amdgcn_readfirstlane(e));
+  most = max(most, (int)__builtin_amdgcn_readfirstlane(wave_max(there && !nan ? x + 127 : 0)) - 127);
   b.ev = (float)(there && !nan ? max(x, most - kScaleSpan) : most);
   b.absent = __ballot(!there);
   b.nan = __ballot(there && nan);

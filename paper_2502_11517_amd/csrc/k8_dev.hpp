@@ -1,6 +1,7 @@
 // Shared by the kernels of the 8-bit cache: its geometry, the plan's records, conversions of codes, sums over a work-group.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -59,18 +60,17 @@ __device__ inline int scale_exponent(uint32_t amax_bits) {
   return min(max(e, kEMin), kEMax);
 }
 
-// Four values in units of the scale -> four codes; nearest, ties to even.
+// Four values in units of the scale, at most Q in magnitude -> four codes; nearest, ties to even.
 template <int CODES>
 __device__ inline uint32_t encode4(float a, float b, float c, float d) {
   if constexpr (CODES == kE4m3) {
-    // beyond 448 only where the exponent was held at kEMax
-    a = fminf(fmaxf(a, -448.f), 448.f), b = fminf(fmaxf(b, -448.f), 448.f);
-    c = fminf(fmaxf(c, -448.f), 448.f), d = fminf(fmaxf(d, -448.f), 448.f);
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
   } else {
-    auto one = [](float x) { return (uint32_t)(int)rintf(fminf(fmaxf(x, -127.f), 127.f)) & 255u; };
-    return one(a) | one(b) << 8 | one(c) << 16 | one(d) << 24;
+    // at 3 * 2^22 a step of fp32 is 1: the sum rounds to a whole number, whose low byte is the code
+    auto whole = [](float x) { return __float_as_uint(x + 12582912.f); };
+    const uint32_t lo = __builtin_amdgcn_perm(whole(b), whole(a), 0x0c0c0400u), hi = __builtin_amdgcn_perm(whole(d), whole(c), 0x04000c0cu);
+    return lo | hi;
   }
 }
 
@@ -107,6 +107,18 @@ __device__ inline half8 codes_to_half8(uint32_t a, uint32_t b) {
     for (int i = 0; i < 4; ++i) r.h[i] -= off;
   }
   return r.v;
+}
+
+// Largest of the wave's 64 values, in every lane: rotations within rows of 16 lanes, then the rows.
+__device__ inline uint32_t wave_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false));  // row_ror:8
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, false));
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max(b[0], b[1]);
 }
 
 // Sum over the lanes below and including this one.

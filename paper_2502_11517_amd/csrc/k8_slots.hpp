@@ -1,15 +1,17 @@
 // Places of a step's rows: pages off and onto the stack, entries of the page tables, slots.
 //
-// One work-group does everything that goes in the order of the requests (two passes over them, NT at a time, with sums that carry
-// over); the rows follow, each by itself: a new page has a first row, which writes its entry of the table.  Nothing here is bound
-// by bandwidth; a step takes a handful of dependent reads and, per pass, two barriers for each sum.  Rows beyond kSlotsHere go to a
-// second launch over the whole chip.
+// Everything goes in the order of the requests, by sums over them; nothing is bound by bandwidth.  What a step takes is its dependent reads, one
+// behind the other, so with up to a thread per request all of them are asked for at once, the sums stay in LDS, and every work-group finds out the
+// same for itself: the first writes what belongs to the requests, all of them return pages and place rows, in one launch.  A page that comes back and is taken in the
+// same step is looked up where it was, not on the stack.  Where lengths or the count are written in place that does not go (one work-group may write
+// what another has still to read), and with more requests than threads neither: one work-group then does the requests, and rows beyond kSlotsHere
+// follow in a second launch.
 #pragma once
 #include "k8_dev.hpp"
 
 namespace k8 {
 
-constexpr int kSlotsHere = 4096;  // rows that the one work-group places itself
+constexpr int kSlotsHere = 4096;  // rows that one work-group places itself
 
 struct SlotsArgs {
   Geometry g;
@@ -31,12 +33,13 @@ struct RequestRows {
   bool fits;
 };
 
-__device__ inline RequestRows request_rows(const SlotsArgs& a, int r) {
+__device__ inline RequestRows request_rows_of(const SlotsArgs& a, int r) {
   RequestRows q;
+  const int length = a.length[r], keep = a.keep ? a.keep[r] : INT32_MAX, first = a.row_offsets[r], next = a.row_offsets[r + 1];
   const int cap = a.g.table_width << a.g.page_shift;
-  q.length = min(max(a.length[r], 0), cap);
-  q.kept = a.keep ? min(q.length, max(a.keep[r], 0)) : q.length;
-  const int lo = min(max(a.row_offsets[r], 0), a.n_rows), hi = min(max(a.row_offsets[r + 1], lo), a.n_rows);
+  q.length = min(max(length, 0), cap);
+  q.kept = min(q.length, max(keep, 0));
+  const int lo = min(max(first, 0), a.n_rows), hi = min(max(next, lo), a.n_rows);
   q.n = hi - lo;
   const int64_t want = (int64_t)q.kept + q.n;
   q.fits = want <= cap;
@@ -45,28 +48,8 @@ __device__ inline RequestRows request_rows(const SlotsArgs& a, int r) {
   return q;
 }
 
-__device__ inline void place_row(const SlotsArgs& a, int i) {
-  int slot = -1;
-  const int r = count_le(a.row_offsets + 1, a.n_requests, i);
-  if (r < a.n_requests) {
-    const int take = a.w_take[r];
-    if (take >= 0) {
-      const int p = a.w_kept[r] + i - max(a.row_offsets[r], 0);
-      const int page_of = p >> a.g.page_shift, old = a.w_old[r];
-      if (p >= 0 && page_of < a.g.table_width) {
-        int* entry = a.table + (int64_t)r * a.g.table_width + page_of;
-        int page;
-        if (page_of < old) {
-          page = *entry;
-        } else {
-          const int at = a.w_top[0] - 1 - (take + page_of - old);
-          page = at >= 0 && at < a.g.n_pages ? a.stack[at] : -1;
-          if ((p & (a.g.page_tokens - 1)) == 0) *entry = page;
-        }
-        if (page >= 0 && page < a.g.n_pages) slot = (page << a.g.page_shift) + (p & (a.g.page_tokens - 1));
-      }
-    }
-  }
+__device__ inline void give_slot(const SlotsArgs& a, int i, int page, int p) {
+  const int slot = page >= 0 && page < a.g.n_pages ? (page << a.g.page_shift) + (p & (a.g.page_tokens - 1)) : -1;
   a.slot[i] = slot;
   if (slot >= 0) {
     if (a.row_tag) a.slot_tag[slot] = a.row_tag[i];
@@ -74,8 +57,82 @@ __device__ inline void place_row(const SlotsArgs& a, int i) {
   }
 }
 
+// At most NT requests.
 template <int NT>
 __global__ __launch_bounds__(NT) void k8_slots(SlotsArgs a) {
+  __shared__ int s_tmp[NT / 64], s_next[NT], s_first[NT], s_kept[NT], s_old[NT], s_take[NT], s_freed[NT], s_page[NT];
+  const int tid = threadIdx.x;
+  const int have = min(max(*a.free_count, 0), a.g.n_pages);
+  RequestRows q{};
+  int first = 0, next = INT32_MAX;
+  if (tid < a.n_requests) {
+    q = request_rows_of(a, tid);
+    first = max(a.row_offsets[tid], 0), next = a.row_offsets[tid + 1];
+  }
+  const int back = q.fits ? max(q.old_pages - q.new_pages, 0) : 0, need = q.fits ? max(q.new_pages - q.old_pages, 0) : 0;
+  int freed, asked, taken;
+  const int back_upto = group_scan<NT>(back, s_tmp, freed);
+  const int need_upto = group_scan<NT>(need, s_tmp, asked);  // (at most n_requests * table_width pages)
+  const int top = min(have + freed, a.g.n_pages);
+  const bool served = q.fits && (need == 0 || need_upto <= top);
+  s_next[tid] = next, s_first[tid] = first, s_kept[tid] = q.kept, s_old[tid] = q.old_pages, s_take[tid] = served ? need_upto - need : -1;
+  s_freed[tid] = back_upto, s_page[tid] = q.new_pages - (back_upto - back);
+  group_scan<NT>(served ? need : 0, s_tmp, taken);  // (its barriers stand between the writes above and what follows)
+  // page j of those that come back
+  auto came_back = [&](int j) {
+    const int r = min(count_le(s_freed, NT, j), max(a.n_requests - 1, 0));
+    return a.table[(int64_t)r * a.g.table_width + s_page[r] + j];
+  };
+  if (blockIdx.x == 0) {
+    if (tid < a.n_requests) a.length_out[tid] = served ? q.kept + q.n : q.length;
+    if (tid == 0) *a.free_out = top - taken;
+  }
+  for (int j = blockIdx.x * NT + tid; j < freed; j += gridDim.x * NT)
+    if (have + j < a.g.n_pages) a.stack[have + j] = came_back(j);
+  for (int i = blockIdx.x * NT + tid; i < a.n_rows; i += gridDim.x * NT) {
+    const int r = count_le(s_next, a.n_requests, i);
+    int page = -1, p = 0;
+    if (r < a.n_requests && s_take[r] >= 0) {
+      p = s_kept[r] + i - s_first[r];
+      const int of = p >> a.g.page_shift, old = s_old[r];
+      if (p >= 0 && of < a.g.table_width) {
+        int* entry = a.table + (int64_t)r * a.g.table_width + of;
+        if (of < old) {
+          page = *entry;
+        } else {
+          const int at = top - 1 - (s_take[r] + of - old);
+          if (at >= 0) page = at < have ? a.stack[at] : came_back(at - have);
+          if ((p & (a.g.page_tokens - 1)) == 0) *entry = page;
+        }
+      }
+    }
+    give_slot(a, i, page, p);
+  }
+}
+
+__device__ inline void place_row(const SlotsArgs& a, int i) {
+  const int r = count_le(a.row_offsets + 1, a.n_requests, i);
+  int page = -1, p = 0;
+  if (r < a.n_requests && a.w_take[r] >= 0) {
+    p = a.w_kept[r] + i - max(a.row_offsets[r], 0);
+    const int of = p >> a.g.page_shift, old = a.w_old[r];
+    if (p >= 0 && of < a.g.table_width) {
+      int* entry = a.table + (int64_t)r * a.g.table_width + of;
+      if (of < old) {
+        page = *entry;
+      } else {
+        const int at = a.w_top[0] - 1 - (a.w_take[r] + of - old);
+        if (at >= 0 && at < a.g.n_pages) page = a.stack[at];
+        if ((p & (a.g.page_tokens - 1)) == 0) *entry = page;
+      }
+    }
+  }
+  give_slot(a, i, page, p);
+}
+
+// Any number of requests, NT at a time, or lengths in place; one work-group.
+template <int NT>
+__global__ __launch_bounds__(NT) void k8_slots_long(SlotsArgs a) {
   __shared__ int s_tmp[NT / 64], s_first[NT], s_page[NT];
   const int tid = threadIdx.x;
   const int have = min(max(*a.free_count, 0), a.g.n_pages);
@@ -85,7 +142,7 @@ __global__ __launch_bounds__(NT) void k8_slots(SlotsArgs a) {
     const int r = r0 + tid;
     int mine = 0, first = 0;
     if (r < a.n_requests) {
-      const RequestRows q = request_rows(a, r);
+      const RequestRows q = request_rows_of(a, r);
       mine = q.fits ? max(q.old_pages - q.new_pages, 0) : 0;
       first = q.new_pages;
     }
@@ -112,11 +169,11 @@ __global__ __launch_bounds__(NT) void k8_slots(SlotsArgs a) {
     RequestRows q{};
     int need = 0;
     if (r < a.n_requests) {
-      q = request_rows(a, r);
+      q = request_rows_of(a, r);
       need = q.fits ? max(q.new_pages - q.old_pages, 0) : 0;
     }
-    int all;
-    const int upto = asked + group_scan<NT>(need, s_tmp, all);  // (at most n_requests * table_width pages)
+    int all, got;
+    const int upto = asked + group_scan<NT>(need, s_tmp, all);
     const bool served = q.fits && (need == 0 || upto <= top);
     if (r < a.n_requests) {
       a.w_kept[r] = q.kept;
@@ -124,7 +181,6 @@ __global__ __launch_bounds__(NT) void k8_slots(SlotsArgs a) {
       a.w_take[r] = served ? upto - need : -1;
       a.length_out[r] = served ? q.kept + q.n : q.length;
     }
-    int got;
     group_scan<NT>(served ? need : 0, s_tmp, got);
     taken += got;
     asked += all;

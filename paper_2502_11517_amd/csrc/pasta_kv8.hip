@@ -99,6 +99,8 @@ uint64_t lay_out(const pasta_kv8_config& c, pasta_kv8* h) {
   return at;
 }
 
+bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) { return (uintptr_t)a < (uintptr_t)(b + m) && (uintptr_t)b < (uintptr_t)(a + n); }
+
 int32_t launched() { return hipGetLastError() == hipSuccess ? PASTA_OK : PASTA_E_DEVICE; }
 
 }  // namespace
@@ -162,11 +164,21 @@ extern "C" int32_t pasta_kv8_slots(pasta_kv8* h, const pasta_kv8_slots_args* a) 
   k.table = c.page_table, k.stack = c.free_pages, k.slot_tag = c.slot_tag, k.slot_position = c.slot_position;
   k.w_kept = h->kept, k.w_old = h->old_pages, k.w_take = h->take, k.w_top = h->top;
   hipStream_t s = (hipStream_t)c.hip_stream;
-  if (a->n_requests <= 64 && a->n_rows <= 256)
-    k8::k8_slots<64><<<1, 64, 0, s>>>(k);
-  else
-    k8::k8_slots<1024><<<1, 1024, 0, s>>>(k);
-  if (a->n_rows > k8::kSlotsHere) k8::k8_place<<<(a->n_rows + 255) / 256, 256, 0, s>>>(k);
+  const bool in_place = overlap(a->length, a->n_requests, a->length_out, a->n_requests) || overlap(a->free_count, 1, a->free_out, 1) ||
+                        (a->keep && overlap(a->keep, a->n_requests, a->length_out, a->n_requests));
+  const int rows = (a->n_rows + 255) / 256;
+  if (a->n_requests <= 64 && a->n_rows <= 256) {
+    k8::k8_slots<64><<<in_place || !rows ? 1 : (a->n_rows + 63) / 64, 64, 0, s>>>(k);
+  } else if (a->n_requests <= 256 && (!in_place || a->n_rows <= k8::kSlotsHere)) {
+    k8::k8_slots<256><<<in_place || !rows ? 1 : rows, 256, 0, s>>>(k);
+  } else if (a->n_requests <= 512 && (!in_place || a->n_rows <= k8::kSlotsHere)) {
+    k8::k8_slots<512><<<in_place || !rows ? 1 : (a->n_rows + 511) / 512, 512, 0, s>>>(k);
+  } else if (a->n_requests <= 1024 && (!in_place || a->n_rows <= k8::kSlotsHere)) {
+    k8::k8_slots<1024><<<in_place || !rows ? 1 : (a->n_rows + 1023) / 1024, 1024, 0, s>>>(k);
+  } else {
+    k8::k8_slots_long<1024><<<1, 1024, 0, s>>>(k);
+    if (a->n_rows > k8::kSlotsHere) k8::k8_place<<<rows, 256, 0, s>>>(k);
+  }
   return launched();
 }
 
