@@ -1,0 +1,225 @@
+"""Asynchronous decoding over the 8-bit paged cache: its operators together, as a model's forward pass calls them.
+
+A Session owns the device buffers of a batch of requests and, on the host, which thread of a request sees which.  Rows carry the
+tag of the thread that wrote them; a thread is the set of tags that it sees.  A fork gives both the child and the parent a new tag: the child goes on from
+what its parent saw then, and does not see what the parent writes later.  A join adds a thread's set to another's.  When a request's last but one thread
+has joined, everything written so far becomes a prefix that all of its rows see, and its tags are free again.
+
+A step is begin() with the threads that write a row, then layer() for every layer; nothing in it depends on values on the device, so a step of the same
+threads can be captured into a graph and replayed, each replay one token further (run this file for an example).
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass, field
+
+import torch
+
+from . import kv8
+
+TAGS = 64
+
+
+@dataclass
+class Thread:
+    request: int
+    tag: int
+    sees: int  # set of tags
+    position: int = 0  # of its next row
+    alive: bool = True
+
+
+@dataclass
+class _Request:
+    threads: list = field(default_factory=list)
+    used: int = 0  # set of tags
+    rows: int = 0
+    prefix: int = 0
+
+
+class Session:
+    def __init__(self, *, codes="e4m3", dtype="bf16", n_q_heads, n_kv_heads, head_dim, softmax_scale, n_layers=1, max_requests=1, max_rows=256,
+                 page_tokens=16, n_phys_pages, pages_per_request, slopes=None, logit_cap=0.0, device="cuda:0"):
+        self.device = torch.device(device)
+        self.cfg = cfg = kv8.make_config(codes, dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale, n_layers=n_layers, max_requests=max_requests,
+                                         max_rows=max_rows, page_tokens=page_tokens, n_phys_pages=n_phys_pages, pages_per_request=pages_per_request)
+        i32 = dict(dtype=torch.int32, device=self.device)
+        k_shape, v_shape, s_shape = kv8.cache_shapes(cfg)
+        # uninitialised on purpose: what has not been written is never read
+        self.k_codes = torch.empty(k_shape, dtype=torch.uint8, device=self.device)
+        self.v_codes = torch.empty(v_shape, dtype=torch.uint8, device=self.device)
+        self.k_scale, self.v_scale = torch.empty(s_shape, device=self.device), torch.empty(s_shape, device=self.device)
+        self.page_table = torch.full((max_requests, pages_per_request), -1, **i32)
+        self.free_pages = torch.arange(n_phys_pages - 1, -1, -1, **i32)
+        self.free_count = torch.full((1,), n_phys_pages, **i32)
+        self.length = torch.zeros(max_requests, **i32)
+        self.prefix_len = torch.zeros(max_requests, **i32)
+        slots = n_phys_pages * page_tokens
+        self.slot_tag, self.slot_position = torch.zeros(slots, dtype=torch.uint8, device=self.device), torch.zeros(slots, **i32)
+        self.slot = torch.full((max_rows,), -1, **i32)
+        self.workspace = torch.empty(kv8.query_workspace_bytes(cfg), dtype=torch.uint8, device=self.device)
+        self.slopes = None if slopes is None else torch.as_tensor(slopes, dtype=torch.float32, device=self.device)
+        self.logit_cap = logit_cap
+        self.requests = [_Request() for _ in range(max_requests)]
+        self.handle = self._step = None
+        self.bind(torch.cuda.current_stream(self.device))
+
+    def bind(self, stream):
+        """Work of later calls goes to this stream; the caller orders it behind what was enqueued before."""
+        self.handle = kv8.PastaKv8(self.cfg, self.workspace, page_table=self.page_table, k_codes=self.k_codes, v_codes=self.v_codes,
+                                   k_scale=self.k_scale, v_scale=self.v_scale, free_pages=self.free_pages, slot_tag=self.slot_tag,
+                                   slot_position=self.slot_position, stream=stream.cuda_stream)
+        self._step = None
+
+    # ---- threads (host) ------------------------------------------------------------------------
+    def _new_tag(self, request):
+        r = self.requests[request]
+        for tag in range(TAGS):
+            if not (r.used >> tag) & 1:
+                r.used |= 1 << tag
+                return tag
+        raise RuntimeError(f"request {request}: {TAGS} tags are in use; join its threads first")
+
+    def open(self, request) -> Thread:
+        """The main thread of an empty request."""
+        r = self.requests[request]
+        if r.threads:
+            raise ValueError(f"request {request} is open")
+        tag = self._new_tag(request)
+        t = Thread(request, tag, 1 << tag)
+        r.threads.append(t)
+        return t
+
+    def fork(self, parent: Thread, position=None) -> Thread:
+        """A child that sees what `parent` sees now.  `position`: id of its first row (estimated ids may leave gaps); else it counts on."""
+        r = self.requests[parent.request]
+        free = TAGS - bin(r.used).count("1")
+        if free < 2:
+            raise RuntimeError(f"request {parent.request}: {TAGS} tags are in use; join its threads first")
+        tag, own = self._new_tag(parent.request), self._new_tag(parent.request)
+        child = Thread(parent.request, tag, parent.sees | 1 << tag, parent.position if position is None else position)
+        parent.tag, parent.sees = own, parent.sees | 1 << own
+        r.threads.append(child)
+        return child
+
+    def join(self, thread: Thread, others):
+        """`thread` sees from now on what `others` saw; they end.  Their rows stay where they are."""
+        r = self.requests[thread.request]
+        for o in others:
+            if o is thread or not o.alive or o.request != thread.request:
+                raise ValueError("joins living threads of one request")
+        for o in others:
+            thread.sees |= o.sees
+            o.alive = False
+            r.threads.remove(o)
+        if len(r.threads) == 1:
+            # everything written is seen: a prefix, and the tags are free again
+            r.prefix, r.used = r.rows, 1
+            thread.tag, thread.sees = 0, 1
+            self.prefix_len[thread.request] = r.rows
+
+    def release(self, request):
+        """Ends the request's threads; its pages go back with the next step."""
+        r = self.requests[request]
+        for t in r.threads:
+            t.alive = False
+        self.requests[request] = _Request()
+        self.prefix_len[request] = 0
+
+    # ---- a step --------------------------------------------------------------------------------
+    def begin(self, rows, positions=None):
+        """Places of a step's rows: `rows` names the thread of each, requests ascending (a thread may write several).  `positions`: their ids."""
+        n = len(rows)
+        where = [t.request for t in rows]
+        if where != sorted(where) or not all(t.alive for t in rows):
+            raise ValueError("rows of living threads, requests ascending")
+        count = [0] * len(self.requests)
+        ids = []
+        for i, t in enumerate(rows):
+            count[t.request] += 1
+            ids.append(t.position if positions is None else int(positions[i]))
+            t.position = ids[-1] + 1
+        for r, k in zip(self.requests, count):
+            r.rows += k
+        offsets = [0]
+        for k in count:
+            offsets.append(offsets[-1] + k)
+        dev = lambda x, t: torch.tensor(x, dtype=t).to(self.device)  # noqa: E731
+        signed = [t.sees - (1 << 64) if t.sees >> 63 else t.sees for t in rows]
+        keep = dev([r.rows - k for r, k in zip(self.requests, count)], torch.int32)
+        self._step = dict(n=n, most=max(count), offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8),
+                          see=dev(signed, torch.int64), position=dev(ids, torch.int32), keep=keep)
+        self.handle.slots(self.length, self._step["offsets"], n, self.slot, self.length, self.free_count, self.free_count, keep=keep,
+                          row_tag=self._step["tag"], row_position=self._step["position"])
+        self._plan()
+
+    def again(self):
+        """The same threads, one row further: what a replayed graph does.  (On the host their counts go on too.)"""
+        s = self._step
+        self.handle.slots(self.length, s["offsets"], s["n"], self.slot, self.length, self.free_count, self.free_count, row_tag=s["tag"],
+                          row_position=s["position"])
+        self._plan()
+        s["position"].add_(1)
+
+    def advanced(self, rows, steps):
+        """Tells the host that `steps` replays of again() with these threads have been enqueued."""
+        for t in rows:
+            t.position += steps
+            self.requests[t.request].rows += steps
+
+    def _plan(self):
+        s = self._step
+        self.handle.plan(self.length, s["offsets"], s["n"], max_request_rows=s["most"], prefix_len=self.prefix_len, slot=self.slot)
+
+    def layer(self, layer, k_new, v_new, q, out, lse=None):
+        """Appends the step's rows of a layer, then attends: row i sees its own row too."""
+        s = self._step
+        self.handle.append(layer, self.slot, k_new, v_new, n_rows=s["n"])
+        self.handle.attend(layer, q, out, lse=lse, logit_cap=self.logit_cap, slopes=self.slopes, row_see=s["see"],
+                           row_position=s["position"] if self.slopes is not None else None)
+
+
+def main():
+    """A prompt, three threads, and thirty-two of their steps as replays of one captured step; then the join."""
+    torch.manual_seed(0)
+    layers, hq, hkv, d, n = 4, 32, 8, 128, 3
+    s = Session(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, softmax_scale=d ** -0.5, n_layers=layers, max_rows=512, n_phys_pages=256, pages_per_request=128)
+    randn = lambda *shape: torch.randn(*shape, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+
+    def forward(rows):
+        q, k, v = randn(layers, rows, hq, d), randn(layers, rows, hkv, d), randn(layers, rows, hkv, d)
+        out = torch.empty_like(q)
+        for l in range(layers):
+            s.layer(l, k[l], v[l], q[l], out[l])
+        return out, (q, k, v)
+
+    root = s.open(0)
+    s.begin([root] * 300)
+    forward(300)
+    threads = [s.fork(root) for _ in range(n)]
+    s.begin(threads)
+    s._step["position"].add_(1)
+    forward(n)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    step = s._step
+    with torch.cuda.stream(stream):
+        s.bind(stream)
+        s._step = step
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            s.again()
+            out, _keep = forward(n)
+        for _ in range(32):
+            graph.replay()
+    stream.synchronize()
+    s.advanced(threads, 32)
+    s.bind(torch.cuda.current_stream())
+    s.join(root, threads)
+    s.begin([root])
+    out, _keep = forward(1)
+    torch.cuda.synchronize()
+    print("tokens", int(s.length[0]), "pages left", int(s.free_count), "output", float(out.float().norm()))
+
+
+if __name__ == "__main__":
+    main()

@@ -164,3 +164,31 @@ def test_the_reference_codes_are_torchs():
     x = np.random.default_rng(0).standard_normal(5000) * 100
     x = np.clip(x, -448, 448).astype(np.float32)
     assert np.array_equal(ref.nearest(x.astype(np.float64), "e4m3"), torch.from_numpy(x).to(torch.float8_e4m3fn).double().numpy())
+
+
+READELF = "/opt/rocm/llvm/bin/llvm-readelf"
+
+
+@pytest.mark.skipif(not os.path.exists(READELF), reason="needs llvm-readelf")
+def test_no_kernel_spills(tmp_path):
+    """What the compiler gave the kernels: no scratch memory, no spilled vector registers, two work-groups of the attention per CU."""
+    import struct
+
+    import yaml
+
+    lib = open(kv8.library_path(), "rb").read()
+    at = lib.index(b"__CLANG_OFFLOAD_BUNDLE__")
+    n, pos = struct.unpack_from("<Q", lib, at + 24)[0], at + 32
+    for _ in range(n):  # offset, size, length of the target's name, name
+        off, size, length = struct.unpack_from("<QQQ", lib, pos)
+        if b"gfx950" in lib[pos + 24:pos + 24 + length]:
+            (tmp_path / "code.o").write_bytes(lib[at + off:at + off + size])
+        pos += 24 + length
+    notes = subprocess.run([READELF, "--notes", str(tmp_path / "code.o")], capture_output=True, text=True, check=True).stdout
+    kernels = yaml.safe_load(notes[notes.index("---"):notes.index("\n...")])["amdhsa.kernels"]
+    attend = [k for k in kernels if "k8_attend" in k[".name"]]
+    assert len(attend) == 16
+    for k in kernels:
+        assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0, k[".name"]
+    for k in attend:
+        assert k[".vgpr_count"] <= 256 and 2 * k[".group_segment_fixed_size"] <= 160 * 1024, k[".name"]
