@@ -240,6 +240,9 @@ __device__ inline Marks load_marks(const AttendArgs& a, const Blocks& b, int k) 
   return Marks{(int)a.slot_tag[at], a.slot_position[at]};
 }
 
+// What a call does to scores, which is known ahead of the launch: nothing but hide by order and prefix, cap or lower them by places too, or anything.
+enum { kPlain = 0, kShaped = 1, kMarked = 2 };
+
 // What the tokens of a pair are to the wave's rows: how far, and who sees them.
 struct Unmarked {
   template <class F>
@@ -301,14 +304,15 @@ struct MarkedThere {
 
 // Scores of a pair, tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
 // left so where nothing has to be done; else they come out in log2 units and f is 1.
-template <bool MARKS, class Source>
+template <int KIND, class Source>
 __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, const Pair& p, const Source& source, float slope, int token,
                                      int first_token, float& f, float16v& s) {
   const int half = (threadIdx.x >> 5) & 1, base = t0 + 16 * half;
   const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || p.absent;
-  const bool masked = cut || (t0 + 32 > prefix && ((MARKS && a.tagged) || ordered));
-  if (!(a.cap_log2 > 0.f) && !a.lowered && !masked) return;
-  if (a.cap_log2 > 0.f) {
+  const bool masked = cut || (t0 + 32 > prefix && ((KIND == kMarked && a.tagged) || ordered));
+  const bool shaped = KIND != kPlain && (a.cap_log2 > 0.f || a.lowered);
+  if (KIND == kPlain ? __builtin_expect(!masked, 1) : !masked && !shaped) return;
+  if (KIND != kPlain && a.cap_log2 > 0.f) {
     // cap * tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap))
     const float g = f * a.cap_in;
 #pragma unroll
@@ -318,8 +322,8 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     for (int i = 0; i < 16; ++i) s[i] *= f;
   }
   f = 1.f;
-  if (a.lowered) {
-    if (MARKS && a.placed) {
+  if (KIND != kPlain && a.lowered) {
+    if (KIND == kMarked && a.placed) {
       source.distances([&](int i, float far) { s[i] = fmaf(-slope, fabsf(far), s[i]); });
     } else {
       const float far = (float)(token - base);
@@ -328,7 +332,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     }
   }
   if (!masked) return;
-  if (MARKS && a.tagged && t0 >= prefix && !ordered && !cut) {  // tags alone
+  if (KIND == kMarked && a.tagged && t0 >= prefix && !ordered && !cut) {  // tags alone
     bool sees;
     if (source.alike(sees)) {
       if (!sees)
@@ -341,7 +345,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
   }
   auto below = [](int n) { return n <= 0 ? 0u : n >= kBlock ? 0xffffu : (1u << n) - 1u; };
   uint32_t bits = below(token + 1 - base);
-  if (MARKS && a.tagged) {
+  if (KIND == kMarked && a.tagged) {
     uint32_t tagged = 0;
     source.sights([&](int i, bool seen) { tagged |= seen ? 1u << i : 0u; });
     bits &= tagged;
@@ -393,7 +397,7 @@ __device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (
     rare |= p[n].nan | p[n].far;
   }
   m = fmaxf(m, other_half(m));
-  if (__any(m > z.m + kSlack)) {
+  if (__builtin_expect(__any(m > z.m + kSlack), 0)) {
     m = fmaxf(m, z.m);
     const float alpha = __builtin_amdgcn_exp2f(z.m - m);
     z.m = m;
@@ -468,7 +472,7 @@ __device__ inline float lse_of(float m, float l) { return l == 0.f ? -INFINITY :
 __device__ inline float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // One step of a wave: N pairs whose codes are in k and v.  `ahead` is called when k may be overwritten, `behind` when v may.
-template <int CODES, int D, bool MARKS, int N, class Ahead, class Behind>
+template <int CODES, int D, int KIND, int N, class Ahead, class Behind>
 __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r, const half8* q, State<D>& z, uint4v (&k)[2][D / 32], uint4v (&v)[2][D / 32],
                             const Pair (&p)[N], const Marks (&marks)[2], const int (&t0)[2], Ahead ahead, Behind behind) {
   float16v s[N];
@@ -493,10 +497,10 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     f[n] = r.c * p[n].ks;
-    if constexpr (MARKS)
-      finish_scores<true>(a, u.prefix, u.hi, t0[n], p[n], MarkedHere{m[n], r.position, r.see}, r.slope, r.token, u.pos0, f[n], s[n]);
+    if constexpr (KIND == kMarked)
+      finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], MarkedHere{m[n], r.position, r.see}, r.slope, r.token, u.pos0, f[n], s[n]);
     else
-      finish_scores<false>(a, u.prefix, u.hi, t0[n], p[n], Unmarked{}, r.slope, r.token, u.pos0, f[n], s[n]);
+      finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], Unmarked{}, r.slope, r.token, u.pos0, f[n], s[n]);
   }
   half8 w[N][2];
   soften<D, N>(z, s, f, p, w, [] {});
@@ -513,9 +517,10 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
   behind();
 }
 
-template <int CODES, int D, bool MARKS>
+template <int CODES, int D, int KIND>
 __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
+  constexpr bool MARKS = KIND == kMarked;
   const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's: wave, wave + 4, ... of the unit's
   Rows<D> r;
   State<D> z;
@@ -561,7 +566,7 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
   for (; i + 1 < n_pairs; i += 2) {
     const Pair p[2] = {pair_of(b, i & 31), pair_of(b, (i + 1) & 31)};
     const int t0[2] = {token(i), token(i + 1)};
-    step<CODES, D, MARKS, 2>(a, u, r, q, z, k, v, p, marks, t0,
+    step<CODES, D, KIND, 2>(a, u, r, q, z, k, v, p, marks, t0,
       [&] {
         if (i + 2 >= n_pairs) return;
         if (((i + 2) & 31) == 0) find(i + 2), load_scales(a, b), finish_scales(b, z.most);
@@ -575,7 +580,7 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
   if (i < n_pairs) {
     const Pair p[1] = {pair_of(b, i & 31)};
     const int t0[2] = {token(i), 0};
-    step<CODES, D, MARKS, 1>(a, u, r, q, z, k, v, p, marks, t0, [] {}, [] {});
+    step<CODES, D, KIND, 1>(a, u, r, q, z, k, v, p, marks, t0, [] {}, [] {});
   }
   // the four waves meet
   float* s_o = lds;                                       // [4][32][kPitch]
@@ -631,8 +636,9 @@ struct ManyMarks {
 // time; pairs, not twice as many tokens, because two sets of scores, O and Q are what the registers hold.  One barrier for two pairs, 2j and 2j + 1:
 // in between the rings hold K up to 2j + 2 and V up to 2j + 1, and K of 2j + 3, 2j + 4 and V of 2j + 2, 2j + 3 are put where older ones were.
 // A wave brings one block of every second pair, 1 KB of neighbouring codes at a time.
-template <int CODES, int D, bool MARKS>
+template <int CODES, int D, int KIND>
 __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int listed, int head, uint8_t* lds) {
+  constexpr bool MARKS = KIND == kMarked;
   constexpr int kPieces = D / 64;  // 1 KB pieces of a block's K, and of its V
   constexpr int kEarly = D / 32;   // operands of K that are read ahead of the maximum
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
@@ -749,9 +755,9 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int liste
     f[0] = r.c * p[0].ks;
     if constexpr (MARKS) {
       const MarkedThere source{there.position[i & 3] + half * 16, (float)(r.position - origin), there.rows[i & 3][half * 16 + (lane & 15)][wave]};
-      finish_scores<true>(a, u.prefix, u.hi, u.lo + i * 32, p[0], source, r.slope, r.token, first_token, f[0], of);
+      finish_scores<KIND>(a, u.prefix, u.hi, u.lo + i * 32, p[0], source, r.slope, r.token, first_token, f[0], of);
     } else {
-      finish_scores<false>(a, u.prefix, u.hi, u.lo + i * 32, p[0], Unmarked{}, r.slope, r.token, first_token, f[0], of);
+      finish_scores<KIND>(a, u.prefix, u.hi, u.lo + i * 32, p[0], Unmarked{}, r.slope, r.token, first_token, f[0], of);
     }
   };
   auto add_values = [&](int i) {
@@ -824,7 +830,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int liste
   }
 }
 
-template <int CODES, int D, bool MANY, bool MARKS>
+template <int CODES, int D, bool MANY, int KIND>
 __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   constexpr int kFewBytes = 4 * kRows * (D + 4) * 4 + 4 * kRows * 8;
   constexpr int kManyBytes = 8 * kPairBytes<D> + sizeof(ManyMarks);
@@ -837,9 +843,9 @@ __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   asm volatile("" ::"s"(u.request), "s"(u.s0), "s"(u.pos0), "s"(u.lo), "s"(u.hi), "s"(u.prefix), "s"(u.part));  // (one load, ahead of the branch)
   if (u.n_rows == 0) return;
   if (MANY && u.n_rows > kRows)
-    attend_many<CODES, D, MARKS>(a, u, listed, head, lds);
+    attend_many<CODES, D, KIND>(a, u, listed, head, lds);
   else
-    attend_few<CODES, D, MARKS>(a, u, dealt, head, (float*)lds);
+    attend_few<CODES, D, KIND>(a, u, dealt, head, (float*)lds);
 }
 
 // Joins the partial rows of the tiles whose tokens are split.  D / 4 lanes hold a row, four dims apiece; the 1024 / D such groups of a

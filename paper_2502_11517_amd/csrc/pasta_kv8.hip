@@ -259,11 +259,14 @@ namespace {
 
 template <int CODES, int D>
 void launch_attend(const k8::AttendArgs& k, bool many, int64_t groups, hipStream_t s) {
-  const bool marks = k.tagged || k.placed;
-  if (many)
-    marks ? k8::k8_attend<CODES, D, true, true><<<(unsigned)groups, 256, 0, s>>>(k) : k8::k8_attend<CODES, D, true, false><<<(unsigned)groups, 256, 0, s>>>(k);
-  else
-    marks ? k8::k8_attend<CODES, D, false, true><<<(unsigned)groups, 256, 0, s>>>(k) : k8::k8_attend<CODES, D, false, false><<<(unsigned)groups, 256, 0, s>>>(k);
+  const int kind = k.tagged || k.placed ? k8::kMarked : k.lowered || k.cap_log2 > 0.f ? k8::kShaped : k8::kPlain;
+  auto launch = [&](auto of, auto kind) { k8::k8_attend<CODES, D, of.value, kind.value><<<(unsigned)groups, 256, 0, s>>>(k); };
+  auto with = [&](auto of) {
+    if (kind == k8::kMarked) launch(of, std::integral_constant<int, k8::kMarked>{});
+    else if (kind == k8::kShaped) launch(of, std::integral_constant<int, k8::kShaped>{});
+    else launch(of, std::integral_constant<int, k8::kPlain>{});
+  };
+  many ? with(std::true_type{}) : with(std::false_type{});
 }
 
 }  // namespace

@@ -187,7 +187,7 @@ def test_no_kernel_spills(tmp_path):
     notes = subprocess.run([READELF, "--notes", str(tmp_path / "code.o")], capture_output=True, text=True, check=True).stdout
     kernels = yaml.safe_load(notes[notes.index("---"):notes.index("\n...")])["amdhsa.kernels"]
     attend = [k for k in kernels if "k8_attend" in k[".name"]]
-    assert len(attend) == 16
+    assert len(attend) == 24
     for k in kernels:
         assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0, k[".name"]
     for k in attend:
