@@ -273,35 +273,6 @@ struct MarkedHere {
   }
 };
 
-// attend_many: from LDS, where positions lie as distances from one row of the work-group, and tags as the rows that see them: bit n of a token's
-// word is row n of the wave.  A lane holds the word of token l & 15 of block l >> 5, so that two words are the lanes that see token i.
-struct MarkedThere {
-  const float* position;
-  float own;
-  uint32_t rows;
-  template <class F>
-  __device__ void distances(F f) const {
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const float4v x = *(const float4v*)(position + i);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) f(i + k, own - x[k]);
-    }
-  }
-  template <class F>
-  __device__ void sights(F f) const {
-    each<16>([&](auto i) {
-      const uint64_t lanes = (uint64_t)__builtin_amdgcn_readlane(rows, 32 + i.value) << 32 | (uint32_t)__builtin_amdgcn_readlane(rows, i.value);
-      f(i.value, __builtin_amdgcn_inverse_ballot_w64(lanes));
-    });
-  }
-  __device__ bool alike(bool& sees) const {
-    const int first = of_row<0>(rows);
-    sees = (first >> (threadIdx.x & 31)) & 1;
-    return __all((int)rows == first);
-  }
-};
-
 // Scores of a pair, tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
 // left so where nothing has to be done; else they come out in log2 units and f is 1.
 template <int KIND, class Source>
@@ -473,7 +444,7 @@ __device__ inline float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // One step of a wave: N pairs whose codes are in k and v.  `ahead` is called when k may be overwritten, `behind` when v may.
 template <int CODES, int D, int KIND, int N, class Ahead, class Behind>
-__device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r, const half8* q, State<D>& z, uint4v (&k)[2][D / 32], uint4v (&v)[2][D / 32],
+__device__ inline void step(const AttendArgs& a, const Unit& u, int first_token, const Rows<D>& r, const half8* q, State<D>& z, uint4v (&k)[2][D / 32], uint4v (&v)[2][D / 32],
                             const Pair (&p)[N], const Marks (&marks)[2], const int (&t0)[2], Ahead ahead, Behind behind) {
   float16v s[N];
 #pragma unroll
@@ -498,9 +469,9 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
   for (int n = 0; n < N; ++n) {
     f[n] = r.c * p[n].ks;
     if constexpr (KIND == kMarked)
-      finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], MarkedHere{m[n], r.position, r.see}, r.slope, r.token, u.pos0, f[n], s[n]);
+      finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], MarkedHere{m[n], r.position, r.see}, r.slope, r.token, first_token, f[n], s[n]);
     else
-      finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], Unmarked{}, r.slope, r.token, u.pos0, f[n], s[n]);
+      finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], Unmarked{}, r.slope, r.token, first_token, f[n], s[n]);
   }
   half8 w[N][2];
   soften<D, N>(z, s, f, p, w, [] {});
@@ -517,18 +488,18 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D>& r
   behind();
 }
 
+// A wave's rows over the pairs first, first + stride, ... of the unit.  Q's operands lie in LDS, a copy for each wave: in registers they would not leave
+// room for two pairs at a time.
 template <int CODES, int D, int KIND>
-__device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
+__device__ inline void attend_rows(const AttendArgs& a, const Unit& u, int hi, int listed, int head, int row0, int first, int stride, half8* q, Rows<D>& r,
+                                   State<D>& z) {
   constexpr bool MARKS = KIND == kMarked;
-  const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's: wave, wave + 4, ... of the unit's
-  Rows<D> r;
-  State<D> z;
-  start(z);
+  const int lane = threadIdx.x & 63;
+  const int n_pairs = max(((hi - u.lo + 31) >> 5) - first + stride - 1, 0) / stride;
   Blocks b;
-  uint4v k[2][D / 32], v[2][D / 32];
+  uint4v k[2][D / 32], v[2][D / 32], raw[D / 16];
   Marks marks[2] = {};
-  auto token = [&](int i) { return u.lo + (wave + 4 * i) * 32; };  // first of the wave's i-th pair
+  auto token = [&](int i) { return u.lo + (first + stride * i) * 32; };  // first of the wave's i-th pair
   auto find = [&](int i) { find_blocks(a, u.request, head, token(i + (lane >> 1)) + (lane & 1) * 16, u.hi, b); };
   auto load_k = [&](int i, int to) {
     const int x = 2 * (i & 31);
@@ -538,15 +509,12 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
     const int x = 2 * (i & 31);
     load_pieces(v_piece(a, __builtin_amdgcn_readlane(b.at, x), __builtin_amdgcn_readlane(b.at, x + 1), D), v[to]);
   };
-  // Q's operands lie in LDS, a copy for each wave where its output goes later: in registers they would not leave room for two pairs
-  constexpr int kPitch = D + 4;
-  half8* q = (half8*)(lds + wave * kRows * kPitch);
-  uint4v raw[D / 16];
-  request_rows<D, MARKS>(a, u, head, 0, r, raw);
+  start(z);
+  request_rows<D, MARKS>(a, u, head, row0, r, raw);
   __builtin_amdgcn_sched_barrier(0);
   // (everything is asked for before anything is waited for: loads come back in their order)
-  if (u.hi - u.lo <= kUnitBlocks * kBlock)
-    on_block(a, 2 * (wave + 4 * (lane >> 1)) + (lane & 1) < kUnitBlocks ? listed : -1, head, b);
+  if (stride == 1 || u.hi - u.lo <= kUnitBlocks * kBlock)
+    on_block(a, token(lane >> 1) + (lane & 1) * 16 < u.hi ? listed : -1, head, b);
   else
     find(0);
   // (where the wave has fewer than two pairs, block 0 is read in their place)
@@ -562,11 +530,12 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
     for (int y = 0; y < D / 16; ++y) q[y * 64 + lane] = x[y];
   }
   finish_scales(b, z.most);
+  const int first_token = u.pos0 + (row0 >> a.g_shift);
   int i = 0;
   for (; i + 1 < n_pairs; i += 2) {
     const Pair p[2] = {pair_of(b, i & 31), pair_of(b, (i + 1) & 31)};
     const int t0[2] = {token(i), token(i + 1)};
-    step<CODES, D, KIND, 2>(a, u, r, q, z, k, v, p, marks, t0,
+    step<CODES, D, KIND, 2>(a, u, first_token, r, q, z, k, v, p, marks, t0,
       [&] {
         if (i + 2 >= n_pairs) return;
         if (((i + 2) & 31) == 0) find(i + 2), load_scales(a, b), finish_scales(b, z.most);
@@ -580,8 +549,21 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
   if (i < n_pairs) {
     const Pair p[1] = {pair_of(b, i & 31)};
     const int t0[2] = {token(i), 0};
-    step<CODES, D, KIND, 1>(a, u, r, q, z, k, v, p, marks, t0, [] {}, [] {});
+    step<CODES, D, KIND, 1>(a, u, first_token, r, q, z, k, v, p, marks, t0, [] {}, [] {});
   }
+}
+
+constexpr int kQBytes(int D) { return kRows * D * 2; }  // of a wave's Q
+
+// Every wave takes a quarter of the unit's tokens; the four meet at the end.
+template <int CODES, int D, int KIND>
+__device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
+  constexpr int kPitch = D + 4;
+  Rows<D> r;
+  State<D> z;
+  // (Q lies where the wave's output goes later)
+  attend_rows<CODES, D, KIND>(a, u, u.hi, listed, head, 0, wave, 4, (half8*)(lds + wave * kRows * kPitch), r, z);
   // the four waves meet
   float* s_o = lds;                                       // [4][32][kPitch]
   float2v* s_ml = (float2v*)(lds + 4 * kRows * kPitch);   // [4][32]
@@ -622,190 +604,17 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
   }
 }
 
-// LDS of the shared tokens: rings of four pairs of blocks (32 tokens) for K and for V, as the products' operands (a lane's 16 bytes next to its
-// neighbour's); a ring for the tokens' positions (less the first row's) and for the rows that see them, a word per wave; and, per tag, those rows.
-template <int D>
-constexpr int kPairBytes = 32 * D * 2;  // K or V
-struct ManyMarks {
-  float position[4][32];
-  uint4v rows[4][32];
-  uint4v tag_rows[64];
-};
-
-// The scores of pair i + 1 are taken between the exponentials of pair i, so that within a wave the matrix pipe and the vector pipe work at the same
-// time; pairs, not twice as many tokens, because two sets of scores, O and Q are what the registers hold.  One barrier for two pairs, 2j and 2j + 1:
-// in between the rings hold K up to 2j + 2 and V up to 2j + 1, and K of 2j + 3, 2j + 4 and V of 2j + 2, 2j + 3 are put where older ones were.
-// A wave brings one block of every second pair, 1 KB of neighbouring codes at a time.
+// Every wave takes 32 rows of its own over all of the unit's tokens.  The four read the same codes at about the same time, and all but the first
+// find them in the CU's cache; turning them into fp16 four times over costs less than bringing them there once, through LDS, with a barrier for every
+// 64 tokens (long_nested of the table: 70.5 us a layer so, 
 template <int CODES, int D, int KIND>
 __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int listed, int head, uint8_t* lds) {
-  constexpr bool MARKS = KIND == kMarked;
-  constexpr int kPieces = D / 64;  // 1 KB pieces of a block's K, and of its V
-  constexpr int kEarly = D / 32;   // operands of K that are read ahead of the maximum
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
-  const int n_pairs = (u.hi - u.lo + 31) >> 5;
-  const int odd = wave >> 1, side = wave & 1;  // this wave's share: block `side` of every second pair
-  ManyMarks& there = *(ManyMarks*)(lds + 8 * kPairBytes<D>);
+  if (wave * kRows >= u.n_rows) return;
+  const int last_token = u.pos0 + ((min(wave * kRows + kRows, u.n_rows) - 1) >> a.g_shift);
   Rows<D> r;
   State<D> z;
-  start(z);
-  const bool works = wave * kRows < u.n_rows;
-  const int first_token = u.pos0 + (wave * kRows >> a.g_shift);
-  Blocks b, ahead;  // of the pair under computation, and of those asked for: 32 pairs, from a multiple of 32 on
-  int group = 0;
-  uint4v k[kPieces], v[kPieces];
-  bool v_absent = false;
-  int tag = 0, position = 0;
-  const int origin = MARKS ? a.row_position[u.s0 >> a.g_shift] : 0;
-  auto find = [&](int i, Blocks& to) { find_blocks(a, u.request, head, u.lo + (i & ~31) * 32 + lane * 16, u.hi, to); };
-  // V of pair i and K of the one behind it: a piece of K is 4 runs of 16 dims x 16 tokens, one of V 64 dims x 16 tokens
-  auto block = [&](int i) {
-    if (i >> 5 != group) group = i >> 5, find(i, ahead);
-    return 2 * (i & 31) + side;
-  };
-  auto request_k = [&](int i) {
-    const int x = block(i), at = __builtin_amdgcn_readlane(ahead.at, x);
-    const uint8_t* from = a.k + (int64_t)max(at, 0) * (kBlock * D);
-#pragma unroll
-    for (int y = 0; y < kPieces; ++y) k[y] = *(const uint4v*)(from + y * 1024 + lane * 16);
-    if constexpr (MARKS) {
-      const int64_t slot = (int64_t)__builtin_amdgcn_readlane(ahead.slot16, x) * kBlock + (lane & 15);
-      tag = a.slot_tag[slot], position = a.slot_position[slot];
-    }
-  };
-  auto request_v = [&](int i) {
-    const int at = __builtin_amdgcn_readlane(ahead.at, block(i));
-    const uint8_t* from = a.v + (int64_t)max(at, 0) * (kBlock * D);
-#pragma unroll
-    for (int y = 0; y < kPieces; ++y) v[y] = *(const uint4v*)(from + y * 1024 + lane * 16);
-    v_absent = at < 0;
-  };
-  // K: run c = lane / 16 of a piece, token t = lane % 16, is lane m + 32 (c & 1) of operands 2 (c / 2) and the next, m = 8 (t / 4) + 4 side + t % 4
-  const int k_place = (lane >> 5) * 128 + ((lane >> 2) & 3) * 8 + side * 4 + (lane & 3) + ((lane >> 4) & 1) * 32;
-  const int v_place = (lane >> 5) * 128 + side * 32 + (lane & 31);
-  auto publish_k = [&](int i) {
-    half8* to = (half8*)(lds + (i & 3) * kPairBytes<D>) + k_place;
-#pragma unroll
-    for (int y = 0; y < kPieces; ++y) {
-      to[y * 256] = codes_to_half8<CODES>(k[y][0], k[y][1]);
-      to[y * 256 + 64] = codes_to_half8<CODES>(k[y][2], k[y][3]);
-    }
-    if (MARKS && lane < 16) {
-      if (a.placed) there.position[i & 3][side * 16 + lane] = (float)(position - origin);
-      if (a.tagged) there.rows[i & 3][side * 16 + lane] = there.tag_rows[tag & 63];
-    }
-  };
-  auto publish_v = [&](int i) {
-    half8* to = (half8*)(lds + (4 + (i & 3)) * kPairBytes<D>) + v_place;
-#pragma unroll
-    for (int y = 0; y < kPieces; ++y) {
-      uint4v c;  // what is not there must not be NaN: its weight is 0
-#pragma unroll
-      for (int x = 0; x < 4; ++x) c[x] = v_absent ? 0u : v[y][x];
-      to[y * 256] = codes_to_half8<CODES>(c[0], c[1]);
-      to[y * 256 + 64] = codes_to_half8<CODES>(c[2], c[3]);
-    }
-  };
-  half8 q[D / 16];
-  {
-    uint4v raw[D / 16];
-    request_rows<D, MARKS>(a, u, head, wave * kRows, r, raw);
-    __builtin_amdgcn_sched_barrier(0);
-    on_block(a, u.lo + lane * 16 < u.hi ? listed : -1, head, b);
-    ahead = b;
-    load_scales(a, b);
-    request_k(odd);
-    request_v(odd);
-    __builtin_amdgcn_sched_barrier(0);
-    finish_rows<D>(a, r, raw, q);
-  }
-  if (MARKS && a.tagged && u.hi > u.prefix) {
-    uint32_t rows = 0;  // lane t: the wave's rows that see tag t
-    for (int t = 0; t < 64; ++t) {
-      const uint32_t now = (uint32_t)__ballot((r.see >> t) & 1);
-      rows = lane == t ? now : rows;
-    }
-    ((uint32_t*)there.tag_rows)[lane * 4 + wave] = rows;
-    __syncthreads();
-  }
-  finish_scales(b, z.most);
-  publish_k(odd);
-  publish_v(odd);
-  if (!odd) request_k(2), publish_k(2);
-  request_v(2 + odd);
-  request_k(3 + odd);
-  __syncthreads();
-  Pair p[1];
-  float f[1];
-  float16v s[1], t[1];  // scores of even and of odd pairs
-  half8 w[1][2], early[kEarly];
-  auto k_ring = [&](int i) { return (const half8*)(lds + (i & 3) * kPairBytes<D>) + lane; };
-  auto look_ahead = [&](int i) {
-#pragma unroll
-    for (int x = 0; x < kEarly; ++x) early[x] = k_ring(i)[x * 64];
-  };
-  auto products = [&](int i, float16v& to) {
-    __builtin_amdgcn_s_setprio(1);  // (the wave that feeds the matrix pipe goes ahead of its neighbour: 3 %)
-#pragma unroll
-    for (int x = 0; x < 16; ++x) to[x] = 0.f;
-#pragma unroll
-    for (int x = 0; x < D / 16; ++x) to = __builtin_amdgcn_mfma_f32_32x32x16_f16(x < kEarly ? early[x] : k_ring(i)[x * 64], q[x], to, 0, 0, 0);
-  };
-  auto finish = [&](int i, float16v& of) {
-    p[0] = pair_of(b, i & 31);
-    f[0] = r.c * p[0].ks;
-    if constexpr (MARKS) {
-      const MarkedThere source{there.position[i & 3] + half * 16, (float)(r.position - origin), there.rows[i & 3][half * 16 + (lane & 15)][wave]};
-      finish_scores<KIND>(a, u.prefix, u.hi, u.lo + i * 32, p[0], source, r.slope, r.token, first_token, f[0], of);
-    } else {
-      finish_scores<KIND>(a, u.prefix, u.hi, u.lo + i * 32, p[0], Unmarked{}, r.slope, r.token, first_token, f[0], of);
-    }
-  };
-  auto add_values = [&](int i) {
-    const half8* from = (const half8*)(lds + (4 + (i & 3)) * kPairBytes<D>) + lane;
-#pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int x = 0; x < D / 32; ++x) z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[(2 * x + y) * 64], w[0][y], z.o[x], 0, 0, 0);
-  };
-  // (in the last round what is put into the rings, and the products of the pair behind the last, are for nobody: their blocks are absent, or older ones)
-  auto publish = [&](int i) {
-    publish_v(i + 2 + odd);
-    publish_k(i + 3 + odd);
-  };
-  if (works && n_pairs > 0) {
-    look_ahead(0);
-    products(0, s[0]);
-    finish(0, s[0]);
-  }
-  __syncthreads();  // (pair 4 goes where pair 0 is)
-  for (int i = 0; i < n_pairs; i += 2) {
-    if (works) {
-      look_ahead(i + 1);
-      soften<D, 1>(z, s, f, p, w, [&] { products(i + 1, t[0]); });
-      add_values(i);
-      __builtin_amdgcn_s_setprio(0);
-      finish(i + 1, t[0]);
-      look_ahead(i + 2);
-      soften<D, 1>(z, t, f, p, w, [&] { products(i + 2, s[0]); });
-      add_values(i + 1);
-      publish(i);
-      __builtin_amdgcn_s_setprio(0);
-    } else {
-      publish(i);
-    }
-    if (i + 2 < n_pairs) {
-      request_v(i + 4 + odd);
-      request_k(i + 5 + odd);
-      if (((i + 2) & 31) == 0) {
-        find(i + 2, b);
-        load_scales(a, b);
-        finish_scales(b, z.most);
-      }
-      if (works) finish(i + 2, s[0]);
-      __syncthreads();
-    }
-  }
-  if (!works) return;
+  attend_rows<CODES, D, KIND>(a, u, min(u.hi, max(last_token + 1, u.prefix)), listed, head, wave * kRows, 0, 1, (half8*)(lds + wave * kQBytes(D)), r, z);
   const float l = z.l + other_half(z.l);
   poison(z);
   if (!r.real) return;
@@ -833,8 +642,7 @@ __device__ inline void attend_many(const AttendArgs& a, const Unit& u, int liste
 template <int CODES, int D, bool MANY, int KIND>
 __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   constexpr int kFewBytes = 4 * kRows * (D + 4) * 4 + 4 * kRows * 8;
-  constexpr int kManyBytes = 8 * kPairBytes<D> + sizeof(ManyMarks);
-  __shared__ __attribute__((aligned(16))) uint8_t lds[MANY && kManyBytes > kFewBytes ? kManyBytes : kFewBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kFewBytes];  // (more than four waves' Q)
   const int head = blockIdx.x % a.g.Hkv, unit = blockIdx.x / a.g.Hkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Unit u = a.units[unit];
   // the lane's block, asked for together with the unit: in attend_few pairs are dealt out to the four waves
