@@ -75,7 +75,7 @@ typedef struct {
   int32_t max_rows;          /* most rows of one step, all requests together */
   int32_t page_tokens;       /* a power of two, 16 .. 4096 */
   int32_t n_phys_pages;      /* n_phys_pages * page_tokens < 2^31 */
-  int32_t pages_per_request; /* columns of page_table; * page_tokens < 2^31 */
+  int32_t pages_per_request; /* columns of page_table; * page_tokens <= 2^27 */
   float softmax_scale;       /* finite; applied to q.k */
   void *k_codes, *v_codes;   /* DEVICE, 16-byte aligned.  Any of the DEVICE pointers from here on may be */
   float *k_scale, *v_scale;  /* DEVICE                     NULL if no call is made that needs it.         */

@@ -17,8 +17,7 @@
 //     the products' operands through registers alone, in whole cache lines, with no transposition;
 //   * the scores that a lane gets (16 tokens of one block, one row) are, as fp16, its operand of the second product.
 //
-// attend_few, <= 32 stacked rows: every wave takes blocks of 32 tokens of its own, and the four meet once at the end.
-// attend_many: four waves of 32 rows each take the same tokens; the codes are turned into fp16 once per work-group, by way of LDS.
+// A work-group takes 32 or 64 stacked rows; its four waves split the tokens, each with codes of its own in registers, and meet once at the end.
 #pragma once
 #include <float.h>
 
@@ -87,6 +86,7 @@ struct Rows {
   float c;      // score factor but for ks
   float slope;  // in log2 units
   int token;    // own place
+  int first_token;  // the wave's first row's
   int position;
   uint64_t see;
   bool real;
@@ -105,6 +105,7 @@ __device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) raw[k] = p[(2 * (k >> 1) + half) * 2 + (k & 1)];
   r.token = u.pos0 + ((first + n) >> a.g_shift);
+  r.first_token = u.pos0 + (first >> a.g_shift);
   r.slope = a.slopes[head * a.g.G + (s & (a.g.G - 1))];
   if constexpr (MARKS) {
     r.see = a.row_see[s >> a.g_shift];
@@ -333,7 +334,6 @@ struct State {
   float16v o[D / 32];
   float m, l;  // the scores' base, at most kSlack below their maximum; l: of this lane's tokens
   float bad;   // NaN: the row sees a block whose V reads as NaN
-  int most;    // largest exponent of V's scales so far
 };
 
 template <int D>
@@ -342,7 +342,7 @@ __device__ inline void start(State<D>& z) {
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int k = 0; k < 16; ++k) z.o[i][k] = 0.f;
-  z.m = -FLT_MAX, z.l = 0.f, z.bad = 0.f, z.most = kEMin;
+  z.m = -FLT_MAX, z.l = 0.f, z.bad = 0.f;
 }
 
 __device__ inline void to_half(const float16v& y, half8 (&w)[2]) {
@@ -353,58 +353,71 @@ __device__ inline void to_half(const float16v& y, half8 (&w)[2]) {
   }
 }
 
-// N pairs of blocks: their scores (times f) become the second product's operands.  `between` is called where the exponentials are taken; from there
-// on there is no branch.
-template <int D, int N, class Between>
-__device__ inline void soften(State<D>& z, const float16v (&s)[N], const float (&f)[N], const Pair (&p)[N], half8 (&w)[N][2], Between between) {
-  float m = -FLT_MAX;
+// N pairs of blocks and G groups of 32 rows: their scores (times f) become the second product's operands.
+template <int D, int G, int N>
+__device__ inline void soften(State<D> (&z)[G], const float16v (&s)[G][N], const float (&f)[G][N], const Pair (&p)[N], half8 (&w)[G][N][2]) {
+  float m[G];
+  bool ahead = false;
   int rare = 0;
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    float most = s[n][0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) most = fmaxf(most, s[n][i]);
-    m = fmaxf(m, fmaf(most, f[n], p[n].ev));
-    rare |= p[n].nan | p[n].far;
-  }
-  m = fmaxf(m, other_half(m));
-  if (__builtin_expect(__any(m > z.m + kSlack), 0)) {
-    m = fmaxf(m, z.m);
-    const float alpha = __builtin_amdgcn_exp2f(z.m - m);
-    z.m = m;
-    z.l *= alpha;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-      for (int k = 0; k < 16; ++k) z.o[i][k] *= alpha;
-  }
-  float off[N];
-#pragma unroll
-  for (int n = 0; n < N; ++n) off[n] = p[n].ev - z.m;
-  if (__builtin_expect(rare, 0)) {
+  for (int g = 0; g < G; ++g) {
+    m[g] = -FLT_MAX;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      bool sees = false;
+      float most = s[g][n][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) most = fmaxf(most, s[g][n][i]);
+      m[g] = fmaxf(m[g], fmaf(most, f[g][n], p[n].ev));
+    }
+    m[g] = fmaxf(m[g], other_half(m[g]));
+    ahead |= m[g] > z[g].m + kSlack;
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) rare |= p[n].nan | p[n].far;
+  if (__builtin_expect(__any(ahead), 0)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float to = fmaxf(m[g], z[g].m), alpha = __builtin_amdgcn_exp2f(z[g].m - to);
+      z[g].m = to;
+      z[g].l *= alpha;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) z[g].o[i][k] *= alpha;
+    }
+  }
+  float off[G][N];
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int n = 0; n < N; ++n) off[g][n] = p[n].ev - z[g].m;
+  if (__builtin_expect(rare, 0)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        bool sees = false;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sees |= s[g][n][i] != -INFINITY, sum += __builtin_amdgcn_exp2f(fmaf(s[g][n][i], f[g][n], off[g][n]));
+        if (of_half(p[n].nan) && sees) z[g].bad = __builtin_nanf("");
+        if (of_half(p[n].far)) z[g].l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z[g].l), off[g][n] = -INFINITY;
+      }
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
       float sum = 0.f;
+      float16v y;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sees |= s[n][i] != -INFINITY, sum += __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off[n]));
-      if (of_half(p[n].nan) && sees) z.bad = __builtin_nanf("");
-      if (of_half(p[n].far)) z.l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z.l), off[n] = -INFINITY;
+      for (int i = 0; i < 16; ++i) {
+        y[i] = __builtin_amdgcn_exp2f(fmaf(s[g][n][i], f[g][n], off[g][n]));
+        sum += y[i];
+      }
+      z[g].l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z[g].l);
+      to_half(y, w[g][n]);
     }
-  }
-  between();
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    float sum = 0.f;
-    float16v y;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      y[i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], f[n], off[n]));
-      sum += y[i];
-    }
-    z.l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z.l);
-    to_half(y, w[n]);
-  }
 }
 
 __device__ inline void store_out(const AttendArgs& a, int64_t at, float4v x) {  // four neighbouring values of the result
@@ -442,39 +455,48 @@ __device__ inline void poison(State<D>& z) {
 __device__ inline float lse_of(float m, float l) { return l == 0.f ? -INFINITY : kLn2 * (m + __builtin_amdgcn_logf(l)); }
 __device__ inline float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
-// One step of a wave: N pairs whose codes are in k and v.  `ahead` is called when k may be overwritten, `behind` when v may.
-template <int CODES, int D, int KIND, int N, class Ahead, class Behind>
-__device__ inline void step(const AttendArgs& a, const Unit& u, int first_token, const Rows<D>& r, const half8* q, State<D>& z, uint4v (&k)[2][D / 32], uint4v (&v)[2][D / 32],
-                            const Pair (&p)[N], const Marks (&marks)[2], const int (&t0)[2], Ahead ahead, Behind behind) {
-  float16v s[N];
+// One step of a wave: N pairs whose codes are in k and v, against G groups of 32 rows.  `ahead` is called when k may be overwritten, `behind` when v may.
+template <int CODES, int D, int KIND, int G, int N, class Ahead, class Behind>
+__device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&r)[G], const half8* q, State<D> (&z)[G], uint4v (&k)[N][D / 32],
+                            uint4v (&v)[N][D / 32], const Pair (&p)[N], const Marks (&marks)[N], const int (&t0)[N], Ahead ahead, Behind behind) {
+  float16v s[G][N];
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+  for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[g][n][i] = 0.f;
 #pragma unroll
   for (int x = 0; x < D / 32; ++x)
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const half8 row = q[(2 * x + y) * 64 + (threadIdx.x & 63)];
+      half8 codes[N];
 #pragma unroll
-      for (int n = 0; n < N; ++n)
-        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half8<CODES>(k[n][x][2 * y], k[n][x][2 * y + 1]), row, s[n], 0, 0, 0);
+      for (int n = 0; n < N; ++n) codes[n] = codes_to_half8<CODES>(k[n][x][2 * y], k[n][x][2 * y + 1]);
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const half8 row = q[(g * (D / 16) + 2 * x + y) * 64 + (threadIdx.x & 63)];
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[g][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes[n], row, s[g][n], 0, 0, 0);
+      }
     }
   Marks m[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) m[n] = marks[n];
   ahead();
-  float f[N];
+  float f[G][N];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    f[n] = r.c * p[n].ks;
-    if constexpr (KIND == kMarked)
-      finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], MarkedHere{m[n], r.position, r.see}, r.slope, r.token, first_token, f[n], s[n]);
-    else
-      finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], Unmarked{}, r.slope, r.token, first_token, f[n], s[n]);
-  }
-  half8 w[N][2];
-  soften<D, N>(z, s, f, p, w, [] {});
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      f[g][n] = r[g].c * p[n].ks;
+      if constexpr (KIND == kMarked)
+        finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], MarkedHere{m[n], r[g].position, r[g].see}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
+      else
+        finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], Unmarked{}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
+    }
+  half8 w[G][N][2];
+  soften<D, G, N>(z, s, f, p, w);
   __builtin_amdgcn_sched_barrier(0);  // (V's codes are turned as they are needed: all at once they take 64 registers more)
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -482,24 +504,36 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, int first_token,
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
-      for (int x = 0; x < D / 32; ++x)
-        z.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half8<CODES>(v[n][x][2 * y], v[n][x][2 * y + 1]), w[n][y], z.o[x], 0, 0, 0);
+      for (int x = 0; x < D / 32; ++x) {
+        const half8 codes = codes_to_half8<CODES>(v[n][x][2 * y], v[n][x][2 * y + 1]);
+#pragma unroll
+        for (int g = 0; g < G; ++g) z[g].o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, w[g][n][y], z[g].o[x], 0, 0, 0);
+      }
   }
   behind();
 }
 
-// A wave's rows over the pairs first, first + stride, ... of the unit.  Q's operands lie in LDS, a copy for each wave: in registers they would not leave
-// room for two pairs at a time.
-template <int CODES, int D, int KIND>
-__device__ inline void attend_rows(const AttendArgs& a, const Unit& u, int hi, int listed, int head, int row0, int first, int stride, half8* q, Rows<D>& r,
-                                   State<D>& z) {
+template <int D>
+constexpr int kPitch = D + 4;  // of the rows that the waves put into LDS at the end
+
+// A unit of G groups of 32 rows.  Every wave takes a quarter of the tokens, pairs wave, wave + 4, ...; the four meet at the end.
+//   G = 1   two pairs at a time, so that a softmax's way through its lanes is taken once for 64 tokens
+//   G = 2   one pair at a time: what turning its codes costs, and reading them, serves twice as many rows
+// Q's operands lie in LDS, a copy for each wave (where its output goes later): in registers they would leave no room for that.
+template <int CODES, int D, int KIND, int G>
+__device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
   constexpr bool MARKS = KIND == kMarked;
-  const int lane = threadIdx.x & 63;
-  const int n_pairs = max(((hi - u.lo + 31) >> 5) - first + stride - 1, 0) / stride;
+  constexpr int N = 3 - G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 31, half = lane >> 5;
+  const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's
+  half8* q = (half8*)(lds + wave * kRows * kPitch<D>);
+  Rows<D> r[G];
+  State<D> z[G];
   Blocks b;
-  uint4v k[2][D / 32], v[2][D / 32], raw[D / 16];
-  Marks marks[2] = {};
-  auto token = [&](int i) { return u.lo + (first + stride * i) * 32; };  // first of the wave's i-th pair
+  int most = kEMin;  // largest exponent of V's scales so far
+  uint4v k[N][D / 32], v[N][D / 32];
+  Marks marks[N] = {};
+  auto token = [&](int i) { return u.lo + (wave + 4 * i) * 32; };  // first of the wave's i-th pair
   auto find = [&](int i) { find_blocks(a, u.request, head, token(i + (lane >> 1)) + (lane & 1) * 16, u.hi, b); };
   auto load_k = [&](int i, int to) {
     const int x = 2 * (i & 31);
@@ -509,151 +543,139 @@ __device__ inline void attend_rows(const AttendArgs& a, const Unit& u, int hi, i
     const int x = 2 * (i & 31);
     load_pieces(v_piece(a, __builtin_amdgcn_readlane(b.at, x), __builtin_amdgcn_readlane(b.at, x + 1), D), v[to]);
   };
-  start(z);
-  request_rows<D, MARKS>(a, u, head, row0, r, raw);
-  __builtin_amdgcn_sched_barrier(0);
-  // (everything is asked for before anything is waited for: loads come back in their order)
-  if (stride == 1 || u.hi - u.lo <= kUnitBlocks * kBlock)
-    on_block(a, token(lane >> 1) + (lane & 1) * 16 < u.hi ? listed : -1, head, b);
-  else
-    find(0);
-  // (where the wave has fewer than two pairs, block 0 is read in their place)
-  load_scales(a, b);
-  if constexpr (MARKS) marks[0] = load_marks(a, b, 0), marks[1] = load_marks(a, b, 1);
-  load_k(0, 0), load_k(1, 1);
-  load_v(0, 0), load_v(1, 1);
-  __builtin_amdgcn_sched_barrier(0);
   {
-    half8 x[D / 16];
-    finish_rows<D>(a, r, raw, x);
+    // Everything is asked for before anything is waited for: loads come back in their order.  (Where the wave has fewer than N pairs, block 0 is read in
+    // their place.)
+    uint4v raw[D / 16];
+    request_rows<D, MARKS>(a, u, head, 0, r[0], raw);
+    __builtin_amdgcn_sched_barrier(0);
+    if (u.hi - u.lo <= kUnitBlocks * kBlock)
+      on_block(a, 2 * (wave + 4 * (lane >> 1)) + (lane & 1) < kUnitBlocks ? listed : -1, head, b);
+    else
+      find(0);
+    load_scales(a, b);
 #pragma unroll
-    for (int y = 0; y < D / 16; ++y) q[y * 64 + lane] = x[y];
+    for (int n = 0; n < N; ++n)
+      if constexpr (MARKS) marks[n] = load_marks(a, b, n);
+#pragma unroll
+    for (int n = 0; n < N; ++n) load_k(n, n);
+#pragma unroll
+    for (int n = 0; n < N; ++n) load_v(n, n);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      half8 x[D / 16];
+      if (g) request_rows<D, MARKS>(a, u, head, g * kRows, r[g], raw);
+      finish_rows<D>(a, r[g], raw, x);
+#pragma unroll
+      for (int y = 0; y < D / 16; ++y) q[(g * (D / 16) + y) * 64 + lane] = x[y];
+    }
   }
-  finish_scales(b, z.most);
-  const int first_token = u.pos0 + (row0 >> a.g_shift);
+  finish_scales(b, most);
+#pragma unroll
+  for (int g = 0; g < G; ++g) start(z[g]);
   int i = 0;
-  for (; i + 1 < n_pairs; i += 2) {
-    const Pair p[2] = {pair_of(b, i & 31), pair_of(b, (i + 1) & 31)};
-    const int t0[2] = {token(i), token(i + 1)};
-    step<CODES, D, KIND, 2>(a, u, first_token, r, q, z, k, v, p, marks, t0,
+  for (; i + N - 1 < n_pairs; i += N) {
+    Pair p[N];
+    int t0[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) p[n] = pair_of(b, (i + n) & 31), t0[n] = token(i + n);
+    step<CODES, D, KIND, G, N>(a, u, r, q, z, k, v, p, marks, t0,
       [&] {
-        if (i + 2 >= n_pairs) return;
-        if (((i + 2) & 31) == 0) find(i + 2), load_scales(a, b), finish_scales(b, z.most);
-        if constexpr (MARKS) marks[0] = load_marks(a, b, (i + 2) & 31), marks[1] = load_marks(a, b, (i + 3) & 31);
-        load_k(i + 2, 0), load_k(i + 3, 1);
+        if (i + N >= n_pairs) return;
+        if (((i + N) & 31) == 0) find(i + N), load_scales(a, b), finish_scales(b, most);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if constexpr (MARKS) marks[n] = load_marks(a, b, (i + N + n) & 31);
+#pragma unroll
+        for (int n = 0; n < N; ++n) load_k(i + N + n, n);
       },
       [&] {
-        if (i + 2 < n_pairs) load_v(i + 2, 0), load_v(i + 3, 1);
+        if (i + N >= n_pairs) return;
+#pragma unroll
+        for (int n = 0; n < N; ++n) load_v(i + N + n, n);
       });
   }
-  if (i < n_pairs) {
-    const Pair p[1] = {pair_of(b, i & 31)};
-    const int t0[2] = {token(i), 0};
-    step<CODES, D, KIND, 1>(a, u, first_token, r, q, z, k, v, p, marks, t0, [] {}, [] {});
-  }
-}
-
-constexpr int kQBytes(int D) { return kRows * D * 2; }  // of a wave's Q
-
-// Every wave takes a quarter of the unit's tokens; the four meet at the end.
-template <int CODES, int D, int KIND>
-__device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
-  constexpr int kPitch = D + 4;
-  Rows<D> r;
-  State<D> z;
-  // (Q lies where the wave's output goes later)
-  attend_rows<CODES, D, KIND>(a, u, u.hi, listed, head, 0, wave, 4, (half8*)(lds + wave * kRows * kPitch), r, z);
-  // the four waves meet
-  float* s_o = lds;                                       // [4][32][kPitch]
-  float2v* s_ml = (float2v*)(lds + 4 * kRows * kPitch);   // [4][32]
-  const float l = z.l + other_half(z.l);
-  poison(z);
-  if (half == 0) s_ml[wave * kRows + n] = float2v{z.m, l};
-  if (r.real) {
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *(float4v*)(s_o + (wave * kRows + n) * kPitch + 32 * x + 8 * q + 4 * half) =
-            float4v{z.o[x][4 * q], z.o[x][4 * q + 1], z.o[x][4 * q + 2], z.o[x][4 * q + 3]};
-  }
-  __syncthreads();
-  for (int j = threadIdx.x; j < u.n_rows * (D / 4); j += 256) {
-    const int row = j / (D / 4), d = j % (D / 4) * 4;
-    float m = -FLT_MAX, all = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, s_ml[w * kRows + row][0]);
-    float4v o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float2v ml = s_ml[w * kRows + row];
-      const float f = __builtin_amdgcn_exp2f(ml[0] - m);
-      all = fmaf(ml[1], f, all);
-      o += *(const float4v*)(s_o + (w * kRows + row) * kPitch + d) * f;
+  if constexpr (N == 2) {
+    if (i < n_pairs) {
+      const Pair p[1] = {pair_of(b, i & 31)};
+      const int t0[1] = {token(i)};
+      const Marks last[1] = {marks[0]};
+      step<CODES, D, KIND, G, 1>(a, u, r, q, z, *(uint4v(*)[1][D / 32]) & k, *(uint4v(*)[1][D / 32]) & v, p, last, t0, [] {}, [] {});
     }
-    if (u.part < 0) {
-      const int64_t to = row_address(a, u.s0 + row, head);
-      store_out(a, to * D + d, o * inverse_of(all));
-      if (a.lse && d == 0) a.lse[to] = lse_of(m, all);
-    } else {
-      const int64_t to = (int64_t)(u.part + row) * a.g.Hkv + head;
-      *(float4v*)(a.part_acc + to * D + d) = o;
-      if (d == 0) a.part_ml[to] = float2v{m, all};
+  }
+  // the four waves meet, group after group
+  float* s_o = lds;                                         // [4][32][kPitch]
+  float2v* s_ml = (float2v*)(lds + 4 * kRows * kPitch<D>);  // [4][32]
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    if (g && u.n_rows <= g * kRows) break;
+    const float l = z[g].l + other_half(z[g].l);
+    poison(z[g]);
+    if (g) __syncthreads();
+    if (half == 0) s_ml[wave * kRows + row] = float2v{z[g].m, l};
+    if (r[g].real) {
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          *(float4v*)(s_o + (wave * kRows + row) * kPitch<D> + 32 * x + 8 * y + 4 * half) =
+              float4v{z[g].o[x][4 * y], z[g].o[x][4 * y + 1], z[g].o[x][4 * y + 2], z[g].o[x][4 * y + 3]};
+    }
+    __syncthreads();
+    const int rows = min(u.n_rows - g * kRows, kRows);
+    for (int j = threadIdx.x; j < rows * (D / 4); j += 256) {
+      const int i = j / (D / 4), d = j % (D / 4) * 4;
+      float m = -FLT_MAX, all = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) m = fmaxf(m, s_ml[w * kRows + i][0]);
+      float4v o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float2v ml = s_ml[w * kRows + i];
+        const float f = __builtin_amdgcn_exp2f(ml[0] - m);
+        all = fmaf(ml[1], f, all);
+        o += *(const float4v*)(s_o + (w * kRows + i) * kPitch<D> + d) * f;
+      }
+      if (u.part < 0) {
+        const int64_t to = row_address(a, u.s0 + g * kRows + i, head);
+        store_out(a, to * D + d, o * inverse_of(all));
+        if (a.lse && d == 0) a.lse[to] = lse_of(m, all);
+      } else {
+        const int64_t to = (int64_t)(u.part + g * kRows + i) * a.g.Hkv + head;
+        *(float4v*)(a.part_acc + to * D + d) = o;
+        if (d == 0) a.part_ml[to] = float2v{m, all};
+      }
     }
   }
 }
 
-// Every wave takes 32 rows of its own over all of the unit's tokens.  The four read the same codes at about the same time, and all but the first
-// find them in the CU's cache; turning them into fp16 four times over costs less than bringing them there once, through LDS, with a barrier for every
-// 64 tokens (long_nested of the table: 70.5 us a layer so, 
+// Two groups at a time do not fit the registers with 128 dims and tags or positions, or int8 codes and a cap: then a work-group (blockIdx.y) takes each.
 template <int CODES, int D, int KIND>
-__device__ inline void attend_many(const AttendArgs& a, const Unit& u, int listed, int head, uint8_t* lds) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
-  if (wave * kRows >= u.n_rows) return;
-  const int last_token = u.pos0 + ((min(wave * kRows + kRows, u.n_rows) - 1) >> a.g_shift);
-  Rows<D> r;
-  State<D> z;
-  attend_rows<CODES, D, KIND>(a, u, min(u.hi, max(last_token + 1, u.prefix)), listed, head, wave * kRows, 0, 1, (half8*)(lds + wave * kQBytes(D)), r, z);
-  const float l = z.l + other_half(z.l);
-  poison(z);
-  if (!r.real) return;
-  const int row = wave * kRows + n;
-  if (u.part < 0) {
-    const int64_t to = row_address(a, u.s0 + row, head);
-    const float f = inverse_of(l);
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        store_out(a, to * D + 32 * x + 8 * q + 4 * half, float4v{z.o[x][4 * q] * f, z.o[x][4 * q + 1] * f, z.o[x][4 * q + 2] * f, z.o[x][4 * q + 3] * f});
-    if (a.lse && half == 0) a.lse[to] = lse_of(z.m, l);
-  } else {
-    const int64_t to = (int64_t)(u.part + row) * a.g.Hkv + head;
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *(float4v*)(a.part_acc + to * D + 32 * x + 8 * q + 4 * half) = float4v{z.o[x][4 * q], z.o[x][4 * q + 1], z.o[x][4 * q + 2], z.o[x][4 * q + 3]};
-    if (half == 0) a.part_ml[to] = float2v{z.m, l};
-  }
-}
+constexpr bool kApart = D == 128 && (KIND == kMarked || (KIND == kShaped && CODES == kInt8));
 
 template <int CODES, int D, bool MANY, int KIND>
 __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
-  constexpr int kFewBytes = 4 * kRows * (D + 4) * 4 + 4 * kRows * 8;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kFewBytes];  // (more than four waves' Q)
+  __shared__ __attribute__((aligned(16))) float lds[4 * kRows * kPitch<D> + 4 * kRows * 2];
   const int head = blockIdx.x % a.g.Hkv, unit = blockIdx.x / a.g.Hkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Unit u = a.units[unit];
-  // the lane's block, asked for together with the unit: in attend_few pairs are dealt out to the four waves
-  const int dealt = a.unit_blocks[unit * kUnitBlocks + min(2 * (wave + 4 * (lane >> 1)) + (lane & 1), kUnitBlocks - 1)];
-  const int listed = MANY ? a.unit_blocks[unit * kUnitBlocks + lane] : 0;
+  Unit u = a.units[unit];
+  // the lane's block, asked for together with the unit: pairs are dealt out to the four waves
+  const int listed = a.unit_blocks[unit * kUnitBlocks + min(2 * (wave + 4 * (lane >> 1)) + (lane & 1), kUnitBlocks - 1)];
   asm volatile("" ::"s"(u.request), "s"(u.s0), "s"(u.pos0), "s"(u.lo), "s"(u.hi), "s"(u.prefix), "s"(u.part));  // (one load, ahead of the branch)
-  if (u.n_rows == 0) return;
-  if (MANY && u.n_rows > kRows)
-    attend_many<CODES, D, KIND>(a, u, listed, head, lds);
-  else
-    attend_few<CODES, D, KIND>(a, u, dealt, head, (float*)lds);
+  if constexpr (MANY && kApart<CODES, D, KIND>) {
+    const int first = blockIdx.y * kRows;
+    u.s0 += first, u.n_rows = min(u.n_rows - first, kRows), u.pos0 += first >> a.g_shift;
+    if (u.part >= 0) u.part += first;
+  }
+  if (u.n_rows <= 0) return;
+  if constexpr (MANY && !kApart<CODES, D, KIND>) {
+    if (u.n_rows > kRows)
+      attend_unit<CODES, D, KIND, 2>(a, u, listed, head, lds);
+    else
+      attend_unit<CODES, D, KIND, 1>(a, u, listed, head, lds);
+  } else {
+    attend_unit<CODES, D, KIND, 1>(a, u, listed, head, lds);
+  }
 }
 
 // Joins the partial rows of the tiles whose tokens are split.  D / 4 lanes hold a row, four dims apiece; the 1024 / D such groups of a

@@ -12,8 +12,11 @@ namespace k8 {
 constexpr int kBlock = 16;           // tokens under one scale
 constexpr int kEMin = -100, kEMax = 119;
 constexpr int kRows = 32;            // stacked rows (query row x head of the kv head's group) of one wave
-constexpr int kWideRows = 128;       // ... of one work-group whose four waves share tiles
-constexpr int kChunkTokens = 128;    // tokens a work-group takes at least
+constexpr int kWideRows = 64;        // ... of one work-group, in requests that have more than kManyRows
+constexpr int kManyRows = 128;
+constexpr int kChunkTokens = 128;    // pieces of a tile's tokens are multiples of this (32 for each wave) ...
+constexpr int kLeastTokens = 384;    // ... and no shorter than this
+constexpr int kMostTokens = 1 << 27; // of a request: a plan's sums over 1024 tiles stay within 32 bits
 constexpr int kUnitBlocks = 64;      // blocks of a unit that are listed with it
 enum { kE4m3 = 0, kInt8 = 1 };
 enum { kF32 = 0, kBf16 = 1, kF16 = 2 };

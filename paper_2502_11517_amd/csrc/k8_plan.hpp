@@ -1,9 +1,10 @@
 // Split of the attention's work: which stacked rows of which request over which tokens, a unit per (rows, tokens), times Hkv.
 //
-// Rows come in tiles of 32 (a work-group whose waves split the tokens) or, in requests with more stacked rows than that, of 128 (four
-// waves of 32 rows over the same tokens).  Tokens are split so that about as many work-groups run as the chip holds; a tile whose
-// tokens are split leaves partial rows, which k8_merge joins.  One work-group; what it takes is the way through its dependent reads and sums,
-// so a step's tiles, where they fit, stay in LDS and are looked at once.
+// Rows come in tiles of 32, or, in requests with more than 128 stacked rows, of 64 (a wave then turns its codes once for two groups; with fewer rows,
+// fewer and longer pieces of the tokens are worth more: 128 rows over 49k tokens 60 us a layer in tiles of 32, 87 of 64).  Tokens are split so that
+// about as many work-groups run as the chip holds; a tile whose tokens are split leaves partial rows, which k8_merge joins.  A piece has at
+// least 384 tokens, if the tile has: 8 x 1 row over 8k tokens in pieces of at least 256 / 384 / 512 / 640 / 768 tokens took 142 / 124 / 128 / 138 / 147 us
+// over eight layers (shorter ones cost more partial rows than they save, longer ones leave CUs idle).
 #pragma once
 #include "k8_dev.hpp"
 
@@ -12,9 +13,8 @@ namespace k8 {
 struct PlanArgs {
   Geometry g;
   int n_requests, n_rows;
-  int wide;       // requests with more than 32 stacked rows take tiles of 128
+  int wide;       // requests with more than kManyRows stacked rows take tiles of 64
   int capacity;   // units that the chip takes at once
-  int whole;      // tokens up to which a tile is not split
   int max_units, max_tiles, max_part_rows;
   const int *length, *row_offsets, *prefix_len, *slot, *table;
   Unit* units;
@@ -44,7 +44,7 @@ __device__ inline RequestTiles request_tiles(const PlanArgs& a, int r) {
   }
   q.prefix = min(max(prefix, 0), q.length);
   const int64_t stacked = (int64_t)q.n * a.g.G;
-  q.tile_rows = a.wide && stacked > kRows ? kWideRows : kRows;
+  q.tile_rows = a.wide && stacked > kManyRows ? kWideRows : kRows;
   q.n_tiles = (int)((stacked + q.tile_rows - 1) / q.tile_rows);
   return q;
 }
@@ -63,9 +63,9 @@ __device__ inline Unit tile_of(const PlanArgs& a, int r, const RequestTiles& q, 
   return u;
 }
 
-__device__ inline int chunks_of(int tokens) { return min((tokens + kChunkTokens - 1) / kChunkTokens, 1 << 20); }
+__device__ inline int chunks_of(int tokens) { return (tokens + kChunkTokens - 1) / kChunkTokens; }
 
-__device__ inline int parts_of(const PlanArgs& a, int tokens, int chunk) { return tokens <= max(chunk, a.whole) ? 1 : (tokens + chunk - 1) / chunk; }
+__device__ inline int parts_of(int tokens, int chunk) { return max(1, (tokens + chunk - 1) / chunk); }
 
 __device__ inline Unit part_of(Unit u, int k, int parts, int chunk, int row_at) {
   const int hi = u.hi;
@@ -123,8 +123,8 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
     __syncthreads();
     chunk = min(chunk, s_tmp[NT / 64]);
   }
-  chunk *= kChunkTokens;
-  const int parts = tid < n_tiles ? parts_of(a, u.hi, chunk) : 0;
+  chunk = max(min(chunk, kMostTokens / kChunkTokens) * kChunkTokens, kLeastTokens);
+  const int parts = tid < n_tiles ? parts_of(u.hi, chunk) : 0;
   int all;
   const int at = group_scan<NT>(parts, s_tmp, all) - parts;
   const int rows = parts > 1 ? parts * u.n_rows : 0;
@@ -142,7 +142,8 @@ template <int NT>
 __global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
   __shared__ int s_tmp[NT / 64];
   const int tid = threadIdx.x;
-  int n_tiles = 0, work = 0;
+  int n_tiles = 0;
+  int64_t work = 0;
   for (int r0 = 0; r0 <= a.n_requests; r0 += NT) {
     const int r = r0 + tid;
     int mine = 0, all;
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
     work += all;
   }
   const int room = max(max(a.capacity - n_tiles, a.capacity / 2), 1);
-  const int chunk = max(1, (work + room - 1) / room) * kChunkTokens;
+  const int chunk = max((int)min((work + room - 1) / room, (int64_t)(kMostTokens / kChunkTokens)) * kChunkTokens, kLeastTokens);
   int n_units = 0, n_part_rows = 0;
   for (int j0 = 0; j0 < n_tiles; j0 += NT) {
     const int j = j0 + tid;
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
     int parts = 0, all, all_rows;
     if (j < n_tiles) {
       u = tile(j);
-      parts = parts_of(a, u.hi, chunk);
+      parts = parts_of(u.hi, chunk);
     }
     const int at = n_units + group_scan<NT>(parts, s_tmp, all) - parts;
     const int rows = parts > 1 ? parts * u.n_rows : 0;

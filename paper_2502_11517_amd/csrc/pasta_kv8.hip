@@ -15,7 +15,6 @@
 namespace {
 
 constexpr uint64_t kMagic = 0x3876'6b61'7473'6170ull;
-constexpr int kWholeTokens = 384;  // of a tile that is not split
 constexpr int kUnitsAtOnce = 512;  // work-groups of the attention: two per CU
 
 struct Bounds {
@@ -57,7 +56,7 @@ int32_t check(const pasta_kv8_config* c) {
   if (c->page_tokens < 16 || c->page_tokens > 4096 || (c->page_tokens & (c->page_tokens - 1))) return PASTA_E_INVAL;
   if (!std::isfinite(c->softmax_scale)) return PASTA_E_INVAL;
   const int64_t most = INT32_MAX;
-  if ((int64_t)c->n_phys_pages * c->page_tokens > most || (int64_t)c->pages_per_request * c->page_tokens > most) return PASTA_E_INVAL;
+  if ((int64_t)c->n_phys_pages * c->page_tokens > most || (int64_t)c->pages_per_request * c->page_tokens > k8::kMostTokens) return PASTA_E_INVAL;
   if ((int64_t)c->n_phys_pages * c->n_kv_heads * (c->page_tokens / 16) > most) return PASTA_E_INVAL;  // index of a scale within a layer
   if ((int64_t)c->max_requests * c->pages_per_request > most || c->max_requests > (1 << 20)) return PASTA_E_INVAL;
   if ((int64_t)c->max_rows * c->n_q_heads > most / 8) return PASTA_E_INVAL;
@@ -80,7 +79,7 @@ Bounds bounds(const pasta_kv8_config& c, int64_t n_rows, int64_t n_requests, boo
 }
 
 uint64_t lay_out(const pasta_kv8_config& c, pasta_kv8* h) {
-  const Bounds b = bounds(c, c.max_rows, c.max_requests, (int64_t)c.max_rows * (c.n_q_heads / c.n_kv_heads) > k8::kRows);
+  const Bounds b = bounds(c, c.max_rows, c.max_requests, (int64_t)c.max_rows * (c.n_q_heads / c.n_kv_heads) > k8::kManyRows);
   uint64_t at = 0;
   auto take = [&](auto*& p, uint64_t n) {
     p = reinterpret_cast<std::remove_reference_t<decltype(p)>>((uint8_t*)c.workspace + at);
@@ -234,14 +233,14 @@ extern "C" int32_t pasta_kv8_plan(pasta_kv8* h, const pasta_kv8_plan_args* a) {
   h->plan_rows = a->n_rows;
   if (a->n_rows == 0) return PASTA_OK;
   const int64_t most = a->max_request_rows < a->n_rows ? a->max_request_rows : a->n_rows;
-  h->plan_wide = most * h->g.G > k8::kRows;
+  h->plan_wide = most * h->g.G > k8::kManyRows;
   h->plan = bounds(c, a->n_rows, a->n_requests, h->plan_wide);
   k8::PlanArgs k{};
   k.g = h->g, k.n_requests = a->n_requests, k.n_rows = a->n_rows, k.wide = h->plan_wide, k.capacity = (int)h->plan.capacity;
   k.max_units = (int)h->plan.units, k.max_tiles = (int)h->plan.tiles, k.max_part_rows = (int)h->plan.part_rows;
   k.length = a->n_requests ? a->length : a->row_offsets;  // (read, not used, without a request)
   k.row_offsets = a->row_offsets, k.prefix_len = a->prefix_len, k.slot = a->slot;
-  k.table = c.page_table, k.whole = kWholeTokens;
+  k.table = c.page_table;
   k.units = h->units, k.unit_blocks = h->unit_blocks, k.tiles = h->tiles, k.w_tiles = h->tiles_upto;
   hipStream_t s = (hipStream_t)c.hip_stream;
   if (h->plan.tiles <= 256 && a->n_requests < 256) {
@@ -260,7 +259,10 @@ namespace {
 template <int CODES, int D>
 void launch_attend(const k8::AttendArgs& k, bool many, int64_t groups, hipStream_t s) {
   const int kind = k.tagged || k.placed ? k8::kMarked : k.lowered || k.cap_log2 > 0.f ? k8::kShaped : k8::kPlain;
-  auto launch = [&](auto of, auto kind) { k8::k8_attend<CODES, D, of.value, kind.value><<<(unsigned)groups, 256, 0, s>>>(k); };
+  auto launch = [&](auto of, auto kind) {
+    const dim3 grid((unsigned)groups, of.value && k8::kApart<CODES, D, kind.value> ? k8::kWideRows / k8::kRows : 1);
+    k8::k8_attend<CODES, D, of.value, kind.value><<<grid, 256, 0, s>>>(k);
+  };
   auto with = [&](auto of) {
     if (kind == k8::kMarked) launch(of, std::integral_constant<int, k8::kMarked>{});
     else if (kind == k8::kShaped) launch(of, std::integral_constant<int, k8::kShaped>{});
@@ -310,7 +312,7 @@ extern "C" int32_t pasta_kv8_attend(pasta_kv8* h, const pasta_kv8_attend_args* a
     c.head_dim == 128 ? launch_attend<k8::kE4m3, 128>(k, many, groups, s) : launch_attend<k8::kE4m3, 64>(k, many, groups, s);
   else
     c.head_dim == 128 ? launch_attend<k8::kInt8, 128>(k, many, groups, s) : launch_attend<k8::kInt8, 64>(k, many, groups, s);
-  if ((int64_t)c.pages_per_request * c.page_tokens > kWholeTokens) {  // no tile is split otherwise
+  if ((int64_t)c.pages_per_request * c.page_tokens > k8::kLeastTokens) {  // no tile is split otherwise
     const int64_t tiles = h->plan.tiles * c.n_kv_heads;
     int64_t split = (2048 + tiles - 1) / tiles;  // work-groups to a tile: rows, one by one where there are so few tiles
     if (split > h->plan.merge_rows) split = h->plan.merge_rows;
