@@ -197,6 +197,17 @@ def test_rows_that_see_nothing(n):
     assert (out[0::2] == 0).all() and np.isneginf(lse[0::2]).all() and np.isfinite(lse[1::2]).all()
 
 
+@pytest.mark.parametrize("codes,dtype,D,Hq,Hkv", SHAPES)
+@pytest.mark.parametrize("n", [5, 70, 161])
+@pytest.mark.parametrize("tags,cap", [(True, 0.0), (True, 20.0), (False, 20.0)])
+def test_everything_at_once_over_split_tokens(codes, dtype, D, Hq, Hkv, n, tags, cap):
+    c = Case([n, tags, int(cap)], codes, dtype, Hq, Hkv, D, 16, [1700, 0, 230], [n, 0, 3])
+    see = c.rng.integers(-2 ** 63, 2 ** 63, c.n)
+    see[n // 2] = 0
+    slopes = c.rng.uniform(0.0, 0.01, Hq).astype(np.float32)
+    c.check(see=see if tags else None, prefix=[90, 0, 17], cap=cap, slopes=slopes, row_position=c.rng.integers(0, 1700, c.n) if tags else None)
+
+
 def test_streams_with_blocks_of_one_tag_and_of_many():
     c = Case(11, length=[260], rows=[8])
     for r in range(1):

@@ -65,7 +65,8 @@ class Step:
 
 
 @pytest.mark.parametrize("P", [16, 64])
-@pytest.mark.parametrize("R,most,rows", [(1, 0, 1), (1, 100, 1), (1, 0, 300), (16, 300, 8), (64, 40, 3), (65, 40, 3), (200, 200, 20), (1500, 90, 5),
+@pytest.mark.parametrize("R,most,rows", [(1, 0, 1), (1, 100, 1), (1, 0, 300), (16, 300, 8), (64, 40, 3), (65, 40, 3), (200, 200, 20), (256, 30, 40), (257, 90, 3), (512, 60, 5),
+                                         (700, 60, 5), (1024, 50, 3), (1025, 50, 3), (1500, 90, 5),
                                          (3, 50, 3000), (3, 50, 6000)])
 def test_steps_of_all_sizes(P, R, most, rows):
     rng = np.random.default_rng([P, R, rows])
@@ -77,7 +78,7 @@ def test_steps_of_all_sizes(P, R, most, rows):
 
 
 @pytest.mark.parametrize("in_place", [False, True])
-@pytest.mark.parametrize("R", [7, 90, 1100])
+@pytest.mark.parametrize("R", [7, 90, 400, 1000, 1100])
 def test_rows_taken_back_and_requests_released(R, in_place):
     rng = np.random.default_rng(R)
     P = 16

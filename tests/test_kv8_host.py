@@ -52,7 +52,7 @@ def test_every_declared_symbol_is_exported():
                                 dict(n_kv_heads=0), dict(n_kv_heads=-8), dict(n_q_heads=257, n_kv_heads=257), dict(head_dim=96), dict(head_dim=256),
                                 dict(n_layers=0), dict(max_requests=0), dict(max_rows=0), dict(page_tokens=8), dict(page_tokens=24),
                                 dict(page_tokens=8192), dict(n_phys_pages=0), dict(pages_per_request=0), dict(softmax_scale=float("nan")),
-                                dict(softmax_scale=float("inf")), dict(n_phys_pages=1 << 27), dict(n_phys_pages=1 << 28, page_tokens=4096),
+                                dict(softmax_scale=float("inf")), dict(n_phys_pages=1 << 27), dict(n_phys_pages=1 << 28, page_tokens=4096), dict(pages_per_request=(1 << 23) + 1),
                                 dict(pages_per_request=1 << 27), dict(max_requests=1 << 20, pages_per_request=1 << 12), dict(max_rows=1 << 24)])
 def test_configurations_that_are_refused(kw):
     with pytest.raises(kv8.PastaError) as e:
