@@ -66,7 +66,7 @@ __device__ inline float other_half(float x) {  // of lane ^ 32
 // uses it (v_subrev_u32 with row_newbcast), every lane got its own value on this chip.
 template <int I>
 __device__ inline int of_row(int x) {
-  int y = __builtin_amdgcn_update_dpp(0, x, 0x150 + I, 0xf, 0xf, false);
+  int y = __builtin_amdgcn_update_dpp(0, x, 0x150 + I, 0xf, 0xf, true);
   asm("" : "+v"(y));
   return y;
 }
@@ -89,6 +89,7 @@ struct Rows {
   int first_token;  // the wave's first row's
   int position;
   uint64_t see;
+  int by_tag;  // lane t: which of the wave's rows see tag t
   bool real;
 };
 
@@ -113,6 +114,17 @@ __device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head
   } else {
     r.see = 0, r.position = 0;
   }
+}
+
+// Lane t: which of the wave's rows see tag t; lane n's `see` is that of row n.
+__device__ inline int rows_by_tag(uint64_t see, int g_shift) {
+  const int heads = (1 << (1 << g_shift)) - 1;
+  int rows = 0;
+  for (int n = 0; n < kRows; n += 1 << g_shift) {
+    const uint64_t tags = (uint32_t)__builtin_amdgcn_readlane((int)see, n) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(see >> 32), n) << 32;
+    rows |= __builtin_amdgcn_inverse_ballot_w64(tags) ? heads << n : 0;
+  }
+  return rows;
 }
 
 template <int D>
@@ -248,31 +260,29 @@ enum { kPlain = 0, kShaped = 1, kMarked = 2 };
 struct Unmarked {
   template <class F>
   __device__ void distances(F) const {}
-  template <class F>
-  __device__ void sights(F) const {}
-  __device__ bool alike(bool&) const { return false; }
+  __device__ int rows() const { return 0; }
 };
 
-// attend_few: from the tokens' marks in the wave's own lanes.
-struct MarkedHere {
+struct Marked {
   Marks marks;
-  int position;
-  uint64_t see;
+  int position, by_tag;
   template <class F>
   __device__ void distances(F f) const {
     each<16>([&](auto i) { f(i.value, (float)(position - of_row<i.value>(marks.position))); });
   }
-  template <class F>
-  __device__ void sights(F f) const {
-    const int up = 63 - (marks.tag & 63);
-    each<16>([&](auto i) { f(i.value, (int64_t)(see << of_row<i.value>(up)) < 0); });
-  }
-  __device__ bool alike(bool& sees) const {  // one tag for all of the lane's tokens, for every lane
-    const int first = of_row<0>(marks.tag);
-    sees = (see >> (first & 63)) & 1;
-    return __all(marks.tag == first);
-  }
+  __device__ int rows() const { return __builtin_amdgcn_ds_bpermute((marks.tag & 63) * 4, by_tag); }  // that see the lane's token
 };
+
+// f(i, whether the lane's row sees token i of its block: -1 or 0), from the rows that see the lane's token.
+template <class F>
+__device__ inline void sights(int rows, F f) {
+  const int row = threadIdx.x & 31;
+  each<16>([&](auto i) { f(i.value, __builtin_amdgcn_sbfe(of_row<i.value>(rows), row, 1)); });
+}
+
+__device__ inline float shown(float s, int seen) {  // where seen is -1, else -inf
+  return __uint_as_float((__float_as_uint(s) & seen) | (0xff800000u & ~seen));
+}
 
 // Scores of a pair, tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
 // left so where nothing has to be done; else they come out in log2 units and f is 1.
@@ -304,28 +314,25 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     }
   }
   if (!masked) return;
-  if (KIND == kMarked && a.tagged && t0 >= prefix && !ordered && !cut) {  // tags alone
-    bool sees;
-    if (source.alike(sees)) {
-      if (!sees)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = -INFINITY;
-    } else {
-      source.sights([&](int i, bool seen) { s[i] = seen ? s[i] : -INFINITY; });
+  int rows = 0;
+  if (KIND == kMarked && a.tagged) {
+    rows = source.rows();
+    if (t0 >= prefix && !ordered && !cut) {  // tags alone
+      if (!__all(rows == -1)) sights(rows, [&](int i, int seen) { s[i] = shown(s[i], seen); });
+      return;
     }
-    return;
   }
   auto below = [](int n) { return n <= 0 ? 0u : n >= kBlock ? 0xffffu : (1u << n) - 1u; };
   uint32_t bits = below(token + 1 - base);
   if (KIND == kMarked && a.tagged) {
     uint32_t tagged = 0;
-    source.sights([&](int i, bool seen) { tagged |= seen ? 1u << i : 0u; });
+    sights(rows, [&](int i, int seen) { tagged |= (uint32_t)seen & (1u << i); });
     bits &= tagged;
   }
   bits |= below(prefix - base);
   bits = of_half(p.absent) ? 0u : bits & below(hi - base);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] = (bits >> i) & 1 ? s[i] : -INFINITY;
+  for (int i = 0; i < 16; ++i) s[i] = shown(s[i], __builtin_amdgcn_sbfe((int)bits, i, 1));
 }
 
 // Running state of a wave's rows.
@@ -491,7 +498,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
     for (int n = 0; n < N; ++n) {
       f[g][n] = r[g].c * p[n].ks;
       if constexpr (KIND == kMarked)
-        finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], MarkedHere{m[n], r[g].position, r[g].see}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
+        finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], Marked{m[n], r[g].position, r[g].by_tag}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
       else
         finish_scores<KIND>(a, u.prefix, u.hi, t0[n], p[n], Unmarked{}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
     }
@@ -567,6 +574,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
       half8 x[D / 16];
       if (g) request_rows<D, MARKS>(a, u, head, g * kRows, r[g], raw);
       finish_rows<D>(a, r[g], raw, x);
+      if constexpr (MARKS) r[g].by_tag = rows_by_tag(r[g].see, a.g_shift);
 #pragma unroll
       for (int y = 0; y < D / 16; ++y) q[(g * (D / 16) + y) * 64 + lane] = x[y];
     }
