@@ -10,6 +10,7 @@ threads can be captured into a graph and replayed, each replay one token further
 """
 from __future__ import annotations
 
+from collections import Counter
 from dataclasses import dataclass, field
 
 import torch
@@ -32,8 +33,6 @@ class Thread:
 class _Request:
     threads: list = field(default_factory=list)
     used: int = 0  # set of tags
-    rows: int = 0
-    prefix: int = 0
 
 
 class Session:
@@ -60,15 +59,18 @@ class Session:
         self.slopes = None if slopes is None else torch.as_tensor(slopes, dtype=torch.float32, device=self.device)
         self.logit_cap = logit_cap
         self.requests = [_Request() for _ in range(max_requests)]
-        self.handle = self._step = None
+        self.handle = self._step = self._stream = None
         self.bind(torch.cuda.current_stream(self.device))
 
     def bind(self, stream):
-        """Work of later calls goes to this stream; the caller orders it behind what was enqueued before."""
+        """Work of later calls goes to this stream; the caller orders it behind what was enqueued before.  A step that had begun goes on with again()."""
+        self._stream = stream
         self.handle = kv8.PastaKv8(self.cfg, self.workspace, page_table=self.page_table, k_codes=self.k_codes, v_codes=self.v_codes,
                                    k_scale=self.k_scale, v_scale=self.v_scale, free_pages=self.free_pages, slot_tag=self.slot_tag,
                                    slot_position=self.slot_position, stream=stream.cuda_stream)
-        self._step = None
+        if self._step is not None:  # memory of the new stream's, that it may be given back behind its work
+            with torch.cuda.stream(stream):
+                self._step = {k: v.clone() if torch.is_tensor(v) else v for k, v in self._step.items()}
 
     # ---- threads (host) ------------------------------------------------------------------------
     def _new_tag(self, request):
@@ -112,18 +114,29 @@ class Session:
             o.alive = False
             r.threads.remove(o)
         if len(r.threads) == 1:
-            # everything written is seen: a prefix, and the tags are free again
-            r.prefix, r.used = r.rows, 1
-            thread.tag, thread.sees = 0, 1
-            self.prefix_len[thread.request] = r.rows
+            # everything written is seen: a prefix, as long as the device says (a step may have been refused), and the tags are free again
+            r.used, thread.tag, thread.sees = 1, 0, 1
+            self._on_stream(lambda: self.prefix_len[thread.request].copy_(self.length[thread.request]))
 
     def release(self, request):
-        """Ends the request's threads; its pages go back with the next step."""
+        """Ends the request's threads and gives its pages back."""
         r = self.requests[request]
         for t in r.threads:
             t.alive = False
         self.requests[request] = _Request()
-        self.prefix_len[request] = 0
+        n = len(self.requests)
+
+        def give_back():
+            self.prefix_len[request].zero_()
+            keep = self.length.clone()
+            keep[request].zero_()
+            self.handle.slots(self.length, torch.zeros(n + 1, dtype=torch.int32, device=self.device), 0, None, self.length, self.free_count,
+                              self.free_count, keep=keep)
+        self._on_stream(give_back)
+
+    def _on_stream(self, what):
+        with torch.cuda.stream(self._stream):
+            what()
 
     # ---- a step --------------------------------------------------------------------------------
     def begin(self, rows, positions=None):
@@ -138,37 +151,33 @@ class Session:
             count[t.request] += 1
             ids.append(t.position if positions is None else int(positions[i]))
             t.position = ids[-1] + 1
-        for r, k in zip(self.requests, count):
-            r.rows += k
         offsets = [0]
         for k in count:
             offsets.append(offsets[-1] + k)
         dev = lambda x, t: torch.tensor(x, dtype=t).to(self.device)  # noqa: E731
         signed = [t.sees - (1 << 64) if t.sees >> 63 else t.sees for t in rows]
-        keep = dev([r.rows - k for r, k in zip(self.requests, count)], torch.int32)
-        self._step = dict(n=n, most=max(count), offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8),
-                          see=dev(signed, torch.int64), position=dev(ids, torch.int32), keep=keep)
-        self.handle.slots(self.length, self._step["offsets"], n, self.slot, self.length, self.free_count, self.free_count, keep=keep,
-                          row_tag=self._step["tag"], row_position=self._step["position"])
-        self._plan()
+        times = Counter(id(t) for t in rows)
+        self._on_stream(lambda: self._enter(dict(
+            n=n, most=max(count), offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8), see=dev(signed, torch.int64),
+            position=dev(ids, torch.int32), stride=dev([times[id(t)] for t in rows], torch.int32))))
+
+    def _enter(self, step):
+        self._step = step
+        self.handle.slots(self.length, step["offsets"], step["n"], self.slot, self.length, self.free_count, self.free_count, row_tag=step["tag"],
+                          row_position=step["position"])
+        self.handle.plan(self.length, step["offsets"], step["n"], max_request_rows=step["most"], prefix_len=self.prefix_len, slot=self.slot)
 
     def again(self):
-        """The same threads, one row further: what a replayed graph does.  (On the host their counts go on too.)"""
-        s = self._step
-        self.handle.slots(self.length, s["offsets"], s["n"], self.slot, self.length, self.free_count, self.free_count, row_tag=s["tag"],
-                          row_position=s["position"])
-        self._plan()
-        s["position"].add_(1)
+        """The step's threads once more, each as many rows further as it has in the step: what a replayed graph does."""
+        def go_on():
+            self._step["position"].add_(self._step["stride"])
+            self._enter(self._step)
+        self._on_stream(go_on)
 
     def advanced(self, rows, steps):
-        """Tells the host that `steps` replays of again() with these threads have been enqueued."""
+        """Tells the host that `steps` calls or replays of again() with these rows have been enqueued."""
         for t in rows:
             t.position += steps
-            self.requests[t.request].rows += steps
-
-    def _plan(self):
-        s = self._step
-        self.handle.plan(self.length, s["offsets"], s["n"], max_request_rows=s["most"], prefix_len=self.prefix_len, slot=self.slot)
 
     def layer(self, layer, k_new, v_new, q, out, lse=None):
         """Appends the step's rows of a layer, then attends: row i sees its own row too."""
@@ -197,14 +206,11 @@ def main():
     forward(300)
     threads = [s.fork(root) for _ in range(n)]
     s.begin(threads)
-    s._step["position"].add_(1)
     forward(n)
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
-    step = s._step
     with torch.cuda.stream(stream):
         s.bind(stream)
-        s._step = step
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=stream):
             s.again()

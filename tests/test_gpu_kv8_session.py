@@ -198,6 +198,61 @@ def test_replays_of_one_captured_step_are_the_steps_called(n):
     assert torch.equal(a.k_scale[:, pages], b.k_scale[:, pages]) and int(a.length[0]) == 100 + n * 31
 
 
+@pytest.mark.parametrize("twice", [False, True])
+def test_going_on_is_the_same_as_beginning_again(twice):
+    """again() against begin() with the same threads: places, positions (and so the scores, which distance lowers), outputs."""
+    got = []
+    for begin in (True, False):
+        torch.manual_seed(11)
+        s = Session(n_q_heads=4, n_kv_heads=2, head_dim=64, softmax_scale=0.125, max_rows=64, n_phys_pages=60, pages_per_request=40,
+                    slopes=[0.5, 0.25, 0.125, 0.0625])
+        root = s.open(0)
+        x = lambda n, h: torch.randn(n, h, 64, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+        s.begin([root] * 20)
+        s.layer(0, x(20, 2), x(20, 2), x(20, 4), torch.empty(20, 4, 64, device="cuda", dtype=torch.bfloat16))
+        threads = [s.fork(root) for _ in range(3)] * (2 if twice else 1)
+        threads.sort(key=id)
+        n = len(threads)
+        for i in range(5):
+            if begin or i == 0:
+                s.begin(threads)
+            else:
+                s.again()
+                s.advanced(threads, 1)
+            out, lse = torch.empty(n, 4, 64, device="cuda", dtype=torch.bfloat16), torch.empty(n, 4, device="cuda")
+            s.layer(0, x(n, 2), x(n, 2), x(n, 4), out, lse)
+            got.append((out, lse, s.slot[:n].clone(), s.slot_position[s.slot[:n].long()]))
+        assert sorted(t.position for t in threads) == [20 + 5 * n // 3] * n
+    for a, b in zip(got[:5], got[5:]):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_what_a_released_request_held_is_not_seen_by_the_next_one_even_if_that_is_refused():
+    s = Session(n_q_heads=2, n_kv_heads=2, head_dim=64, softmax_scale=0.125, max_requests=2, max_rows=64, n_phys_pages=4, pages_per_request=8)
+    x = lambda n, h: torch.randn(n, h, 64, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+
+    def step(rows):
+        n = len(rows)
+        out, lse = torch.empty(n, 2, 64, device="cuda", dtype=torch.bfloat16), torch.zeros(n, 2, device="cuda")
+        s.begin(rows)
+        s.layer(0, x(n, 2), x(n, 2), x(n, 2), out, lse)
+        return out, lse
+
+    a, b = s.open(0), s.open(1)
+    step([a] * 32 + [b] * 16)
+    s.release(0)
+    assert s.length.tolist() == [0, 16] and int(s.free_count) == 3
+    a = s.open(0)
+    out, lse = step([a] * 60)  # four pages
+    assert s.length.tolist() == [0, 16] and (out == 0).all() and torch.isneginf(lse).all()
+    kid = s.fork(a)
+    step([a] * 5 + [kid] * 3)
+    s.join(a, [kid])
+    assert s.prefix_len.tolist() == [8, 0] == [int(s.length[0]), 0]
+    step([a])
+    assert s.length.tolist() == [9, 16]
+
+
 def test_the_example_runs(capsys):
     main()
     assert "tokens 400" in capsys.readouterr().out
