@@ -260,6 +260,7 @@ enum { kPlain = 0, kShaped = 1, kMarked = 2 };
 struct Unmarked {
   template <class F>
   __device__ void distances(F) const {}
+  __device__ bool in_order(float&) const { return false; }
   __device__ int rows() const { return 0; }
 };
 
@@ -269,6 +270,12 @@ struct Marked {
   template <class F>
   __device__ void distances(F f) const {
     each<16>([&](auto i) { f(i.value, (float)(position - of_row<i.value>(marks.position))); });
+  }
+  // Whether the tokens' positions go up by one from each to the next, as in a prompt; then how far the lane's first token is from its row.
+  __device__ bool in_order(float& far) const {
+    const int first = of_row<0>(marks.position);
+    far = (float)(position - first);
+    return __all(marks.position - first == (int)(threadIdx.x & 15));
   }
   __device__ int rows() const { return __builtin_amdgcn_ds_bpermute((marks.tag & 63) * 4, by_tag); }  // that see the lane's token
 };
@@ -299,21 +306,30 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     const float g = f * a.cap_in;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[i] * g)), a.cap_log2);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] *= f;
+    f = 1.f;
   }
-  f = 1.f;
   if (KIND != kPlain && a.lowered) {
-    if (KIND == kMarked && a.placed) {
-      source.distances([&](int i, float far) { s[i] = fmaf(-slope, fabsf(far), s[i]); });
-    } else {
-      const float far = (float)(token - base);
+    float far = (float)(token - base);
+    if (KIND != kMarked || !a.placed || source.in_order(far)) {
+      if (KIND == kMarked && __all(far >= 15.f)) {  // the row is behind them all
+        const float least = -slope * far;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = fmaf(-slope, fabsf(far - (float)i), s[i]);
+        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], f, fmaf(slope, (float)i, least));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], f, -slope * fabsf(far - (float)i));
+      }
+    } else {
+      source.distances([&](int i, float far) { s[i] = fmaf(s[i], f, -slope * fabsf(far)); });
     }
+    f = 1.f;
   }
   if (!masked) return;
+  if (!shaped) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] *= f;
+    f = 1.f;
+  }
   int rows = 0;
   if (KIND == kMarked && a.tagged) {
     rows = source.rows();
@@ -473,6 +489,8 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
     for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[g][n][i] = 0.f;
+  // A wave at the matrix pipe goes first: else the older of a SIMD's two runs ahead, and the younger ends alone.
+  __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int x = 0; x < D / 32; ++x)
 #pragma unroll
@@ -487,6 +505,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
         for (int n = 0; n < N; ++n) s[g][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes[n], row, s[g][n], 0, 0, 0);
       }
     }
+  __builtin_amdgcn_s_setprio(0);
   Marks m[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) m[n] = marks[n];
@@ -504,6 +523,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
     }
   half8 w[G][N][2];
   soften<D, G, N>(z, s, f, p, w);
+  __builtin_amdgcn_s_setprio(1);
   __builtin_amdgcn_sched_barrier(0);  // (V's codes are turned as they are needed: all at once they take 64 registers more)
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -517,6 +537,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
         for (int g = 0; g < G; ++g) z[g].o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, w[g][n][y], z[g].o[x], 0, 0, 0);
       }
   }
+  __builtin_amdgcn_s_setprio(0);
   behind();
 }
 
@@ -631,20 +652,26 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
               float4v{z[g].o[x][4 * y], z[g].o[x][4 * y + 1], z[g].o[x][4 * y + 2], z[g].o[x][4 * y + 3]};
     }
     __syncthreads();
-    const int rows = min(u.n_rows - g * kRows, kRows);
-    for (int j = threadIdx.x; j < rows * (D / 4); j += 256) {
-      const int i = j / (D / 4), d = j % (D / 4) * 4;
-      float m = -FLT_MAX, all = 0.f;
+    // a thread takes the same four dims of several rows; what lies in LDS is read for rows that there are not, too
+    constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;
+    const int i0 = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4, rows = min(u.n_rows - g * kRows, kRows);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) m = fmaxf(m, s_ml[w * kRows + i][0]);
+    for (int j = 0; j < kRows / kAtOnce; ++j) {
+      const int i = i0 + j * kAtOnce;
+      float2v ml[4];
+      float4v part[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) ml[w] = s_ml[w * kRows + i], part[w] = *(const float4v*)(s_o + (w * kRows + i) * kPitch<D> + d);
+      const float m = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
+      float all = 0.f;
       float4v o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float2v ml = s_ml[w * kRows + i];
-        const float f = __builtin_amdgcn_exp2f(ml[0] - m);
-        all = fmaf(ml[1], f, all);
-        o += *(const float4v*)(s_o + (w * kRows + i) * kPitch<D> + d) * f;
+        const float f = __builtin_amdgcn_exp2f(ml[w][0] - m);
+        all = fmaf(ml[w][1], f, all);
+        o += part[w] * f;
       }
+      if (i >= rows) continue;
       if (u.part < 0) {
         const int64_t to = row_address(a, u.s0 + g * kRows + i, head);
         store_out(a, to * D + d, o * inverse_of(all));

@@ -14,6 +14,7 @@ struct PlanArgs {
   Geometry g;
   int n_requests, n_rows;
   int wide;       // requests with more than kManyRows stacked rows take tiles of 64
+  int whole;      // no tile is split
   int capacity;   // units that the chip takes at once
   int max_units, max_tiles, max_part_rows;
   const int *length, *row_offsets, *prefix_len, *slot, *table;
@@ -65,11 +66,30 @@ __device__ inline Unit tile_of(const PlanArgs& a, int r, const RequestTiles& q, 
 
 __device__ inline int chunks_of(int tokens) { return (tokens + kChunkTokens - 1) / kChunkTokens; }
 
-__device__ inline int parts_of(int tokens, int chunk) { return max(1, (tokens + chunk - 1) / chunk); }
+// What a tile's tokens cost, in halves of kChunkTokens plain ones: behind the prefix of a request with few rows, where every token's tag has to be looked
+// at, three for two.
+struct Cost {
+  int chunks, cheap;  // the first `cheap` of them plain
+  __device__ int all() const { return 3 * chunks - cheap; }
+  __device__ int chunk_at(int64_t cost) const { return (int)(cost <= 2 * cheap ? cost / 2 : cheap + (cost - 2 * cheap) / 3); }
+};
 
-__device__ inline Unit part_of(Unit u, int k, int parts, int chunk, int row_at) {
-  const int hi = u.hi;
-  u.lo = k * chunk, u.hi = parts > 1 ? min(hi, (k + 1) * chunk) : hi, u.part = parts > 1 ? row_at + k * u.n_rows : -1;
+__device__ inline Cost cost_of(const Unit& u, const RequestTiles& q) {
+  const int chunks = chunks_of(u.hi);
+  return Cost{chunks, q.prefix > 0 && q.n <= kTaggedRows ? min(q.prefix / kChunkTokens, chunks) : chunks};
+}
+
+// Into how many pieces of at most `most` (in Cost's units) a tile goes.
+__device__ inline int parts_of(const PlanArgs& a, int cost, int most) {
+  return a.whole ? 1 : max(1, (cost + most - 1) / most);
+}
+
+__device__ inline Unit part_of(Unit u, const Cost& c, int k, int parts, int row_at) {
+  if (parts == 1) return u.lo = 0, u.part = -1, u;
+  const int64_t all = c.all();
+  u.lo = c.chunk_at(all * k / parts) * kChunkTokens;
+  if (k + 1 < parts) u.hi = c.chunk_at(all * (k + 1) / parts) * kChunkTokens;
+  u.part = row_at + k * u.n_rows;
   return u;
 }
 
@@ -86,7 +106,7 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
   __shared__ int s_tmp[NT / 64 + 1], s_upto[NT], s_chunks[NT];
   __shared__ RequestTiles s_request[NT];
   __shared__ Unit s_unit;
-  const int tid = threadIdx.x, unit = blockIdx.x;
+  const int tid = threadIdx.x;
   int mine = 0, n_tiles, work;
   if (tid <= a.n_requests) {
     s_request[tid] = request_tiles(a, tid);
@@ -98,15 +118,17 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
   __syncthreads();
   n_tiles = min(n_tiles, a.max_tiles);
   Unit u{};
+  Cost cost{};
   if (tid < n_tiles) {
     const int r = min(count_le(s_upto, a.n_requests + 1, tid), a.n_requests);
     const RequestTiles q = s_request[r];
     u = tile_of(a, r, q, tid - (s_upto[r] - q.n_tiles));
+    cost = cost_of(u, q);
   }
-  const int own = tid < n_tiles ? chunks_of(u.hi) : 0;
+  const int own = cost.all();
   s_chunks[tid] = own;
   group_scan<NT>(own, s_tmp, work);
-  // Chunks of this many times 128 tokens.  With one remainder per tile that makes at most `capacity` units while there are few tiles; from
+  // Chunks of this cost.  With one remainder per tile that makes at most `capacity` units while there are few tiles; from
   // half as many tiles on, chunks are twice the mean load.
   const int room = max(max(a.capacity - n_tiles, a.capacity / 2), 1);
   int chunk = max(1, (work + room - 1) / room);
@@ -123,18 +145,20 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
     __syncthreads();
     chunk = min(chunk, s_tmp[NT / 64]);
   }
-  chunk = max(min(chunk, kMostTokens / kChunkTokens) * kChunkTokens, kLeastTokens);
-  const int parts = tid < n_tiles ? parts_of(u.hi, chunk) : 0;
-  int all;
-  const int at = group_scan<NT>(parts, s_tmp, all) - parts;
+  chunk = max(chunk, 2 * kLeastTokens / kChunkTokens);
+  const int parts = tid < n_tiles ? parts_of(a, own, chunk) : 0;
+  int n_units, all;
+  const int at = group_scan<NT>(parts, s_tmp, n_units) - parts;
   const int rows = parts > 1 ? parts * u.n_rows : 0;
   const int row_at = group_scan<NT>(rows, s_tmp, all) - rows;
+  // the second half of what runs at once stands in reverse
+  const int half = a.capacity / 2, unit = n_units <= a.capacity && (int)blockIdx.x >= half && (int)blockIdx.x < n_units ? half + n_units - 1 - (int)blockIdx.x : blockIdx.x;
   const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;  // (the host's bounds hold: see pasta_kv8.hip)
-  if (unit >= at && unit < at + parts && fits) s_unit = part_of(u, unit - at, parts, chunk, row_at);
-  if (unit == 0 && tid < a.max_tiles) a.tiles[tid] = Tile{u.s0, u.n_rows, row_at, tid < n_tiles && fits ? parts : 0};
+  if (unit >= at && unit < at + parts && fits) s_unit = part_of(u, cost, unit - at, parts, row_at);
+  if (blockIdx.x == 0 && tid < a.max_tiles) a.tiles[tid] = Tile{u.s0, u.n_rows, row_at, tid < n_tiles && fits ? parts : 0};
   __syncthreads();
-  if (tid == 0) a.units[unit] = s_unit;
-  if (tid < kUnitBlocks && s_unit.n_rows) list_blocks(a, s_unit, unit, tid);
+  if (tid == 0) a.units[blockIdx.x] = s_unit;
+  if (tid < kUnitBlocks && s_unit.n_rows) list_blocks(a, s_unit, blockIdx.x, tid);
 }
 
 // Any number of them, one work-group, NT at a time; the units' blocks follow in a launch of their own.
@@ -159,13 +183,14 @@ __global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
     const RequestTiles q = request_tiles(a, r);
     return tile_of(a, r, q, j - (a.w_tiles[r] - q.n_tiles));
   };
+  auto plain = [](const Unit& u) { return Cost{chunks_of(u.hi), chunks_of(u.hi)}; };
   for (int j0 = 0; j0 < n_tiles; j0 += NT) {
     int all;
     group_scan<NT>(j0 + tid < n_tiles ? chunks_of(tile(j0 + tid).hi) : 0, s_tmp, all);
     work += all;
   }
   const int room = max(max(a.capacity - n_tiles, a.capacity / 2), 1);
-  const int chunk = max((int)min((work + room - 1) / room, (int64_t)(kMostTokens / kChunkTokens)) * kChunkTokens, kLeastTokens);
+  const int chunk = max((int)min((2 * work + room - 1) / room, (int64_t)(2 * kMostTokens / kChunkTokens)), 2 * kLeastTokens / kChunkTokens);
   int n_units = 0, n_part_rows = 0;
   for (int j0 = 0; j0 < n_tiles; j0 += NT) {
     const int j = j0 + tid;
@@ -173,14 +198,14 @@ __global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
     int parts = 0, all, all_rows;
     if (j < n_tiles) {
       u = tile(j);
-      parts = parts_of(u.hi, chunk);
+      parts = parts_of(a, plain(u).all(), chunk);
     }
     const int at = n_units + group_scan<NT>(parts, s_tmp, all) - parts;
     const int rows = parts > 1 ? parts * u.n_rows : 0;
     const int row_at = n_part_rows + group_scan<NT>(rows, s_tmp, all_rows) - rows;
     if (j < n_tiles) {
       const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;
-      for (int k = 0; k < parts && fits; ++k) a.units[at + k] = part_of(u, k, parts, chunk, row_at);
+      for (int k = 0; k < parts && fits; ++k) a.units[at + k] = part_of(u, plain(u), k, parts, row_at);
       a.tiles[j] = Tile{u.s0, u.n_rows, row_at, fits ? parts : 0};
     }
     n_units += all;

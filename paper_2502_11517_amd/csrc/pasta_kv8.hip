@@ -36,7 +36,7 @@ struct pasta_kv8 {
   float* part_acc = nullptr;
   // the last plan
   bool planned = false;
-  int plan_rows = 0, plan_wide = 0;
+  int plan_rows = 0, plan_wide = 0, plan_whole = 0;
   Bounds plan{};
 };
 
@@ -234,9 +234,11 @@ extern "C" int32_t pasta_kv8_plan(pasta_kv8* h, const pasta_kv8_plan_args* a) {
   if (a->n_rows == 0) return PASTA_OK;
   const int64_t most = a->max_request_rows < a->n_rows ? a->max_request_rows : a->n_rows;
   h->plan_wide = most * h->g.G > k8::kManyRows;
+  // where every tile is that short, splitting it costs more (a launch, partial rows) than it saves
+  h->plan_whole = (int64_t)c.pages_per_request * c.page_tokens <= (h->plan_wide ? k8::kLeastTokens : k8::kWholeTokens);
   h->plan = bounds(c, a->n_rows, a->n_requests, h->plan_wide);
   k8::PlanArgs k{};
-  k.g = h->g, k.n_requests = a->n_requests, k.n_rows = a->n_rows, k.wide = h->plan_wide, k.capacity = (int)h->plan.capacity;
+  k.g = h->g, k.n_requests = a->n_requests, k.n_rows = a->n_rows, k.wide = h->plan_wide, k.whole = h->plan_whole, k.capacity = (int)h->plan.capacity;
   k.max_units = (int)h->plan.units, k.max_tiles = (int)h->plan.tiles, k.max_part_rows = (int)h->plan.part_rows;
   k.length = a->n_requests ? a->length : a->row_offsets;  // (read, not used, without a request)
   k.row_offsets = a->row_offsets, k.prefix_len = a->prefix_len, k.slot = a->slot;
@@ -312,7 +314,7 @@ extern "C" int32_t pasta_kv8_attend(pasta_kv8* h, const pasta_kv8_attend_args* a
     c.head_dim == 128 ? launch_attend<k8::kE4m3, 128>(k, many, groups, s) : launch_attend<k8::kE4m3, 64>(k, many, groups, s);
   else
     c.head_dim == 128 ? launch_attend<k8::kInt8, 128>(k, many, groups, s) : launch_attend<k8::kInt8, 64>(k, many, groups, s);
-  if ((int64_t)c.pages_per_request * c.page_tokens > k8::kLeastTokens) {  // no tile is split otherwise
+  if (!h->plan_whole) {
     const int64_t tiles = h->plan.tiles * c.n_kv_heads;
     int64_t split = (2048 + tiles - 1) / tiles;  // work-groups to a tile: rows, one by one where there are so few tiles
     if (split > h->plan.merge_rows) split = h->plan.merge_rows;
