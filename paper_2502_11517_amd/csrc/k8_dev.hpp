@@ -24,6 +24,7 @@ enum { kE4m3 = 0, kInt8 = 1 };
 enum { kF32 = 0, kBf16 = 1, kF16 = 2 };
 
 using half2v = __attribute__((ext_vector_type(2))) _Float16;
+using int2v = __attribute__((ext_vector_type(2))) int;
 using half8 = __attribute__((ext_vector_type(8))) _Float16;
 using float2v = __attribute__((ext_vector_type(2))) float;
 using float4v = __attribute__((ext_vector_type(4))) float;
@@ -126,36 +127,47 @@ __device__ inline uint32_t wave_max(uint32_t x) {
   return max(b[0], b[1]);
 }
 
-// Sum over the lanes below and including this one.
+// Sum over the lanes below and including this one: within rows of 16 lanes, then each row's end into the next row, then half into half.
 __device__ inline int wave_scan(int x) {
-  const int lane = threadIdx.x & 63;
-  for (int d = 1; d < 64; d <<= 1) {
-    int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15, rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31, rows 2 and 3
   return x;
 }
 
-// Inclusive sum over the work-group and its total; `tmp` holds a word per wave.  Every thread calls it; it ends with a barrier.
+// Inclusive sums over the work-group and their totals; `tmp` holds a pair per wave.  Every thread calls it; it ends with a barrier.
 template <int NT>
-__device__ inline int group_scan(int x, int* tmp, int& total) {
+__device__ inline int2v group_scan(int2v x, int2v* tmp, int2v& total) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  x = wave_scan(x);
+  x[0] = wave_scan(x[0]), x[1] = wave_scan(x[1]);
   if constexpr (NT == 64) {
-    total = __shfl(x, 63);
+    total = int2v{__builtin_amdgcn_readlane(x[0], 63), __builtin_amdgcn_readlane(x[1], 63)};
+    __syncthreads();
     return x;
   }
   if (lane == 63) tmp[wave] = x;
   __syncthreads();
-  int before = 0, all = 0;
+  int2v before{0, 0}, all{0, 0};
+#pragma unroll
   for (int w = 0; w < NT / 64; ++w) {
-    int t = tmp[w];
+    const int2v t = tmp[w];
     if (w < wave) before += t;
     all += t;
   }
   __syncthreads();
   total = all;
   return x + before;
+}
+
+template <int NT>
+__device__ inline int group_scan(int x, int2v* tmp, int& total) {
+  int2v all;
+  const int2v y = group_scan<NT>(int2v{x, 0}, tmp, all);
+  total = all[0];
+  return y[0];
 }
 
 // How many of v[0 .. n) are <= x; v ascending.

@@ -103,7 +103,8 @@ __device__ inline void list_blocks(const PlanArgs& a, const Unit& u, int unit, i
 // writes down the unit of its own number, so that the whole plan is one launch whose way is no longer than one page's.
 template <int NT>
 __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
-  __shared__ int s_tmp[NT / 64 + 1], s_upto[NT], s_chunks[NT];
+  __shared__ int2v s_tmp[NT / 64];
+  __shared__ int s_upto[NT], s_chunks[NT], s_chunk;
   __shared__ RequestTiles s_request[NT];
   __shared__ Unit s_unit;
   const int tid = threadIdx.x;
@@ -140,17 +141,17 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
       int units = 0;
       for (int j = 0; j < n_tiles; ++j) units += max(1, (s_chunks[j] + c - 1) / c);
       const uint64_t fits = __ballot(units <= a.capacity);
-      if (tid == 0) s_tmp[NT / 64] = fits ? least + __builtin_ctzll(fits) : chunk;
+      if (tid == 0) s_chunk = fits ? least + __builtin_ctzll(fits) : chunk;
     }
     __syncthreads();
-    chunk = min(chunk, s_tmp[NT / 64]);
+    chunk = min(chunk, s_chunk);
   }
   chunk = max(chunk, 2 * kLeastTokens / kChunkTokens);
   const int parts = tid < n_tiles ? parts_of(a, own, chunk) : 0;
-  int n_units, all;
-  const int at = group_scan<NT>(parts, s_tmp, n_units) - parts;
   const int rows = parts > 1 ? parts * u.n_rows : 0;
-  const int row_at = group_scan<NT>(rows, s_tmp, all) - rows;
+  int2v all;
+  const int2v upto_here = group_scan<NT>(int2v{parts, rows}, s_tmp, all);
+  const int at = upto_here[0] - parts, row_at = upto_here[1] - rows, n_units = all[0];
   // the second half of what runs at once stands in reverse
   const int half = a.capacity / 2, unit = n_units <= a.capacity && (int)blockIdx.x >= half && (int)blockIdx.x < n_units ? half + n_units - 1 - (int)blockIdx.x : blockIdx.x;
   const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;  // (the host's bounds hold: see pasta_kv8.hip)
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
 // Any number of them, one work-group, NT at a time; the units' blocks follow in a launch of their own.
 template <int NT>
 __global__ __launch_bounds__(NT) void k8_plan_long(PlanArgs a) {
-  __shared__ int s_tmp[NT / 64];
+  __shared__ int2v s_tmp[NT / 64];
   const int tid = threadIdx.x;
   int n_tiles = 0;
   int64_t work = 0;

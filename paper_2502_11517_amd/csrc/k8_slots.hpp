@@ -60,7 +60,8 @@ __device__ inline void give_slot(const SlotsArgs& a, int i, int page, int p) {
 // At most NT requests.
 template <int NT>
 __global__ __launch_bounds__(NT) void k8_slots(SlotsArgs a) {
-  __shared__ int s_tmp[NT / 64], s_next[NT], s_first[NT], s_kept[NT], s_old[NT], s_take[NT], s_freed[NT], s_page[NT];
+  __shared__ int2v s_tmp[NT / 64];
+  __shared__ int s_next[NT], s_first[NT], s_kept[NT], s_old[NT], s_take[NT], s_freed[NT], s_page[NT];
   const int tid = threadIdx.x;
   const int have = min(max(*a.free_count, 0), a.g.n_pages);
   RequestRows q{};
@@ -70,9 +71,10 @@ __global__ __launch_bounds__(NT) void k8_slots(SlotsArgs a) {
     first = max(a.row_offsets[tid], 0), next = a.row_offsets[tid + 1];
   }
   const int back = q.fits ? max(q.old_pages - q.new_pages, 0) : 0, need = q.fits ? max(q.new_pages - q.old_pages, 0) : 0;
-  int freed, asked, taken;
-  const int back_upto = group_scan<NT>(back, s_tmp, freed);
-  const int need_upto = group_scan<NT>(need, s_tmp, asked);  // (at most n_requests * table_width pages)
+  int2v all;
+  int taken;
+  const int2v upto = group_scan<NT>(int2v{back, need}, s_tmp, all);  // (at most n_requests * table_width pages)
+  const int back_upto = upto[0], need_upto = upto[1], freed = all[0];
   const int top = min(have + freed, a.g.n_pages);
   const bool served = q.fits && (need == 0 || need_upto <= top);
   s_next[tid] = next, s_first[tid] = first, s_kept[tid] = q.kept, s_old[tid] = q.old_pages, s_take[tid] = served ? need_upto - need : -1;
@@ -133,7 +135,8 @@ __device__ inline void place_row(const SlotsArgs& a, int i) {
 // Any number of requests, NT at a time, or lengths in place; one work-group.
 template <int NT>
 __global__ __launch_bounds__(NT) void k8_slots_long(SlotsArgs a) {
-  __shared__ int s_tmp[NT / 64], s_first[NT], s_page[NT];
+  __shared__ int2v s_tmp[NT / 64];
+  __shared__ int s_first[NT], s_page[NT];
   const int tid = threadIdx.x;
   const int have = min(max(*a.free_count, 0), a.g.n_pages);
   // pages that go back
