@@ -713,19 +713,20 @@ __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
   }
 }
 
-// Joins the partial rows of the tiles whose tokens are split.  D / 4 lanes hold a row, four dims apiece; the 1024 / D such groups of a
-// work-group take a row each where there are few parts, else share a row's parts, two or all of them.
+// Joins the partial rows of the tiles whose tokens are split.  D / 4 lanes hold a row, four dims apiece; of the 1024 / D such groups of a
+// work-group as many share a row's parts as leave each four of them, or all.  A group asks for its parts at once and goes by their own maximum, so
+// that nothing waits for a maximum over all; the groups' results are joined in LDS.
 template <int D>
 __global__ __launch_bounds__(256) void k8_merge(AttendArgs a) {
-  constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAtOnce = 4;
   __shared__ float4v s_o[kGroups][kLanes];
-  __shared__ float s_l[kGroups];
+  __shared__ float2v s_ml[kGroups];
   const int t = blockIdx.x / a.g.Hkv, head = blockIdx.x % a.g.Hkv;
   const Tile tile = a.tiles[t];
   if (tile.n_parts < 2) return;
   const int group = threadIdx.x / kLanes, d = threadIdx.x % kLanes;
-  const int share = tile.n_parts <= 8 ? 1 : tile.n_parts <= 32 ? kGroups / 2 : kGroups;  // groups to a row
-  const int rows = kGroups / share;                                                      // rows at a time
+  const int share = tile.n_parts <= kAtOnce ? 1 : tile.n_parts <= 2 * kAtOnce ? 2 : tile.n_parts <= 4 * kAtOnce ? 4 : kGroups;  // groups to a row
+  const int rows = kGroups / share;                                                                                         // rows at a time
   const int64_t step = (int64_t)tile.n_rows * a.g.Hkv;
   for (int row0 = blockIdx.y * rows; row0 < tile.n_rows; row0 += gridDim.y * rows) {
     const int row = row0 + group / share;
@@ -733,29 +734,43 @@ __global__ __launch_bounds__(256) void k8_merge(AttendArgs a) {
     const int64_t at = (int64_t)(tile.part + (real ? row : 0)) * a.g.Hkv + head;
     const float2v* ml = a.part_ml + at;
     const float* acc = a.part_acc + at * D + 4 * d;
-    float m = -FLT_MAX;
-    if (tile.n_parts <= 8) {
-      for (int k = 0; k < tile.n_parts; ++k) m = fmaxf(m, ml[k * step][0]);
-    } else {
-      for (int k = d; k < tile.n_parts; k += kLanes) m = fmaxf(m, ml[k * step][0]);
-      for (int x = kLanes / 2; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-    }
+    float m = -FLT_MAX, l = 0.f;
     float4v o{0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-#pragma unroll 4
-    for (int k = group % share; k < tile.n_parts; k += share) {
-      const float2v x = ml[k * step];
-      const float f = __builtin_amdgcn_exp2f(x[0] - m);
-      l = fmaf(x[1], f, l);
-      o += *(const float4v*)(acc + k * step * D) * f;
+    for (int k0 = group % share; k0 < tile.n_parts; k0 += kAtOnce * share) {
+      float2v x[kAtOnce];
+      float4v y[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int64_t k = min(k0 + i * share, tile.n_parts - 1);
+        x[i] = ml[k * step], y[i] = *(const float4v*)(acc + k * step * D);
+      }
+      const float before = m;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) m = fmaxf(m, x[i][0]);
+      const float f = __builtin_amdgcn_exp2f(before - m);
+      l *= f, o *= f;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        if (k0 + i * share >= tile.n_parts) continue;
+        const float f = __builtin_amdgcn_exp2f(x[i][0] - m);
+        l = fmaf(x[i][1], f, l);
+        o += y[i] * f;
+      }
     }
     if (share > 1) {
       __syncthreads();
       s_o[group][d] = o;
-      if (d == 0) s_l[group] = l;
+      if (d == 0) s_ml[group] = float2v{m, l};
       __syncthreads();
       if (group % share) continue;
-      for (int x = 1; x < share; ++x) o += s_o[group + x][d], l += s_l[group + x];
+      for (int x = 1; x < share; ++x) m = fmaxf(m, s_ml[group + x][0]);
+      l = 0.f, o = float4v{0.f, 0.f, 0.f, 0.f};
+      for (int x = 0; x < share; ++x) {
+        const float2v y = s_ml[group + x];
+        const float f = __builtin_amdgcn_exp2f(y[0] - m);
+        l = fmaf(y[1], f, l);
+        o += s_o[group + x][d] * f;
+      }
     }
     if (!real) continue;
     const int64_t to = row_address(a, tile.s0 + row, head);
