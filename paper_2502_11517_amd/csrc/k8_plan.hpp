@@ -104,7 +104,7 @@ __device__ inline void list_blocks(const PlanArgs& a, const Unit& u, int unit, i
 template <int NT>
 __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
   __shared__ int2v s_tmp[NT / 64];
-  __shared__ int s_upto[NT], s_chunks[NT], s_chunk;
+  __shared__ int s_upto[NT], s_chunks[NT], s_chunk[2];
   __shared__ RequestTiles s_request[NT];
   __shared__ Unit s_unit;
   const int tid = threadIdx.x;
@@ -129,24 +129,22 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
   const int own = cost.all();
   s_chunks[tid] = own;
   group_scan<NT>(own, s_tmp, work);
-  // Chunks of this cost.  With one remainder per tile that makes at most `capacity` units while there are few tiles; from
-  // half as many tiles on, chunks are twice the mean load.
-  const int room = max(max(a.capacity - n_tiles, a.capacity / 2), 1);
-  int chunk = max(1, (work + room - 1) / room);
-  if (n_tiles > 1 && n_tiles < a.capacity) {
-    // the least that does: 64 candidates from the one without remainders on, looked at by a lane each
-    const int least = max(1, (work + a.capacity - 1) / a.capacity);
-    if (tid < 64) {
-      const int c = least + tid;
-      int units = 0;
+  // The least chunk that makes at most `capacity` units, and the least that makes half as many: 64 candidates for each from the one without
+  // remainders on, a lane for each.  Else one that does in any case: with one remainder per tile while there are few tiles; from half as many
+  // tiles on, twice the mean load.
+  if (tid < 128) {
+    const int most = max(a.capacity >> (tid >> 6), 1), room = max(max(most - n_tiles, most / 2), 1);
+    const int least = max(1, (work + most - 1) / most), c = least + (tid & 63);
+    int units = n_tiles > most ? INT_MAX : 0;
+    if (n_tiles <= most && n_tiles > 1)
       for (int j = 0; j < n_tiles; ++j) units += max(1, (s_chunks[j] + c - 1) / c);
-      const uint64_t fits = __ballot(units <= a.capacity);
-      if (tid == 0) s_chunk = fits ? least + __builtin_ctzll(fits) : chunk;
-    }
-    __syncthreads();
-    chunk = min(chunk, s_chunk);
+    const uint64_t fits = __ballot(units <= most);
+    const int any = max(1, (work + room - 1) / room);
+    if ((tid & 63) == 0) s_chunk[tid >> 6] = min(any, fits ? least + __builtin_ctzll(fits) : any);
   }
-  chunk = max(chunk, 2 * kLeastTokens / kChunkTokens);
+  __syncthreads();
+  const bool alone = 2 * n_tiles <= a.capacity && s_chunk[1] * (kChunkTokens / 2) <= kAloneTokens;
+  const int chunk = alone ? max(s_chunk[1], 2 * kLeastAlone / kChunkTokens) : max(s_chunk[0], 2 * kLeastTokens / kChunkTokens);
   const int parts = tid < n_tiles ? parts_of(a, own, chunk) : 0;
   const int rows = parts > 1 ? parts * u.n_rows : 0;
   int2v all;

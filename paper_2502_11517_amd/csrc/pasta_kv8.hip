@@ -2,6 +2,7 @@
 // No call here depends on what a device array holds: grids go by the sizes that the caller gives, work-groups that find nothing to do end.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -64,14 +65,17 @@ int32_t check(const pasta_kv8_config* c) {
 }
 
 // What a plan over n_rows rows of n_requests requests can come to (k8_plan.hpp: with R tiles, at most max(capacity, capacity / 2 + R, 1 + R)
-// units; a tile is split only into pieces of more than half a chunk on the mean, so that at most twice max(capacity, 1) of them are partial).
-Bounds bounds(const pasta_kv8_config& c, int64_t n_rows, int64_t n_requests, bool wide) {
+// units, which a launch goes over one by one: 256 work-groups that find nothing cost 1.5 us; a tile is split only into pieces of more than half a chunk
+// on the mean, so that at most twice max(capacity, 1) of them are partial).
+Bounds bounds(const pasta_kv8_config& c, int64_t n_rows, int64_t n_requests, bool wide, bool whole) {
   const int64_t G = c.n_q_heads / c.n_kv_heads, stacked = n_rows * G;
   Bounds b;
   b.capacity = kUnitsAtOnce / c.n_kv_heads;
-  b.tiles = (stacked + k8::kRows - 1) / k8::kRows + n_requests + 1;
-  if (b.tiles > n_rows * G) b.tiles = n_rows * G;  // a tile has a row
-  b.units = b.capacity + b.tiles + 1;
+  b.tiles = (stacked + (n_requests + 1) * (k8::kRows - 1)) / k8::kRows;  // of requests, and of rows that none has, each rounded up
+  if (b.tiles > stacked) b.tiles = stacked;
+  const int64_t chunks = ((int64_t)c.pages_per_request * c.page_tokens + k8::kChunkTokens - 1) / k8::kChunkTokens;
+  b.units = std::min(std::max(b.capacity, std::max(b.capacity / 2, (int64_t)1) + b.tiles), b.tiles * ((3 * chunks + 3) / 4));
+  if (whole) b.units = b.tiles;
   int64_t rows = wide ? k8::kWideRows : k8::kRows;
   b.merge_rows = rows < stacked ? rows : stacked;
   b.part_rows = 2 * b.capacity * b.merge_rows;
@@ -79,7 +83,7 @@ Bounds bounds(const pasta_kv8_config& c, int64_t n_rows, int64_t n_requests, boo
 }
 
 uint64_t lay_out(const pasta_kv8_config& c, pasta_kv8* h) {
-  const Bounds b = bounds(c, c.max_rows, c.max_requests, (int64_t)c.max_rows * (c.n_q_heads / c.n_kv_heads) > k8::kManyRows);
+  const Bounds b = bounds(c, c.max_rows, c.max_requests, (int64_t)c.max_rows * (c.n_q_heads / c.n_kv_heads) > k8::kManyRows, false);
   uint64_t at = 0;
   auto take = [&](auto*& p, uint64_t n) {
     p = reinterpret_cast<std::remove_reference_t<decltype(p)>>((uint8_t*)c.workspace + at);
@@ -235,8 +239,8 @@ extern "C" int32_t pasta_kv8_plan(pasta_kv8* h, const pasta_kv8_plan_args* a) {
   const int64_t most = a->max_request_rows < a->n_rows ? a->max_request_rows : a->n_rows;
   h->plan_wide = most * h->g.G > k8::kManyRows;
   // where every tile is that short, splitting it costs more (a launch, partial rows) than it saves
-  h->plan_whole = (int64_t)c.pages_per_request * c.page_tokens <= (h->plan_wide ? k8::kLeastTokens : k8::kWholeTokens);
-  h->plan = bounds(c, a->n_rows, a->n_requests, h->plan_wide);
+  h->plan_whole = (int64_t)c.pages_per_request * c.page_tokens <= (h->plan_wide ? k8::kWholeWide : k8::kWholeTokens);
+  h->plan = bounds(c, a->n_rows, a->n_requests, h->plan_wide, h->plan_whole);
   k8::PlanArgs k{};
   k.g = h->g, k.n_requests = a->n_requests, k.n_rows = a->n_rows, k.wide = h->plan_wide, k.whole = h->plan_whole, k.capacity = (int)h->plan.capacity;
   k.max_units = (int)h->plan.units, k.max_tiles = (int)h->plan.tiles, k.max_part_rows = (int)h->plan.part_rows;
