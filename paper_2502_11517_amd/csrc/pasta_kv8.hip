@@ -72,6 +72,8 @@ Bounds bounds(const pasta_kv8_config& c, int64_t n_rows, int64_t n_requests, boo
   Bounds b;
   b.capacity = kUnitsAtOnce / c.n_kv_heads;
   b.tiles = (stacked + (n_requests + 1) * (k8::kRows - 1)) / k8::kRows;  // of requests, and of rows that none has, each rounded up
+  // (with tiles of 64 a request has as many as that again rounds up to, or, being small, at most two more)
+  if (wide) b.tiles = std::min(b.tiles, (stacked + (n_requests + 1) * (k8::kWideRows - 1)) / k8::kWideRows + 2 * (n_requests + 1));
   if (b.tiles > stacked) b.tiles = stacked;
   const int64_t chunks = ((int64_t)c.pages_per_request * c.page_tokens + k8::kChunkTokens - 1) / k8::kChunkTokens;
   b.units = std::min(std::max(b.capacity, std::max(b.capacity / 2, (int64_t)1) + b.tiles), b.tiles * ((3 * chunks + 3) / 4));
@@ -83,7 +85,8 @@ Bounds bounds(const pasta_kv8_config& c, int64_t n_rows, int64_t n_requests, boo
 }
 
 uint64_t lay_out(const pasta_kv8_config& c, pasta_kv8* h) {
-  const Bounds b = bounds(c, c.max_rows, c.max_requests, (int64_t)c.max_rows * (c.n_q_heads / c.n_kv_heads) > k8::kManyRows, false);
+  Bounds b = bounds(c, c.max_rows, c.max_requests, false, false);
+  if ((int64_t)c.max_rows * (c.n_q_heads / c.n_kv_heads) > k8::kManyRows) b.part_rows = bounds(c, c.max_rows, c.max_requests, true, false).part_rows;
   uint64_t at = 0;
   auto take = [&](auto*& p, uint64_t n) {
     p = reinterpret_cast<std::remove_reference_t<decltype(p)>>((uint8_t*)c.workspace + at);
