@@ -200,18 +200,18 @@ __global__ __launch_bounds__(256) void k8_append(AppendArgs a) {
   if (head >= a.g.Hkv) return;
   const int n_slots = a.g.n_pages << a.g.page_shift;
   const int first = blockIdx.x * a.group, last = min(first + a.group, a.n_rows);
+  // lane k: the slot of row first + k - 1; a run that begins within the group ends within 16 more rows
+  const int row = first + lane - 1;
+  const int mine = lane <= a.group + kBlock && row >= 0 && row < a.n_rows ? a.slot[row] : -1;
   int i = first;
   while (i < last) {
-    // lane k: the slot of row i + k - 1
-    const int at = i + lane - 1;
-    const int mine = lane <= kBlock && at >= 0 && at < a.n_rows ? a.slot[at] : -1;
-    const int prev = __builtin_amdgcn_readlane(mine, 0), slot = __builtin_amdgcn_readlane(mine, 1);
+    const int at = i - first + 1, prev = __builtin_amdgcn_readlane(mine, at - 1), slot = __builtin_amdgcn_readlane(mine, at);
     if (slot < 0 || slot >= n_slots) {
       ++i;
       continue;
     }
-    const bool goes_on = lane >= 1 && lane <= kBlock && mine == slot + lane - 1 && (mine >> 4) == (slot >> 4);
-    const int n = __builtin_ctzll(~(__ballot(goes_on) >> 1));
+    const bool goes_on = lane >= at && mine == slot + lane - at && (mine >> 4) == (slot >> 4);
+    const int n = __builtin_ctzll(~(__ballot(goes_on) >> at));
     if (!(prev >= 0 && slot == prev + 1 && (slot & 15))) {  // the run begins here
       const int page = slot >> a.g.page_shift, b = (slot & (a.g.page_tokens - 1)) >> 4;
       const int64_t block = ((int64_t)page * a.g.Hkv + head) * a.g.blocks_per_page + b;
