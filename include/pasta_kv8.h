@@ -164,7 +164,7 @@ int32_t pasta_kv8_append(pasta_kv8 *h, const pasta_kv8_append_args *a);
  * the step's own rows, which are a request's last n (length_out of pasta_kv8_slots).
  * slot (optional): a request whose first row has no slot was refused; its rows get
  * the result of a row that sees nothing.
-* Needs page_table and the workspace.  Errors: E_INVAL, E_CAPACITY, E_DEVICE,
+ * Needs page_table and the workspace.  Errors: E_INVAL, E_CAPACITY, E_DEVICE,
  * E_STATE.                                                                       */
 typedef struct {
   uint32_t struct_size, flags;    /* flags: 0 */
@@ -195,7 +195,8 @@ int32_t pasta_kv8_plan(pasta_kv8 *h, const pasta_kv8_plan_args *a);
  * have joined, prefix_len covers them and their tags are free again.
  *
  * Sums, maxima and the output are held in fp32, the softmax weights enter the
- * product with V as fp16.  Rows that no request has (behind
+ * product with V as fp16.  A block whose V scale is more than 2^60 below another's
+ * of the request adds its tokens to the sums, but nothing to out.  Rows that no request has (behind
  * row_offsets[n_requests]) get out = 0, lse = -inf.
  * Needs everything but free_pages; slot_tag with row_see, slot_position with
  * row_position.  n_rows is that of the last plan (E_STATE otherwise, or without one).

@@ -4,6 +4,10 @@
 // largest magnitude gives the scale, codes ahead of the run are rounded again if the scale grew, and a block begun by the run is
 // written whole.  Scales are powers of two, so x / scale is exact and a code is one rounding of its value.  Magnitudes are compared
 // as bits: what is not finite is then larger than everything finite.
+//
+// Bound by memory for prompts: 8192 rows of 8 heads of 128, bf16, 50 MB in 13.0 us, 3.9 TB/s (K's half alone 4.0; a large copy 4.9).  A step of eight
+// rows takes 3.0 us, its launch and two dependent reads (slots, then rows with scales and codes).  Loads that bypass the caches took 69 us instead of 77
+// where the rows came from HBM, and 14 instead of 11 where they were near, as behind the projection that wrote them: not taken.
 #pragma once
 #include "k8_dev.hpp"
 
@@ -153,7 +157,7 @@ __device__ inline void append_v(const AppendArgs& a, int row, int n, int offset,
   float x[kBlock][N];
   uint32_t amax = 0;
   // Places without a row get the nearest one's, which changes no maximum and is dropped below: loads under branches wait for one another (8192 rows of 8
-  // heads, a layer: 19 us with them).
+  // heads, a layer: 19 us with them, 13 without; a step of eight rows 4.0 and 3.3).
 #pragma unroll
   for (int t = 0; t < kBlock; ++t)
     load_row<IN, N>(a.v_new, ((int64_t)(row + min(max(t - offset, 0), n - 1)) * a.g.Hkv + head) * D + lane * N, x[t]);

@@ -18,6 +18,18 @@
 //   * the scores that a lane gets (16 tokens of one block, one row) are, as fp16, its operand of the second product.
 //
 // A work-group takes 32 or 64 stacked rows; its four waves split the tokens, each with codes of its own in registers, and meet once at the end.
+//
+// What bounds it (8 kv heads of 128; a layer):
+//   8 streams over 8k tokens, 21 MB        10.5 us: the ramp.  1.2 us to the first codes alone, 3.1 with the whole chip asking, 3.3 for the three pairs of a
+//                                          wave, 1.5 for the waves' meeting, 2.5 of launch; the bytes are 4.3 us at a large copy's 4.9 TB/s
+//   16 ragged requests, 95 MB              25.4 us, 3.8 TB/s: memory
+//   16 x 8 rows over 51k tokens, 100 MB    58 us: vector instructions, 21 a score (codes to fp16, exponentials, distances, tags); the four tiles of rows
+//                                          share codes through the L2 only, since two groups of rows with marks do not fit the registers
+//   2048 x 4 rows over 8k tokens, 309 GF   320 us, 965 TFLOP/s against 1190 of a large library product: vector instructions busy 63% of the time, matrix
+//                                          instructions 42%
+// Tried and not taken: eight waves to a work-group (8 streams over 8k 123 -> 133 us a pass; 128 registers would be needed for four waves to a SIMD, and spill),
+// one copy of Q's operands for all waves (a barrier; 1 to 3% more), touching the codes of the step after next ahead of their turn (4 to 7% more), three
+// waves to a SIMD with 64 dims (spills), no priority for waves at the matrix pipe (nested forks over 35k 4% more).
 #pragma once
 #include <float.h>
 
@@ -715,7 +727,9 @@ __global__ __launch_bounds__(256, 2) void k8_attend(AttendArgs a) {
 
 // Joins the partial rows of the tiles whose tokens are split.  D / 4 lanes hold a row, four dims apiece; of the 1024 / D such groups of a
 // work-group as many share a row's parts as leave each four of them, or all.  A group asks for its parts at once and goes by their own maximum, so
-// that nothing waits for a maximum over all; the groups' results are joined in LDS.
+// that nothing waits for a maximum over all; the groups' results are joined in LDS.  Bound by its launch and one way to memory: 3.8 us for 32 rows x 28
+// parts of 8 heads (3.8 MB), of which 2.5 are the launch.  Joining in k8_attend, by the last work-group to come, would need partial rows written past the
+// L2s of eight dies and one CU to read all parts of a tile.
 template <int D>
 __global__ __launch_bounds__(256) void k8_merge(AttendArgs a) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kAtOnce = 4;

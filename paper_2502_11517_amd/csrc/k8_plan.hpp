@@ -1,10 +1,15 @@
 // Split of the attention's work: which stacked rows of which request over which tokens, a unit per (rows, tokens), times Hkv.
 //
 // Rows come in tiles of 32, or, in requests with more than 128 stacked rows, of 64 (a wave then turns its codes once for two groups; with fewer rows,
-// fewer and longer pieces of the tokens are worth more: 128 rows over 49k tokens 60 us a layer in tiles of 32, 87 of 64).  Tokens are split so that
-// about as many work-groups run as the chip holds; a tile whose tokens are split leaves partial rows, which k8_merge joins.  A piece has at
-// least 384 tokens, if the tile has: 8 x 1 row over 8k tokens in pieces of at least 256 / 384 / 512 / 640 / 768 tokens took 142 / 124 / 128 / 138 / 147 us
-// over eight layers (shorter ones cost more partial rows than they save, longer ones leave CUs idle).
+// fewer and longer pieces of the tokens are worth more: 128 rows over 49k tokens 60 us a layer in tiles of 32, 87 of 64).  A tile's tokens go in even
+// pieces, and what they leave, partial rows, k8_merge joins.  How long pieces are:
+//   * One work-group a CU where pieces of up to 1024 tokens do with that, no shorter than 256.  Two on a CU take turns at its SIMDs and gain a tenth; 328 of
+//     them take as long as 512 would.  Eight rows over 10k tokens in 224 / 328 pieces: 14.2 / 17.5 us a layer; 22 rows over 30k 134 / 148 us a pass.
+//   * Else two, in pieces no shorter than 384 tokens.  The older one of a SIMD's two waves runs ahead, so the second half of the list stands in reverse:
+//     a CU that starts with a dear piece (behind the prefix, where tags are looked at) gets a plain one with it.
+//   * Tables that hold at most 768 tokens (512 with tiles of 64) are not split, which saves the launch of k8_merge: 0.6 us a layer less for 500 tokens; 1200
+//     would take 2.2 more.
+// What it takes, 3 to 5 us a step for all layers, is the launch and its chain of reads and sums.
 #pragma once
 #include "k8_dev.hpp"
 
