@@ -558,12 +558,13 @@ constexpr int kPitch = D + 4;  // of the rows that the waves put into LDS at the
 
 // A unit of G groups of 32 rows.  Every wave takes a quarter of the tokens, pairs wave, wave + 4, ...; the four meet at the end.
 //   G = 1   two pairs at a time, so that a softmax's way through its lanes is taken once for 64 tokens
-//   G = 2   one pair at a time: what turning its codes costs, and reading them, serves twice as many rows
+//   G = 2   what turning a pair's codes costs, and reading them, serves twice as many rows; with 128 dims there are registers for one pair at a time (with 64,
+//           two instead of one are worth 5%: four requests' pieces of prompts 107 -> 102 us a pass)
 // Q's operands lie in LDS, a copy for each wave (where its output goes later): in registers they would leave no room for that.
 template <int CODES, int D, int KIND, int G>
 __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
   constexpr bool MARKS = KIND == kMarked;
-  constexpr int N = 3 - G;
+  constexpr int N = G == 1 || D == 64 ? 2 : 1;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 31, half = lane >> 5;
   const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's
   half8* q = (half8*)(lds + wave * kRows * kPitch<D>);
