@@ -156,7 +156,8 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
   const int2v upto_here = group_scan<NT>(int2v{parts, rows}, s_tmp, all);
   const int at = upto_here[0] - parts, row_at = upto_here[1] - rows, n_units = all[0];
   // the second half of what runs at once stands in reverse
-  const int half = a.capacity / 2, unit = n_units <= a.capacity && (int)blockIdx.x >= half && (int)blockIdx.x < n_units ? half + n_units - 1 - (int)blockIdx.x : blockIdx.x;
+  const int here = blockIdx.x, half = a.capacity / 2;
+  const int unit = n_units <= a.capacity && here >= half && here < n_units ? half + n_units - 1 - here : here;
   const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;  // (the host's bounds hold: see pasta_kv8.hip)
   if (unit >= at && unit < at + parts && fits) s_unit = part_of(u, cost, unit - at, parts, row_at);
   if (blockIdx.x == 0 && tid < a.max_tiles) a.tiles[tid] = Tile{u.s0, u.n_rows, row_at, tid < n_tiles && fits ? parts : 0};

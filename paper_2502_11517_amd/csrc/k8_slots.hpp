@@ -2,8 +2,8 @@
 //
 // Everything goes in the order of the requests, by sums over them; nothing is bound by bandwidth.  What a step takes is its dependent reads, one
 // behind the other, so with up to a thread per request all of them are asked for at once, the sums stay in LDS, and every work-group finds out the
-// same for itself: the first writes what belongs to the requests, all of them return pages and place rows, in one launch.  A page that comes back and is taken in the
-// same step is looked up where it was, not on the stack.  Where lengths or the count are written in place that does not go (one work-group may write
+// same for itself: the first writes what belongs to the requests, all of them return pages and place rows, in one launch.  A page that comes back
+// and is taken in the same step is looked up where it was, not on the stack.  Where lengths or the count are written in place that does not go (one work-group may write
 // what another has still to read), and with more requests than threads neither: one work-group then does the requests, and rows beyond kSlotsHere
 // follow in a second launch.  16 requests of up to eight rows 2.7 us, 512 requests with drafts taken back 5.4, 64 prompts with 259k rows 4.1 (3.7 MB):
 // launch, three reads behind one another, two sums over the requests and a search per row.
