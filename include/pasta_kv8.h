@@ -194,10 +194,11 @@ int32_t pasta_kv8_plan(pasta_kv8 *h, const pasta_kv8_plan_args *a);
  * streams whose rows a row's stream descends from; once all streams of a request
  * have joined, prefix_len covers them and their tags are free again.
  *
- * Sums, maxima and the output are held in fp32, the softmax weights enter the
- * product with V as fp16.  A block whose V scale is more than 2^60 below another's
- * of the request adds its tokens to the sums, but nothing to out.  Rows that no request has (behind
- * row_offsets[n_requests]) get out = 0, lse = -inf.
+ * Sums, maxima and the output are held in fp32.  The softmax weights, each times
+ * its block's V scale and in units of the row's largest such product, enter the
+ * product with V as fp16: what is 2^-25 of the largest or less adds to the sums, but
+ * nothing to out.  Rows that no request has (behind row_offsets[n_requests]) get
+ * out = 0, lse = -inf.
  * Needs everything but free_pages; slot_tag with row_see, slot_position with
  * row_position.  n_rows is that of the last plan (E_STATE otherwise, or without one).
  * Errors: E_INVAL, E_DEVICE, E_STATE.                                            */

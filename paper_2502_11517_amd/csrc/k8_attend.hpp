@@ -67,12 +67,16 @@ struct AttendArgs {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;   // the base of the scores follows their maximum when that is 2^8 ahead: O is rescaled rarely, and weights up to 256
                                 // lose nothing in fp16
-constexpr int kScaleSpan = 60;  // V of blocks whose scale is more powers of two than this below the largest counts as 0
+constexpr int kScaleSpan = 60;  // blocks whose V scale is more powers of two than this below the largest so far have their part of l summed apart
 
 __device__ inline float other_half(float x) {  // of lane ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
+
+// 2^d as h * h.  O goes by the product; l, which carries the inverse of V's scales and may be 2^100 where 2^d is less than any number of fp32, by one
+// factor after the other.
+__device__ inline float root_exp2(float d) { return __builtin_amdgcn_exp2f(0.5f * d); }
 
 // Lane i of each row of 16 lanes, for all lanes of the row.  The move stays one of its own: joined by the compiler with the subtraction that
 // uses it (v_subrev_u32 with row_newbcast), every lane got its own value on this chip.
@@ -193,12 +197,12 @@ __device__ inline void load_scales(const AttendArgs& a, Blocks& b) {
   b.vs = a.vs[max(b.at, 0)];
 }
 
-// `most`: the largest exponent of V's scales so far; these blocks' are added to it.
+// `most`: the largest exponent of V's scales so far; these blocks' are added to it.  (A block that is absent has no weight, one that reads as NaN any.)
 __device__ inline void finish_scales(Blocks& b, int& most) {
   const int x = (int)((__float_as_uint(b.vs) >> 23) & 255) - 127;
   const bool there = b.at >= 0, nan = x == 128;
   most = max(most, (int)__builtin_amdgcn_readfirstlane(wave_max(there && !nan ? x + 127 : 0)) - 127);
-  b.ev = (float)(there && !nan ? max(x, most - kScaleSpan) : most);
+  b.ev = (float)(there && !nan ? max(x, kEMin) : most);
   b.absent = __ballot(!there);
   b.nan = __ballot(there && nan);
   b.far = __ballot(there && x < most - kScaleSpan);
@@ -412,32 +416,41 @@ __device__ inline void soften(State<D> (&z)[G], const float16v (&s)[G][N], const
   if (__builtin_expect(__any(ahead), 0)) {
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      const float to = fmaxf(m[g], z[g].m), alpha = __builtin_amdgcn_exp2f(z[g].m - to);
+      const float to = fmaxf(m[g], z[g].m), h = root_exp2(z[g].m - to), alpha = h * h;
       z[g].m = to;
-      z[g].l *= alpha;
+      z[g].l = z[g].l * h * h;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int k = 0; k < 16; ++k) z[g].o[i][k] *= alpha;
     }
   }
-  float off[G][N];
+  float off[G][N], back[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) back[n] = __builtin_amdgcn_exp2f(-p[n].ev);
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
     for (int n = 0; n < N; ++n) off[g][n] = p[n].ev - z[g].m;
+  // Of a block whose scale is far below the largest, y may be less than any number of fp32 where y / vs still counts: its part of l goes by the
+  // largest score of its own.
   if (__builtin_expect(rare, 0)) {
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         bool sees = false;
-        float sum = 0.f;
+        float most = -FLT_MAX, sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sees |= s[g][n][i] != -INFINITY, sum += __builtin_amdgcn_exp2f(fmaf(s[g][n][i], f[g][n], off[g][n]));
+        for (int i = 0; i < 16; ++i) sees |= s[g][n][i] != -INFINITY, most = fmaxf(most, s[g][n][i] * f[g][n]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(fmaf(s[g][n][i], f[g][n], -most));
         if (of_half(p[n].nan) && sees) z[g].bad = __builtin_nanf("");
-        if (of_half(p[n].far)) z[g].l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z[g].l), off[g][n] = -INFINITY;
+        const float h = root_exp2(most - z[g].m);
+        if (of_half(p[n].far)) z[g].l = fmaf(sum * h, h, z[g].l);
       }
+#pragma unroll
+    for (int n = 0; n < N; ++n) back[n] = of_half(p[n].far) ? 0.f : back[n];
   }
 #pragma unroll
   for (int g = 0; g < G; ++g)
@@ -450,7 +463,7 @@ __device__ inline void soften(State<D> (&z)[G], const float16v (&s)[G][N], const
         y[i] = __builtin_amdgcn_exp2f(fmaf(s[g][n][i], f[g][n], off[g][n]));
         sum += y[i];
       }
-      z[g].l = fmaf(sum, __builtin_amdgcn_exp2f(-p[n].ev), z[g].l);
+      z[g].l = fmaf(sum, back[n], z[g].l);
       to_half(y, w[g][n]);
     }
 }
@@ -680,9 +693,9 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
       float4v o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float f = __builtin_amdgcn_exp2f(ml[w][0] - m);
-        all = fmaf(ml[w][1], f, all);
-        o += part[w] * f;
+        const float h = root_exp2(ml[w][0] - m);
+        all = fmaf(ml[w][1] * h, h, all);
+        o += part[w] * (h * h);
       }
       if (i >= rows) continue;
       if (u.part < 0) {
@@ -762,14 +775,14 @@ __global__ __launch_bounds__(256) void k8_merge(AttendArgs a) {
       const float before = m;
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) m = fmaxf(m, x[i][0]);
-      const float f = __builtin_amdgcn_exp2f(before - m);
-      l *= f, o *= f;
+      const float h = root_exp2(before - m);
+      l = l * h * h, o *= h * h;
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
         if (k0 + i * share >= tile.n_parts) continue;
-        const float f = __builtin_amdgcn_exp2f(x[i][0] - m);
-        l = fmaf(x[i][1], f, l);
-        o += y[i] * f;
+        const float h = root_exp2(x[i][0] - m);
+        l = fmaf(x[i][1] * h, h, l);
+        o += y[i] * (h * h);
       }
     }
     if (share > 1) {
@@ -782,9 +795,9 @@ __global__ __launch_bounds__(256) void k8_merge(AttendArgs a) {
       l = 0.f, o = float4v{0.f, 0.f, 0.f, 0.f};
       for (int x = 0; x < share; ++x) {
         const float2v y = s_ml[group + x];
-        const float f = __builtin_amdgcn_exp2f(y[0] - m);
-        l = fmaf(y[1], f, l);
-        o += s_o[group + x][d] * f;
+        const float h = root_exp2(y[0] - m);
+        l = fmaf(y[1] * h, h, l);
+        o += s_o[group + x][d] * (h * h);
       }
     }
     if (!real) continue;
