@@ -42,7 +42,7 @@ struct AttendArgs {
   int Hq, g_shift, dtype, n_rows;
   float scale_log2;       // |softmax_scale| * log2(e)
   int negate;             // softmax_scale < 0
-  float cap_log2, cap_in; // logit_cap * log2(e), 2 / logit_cap; 0: none
+  float cap_log2, cap_in; // logit_cap * log2(e), 2 / logit_cap, both held within fp32; 0: none
   const uint8_t *k, *v;
   const float *ks, *vs;
   const int* table;
@@ -67,6 +67,7 @@ struct AttendArgs {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;   // the base of the scores follows their maximum when that is 2^8 ahead: O is rescaled rarely, and weights up to 256
                                 // lose nothing in fp16
+constexpr float kLowCap = 128.f;  // caps up to this (log2 units) need no second form for small scores
 constexpr int kScaleSpan = 60;  // blocks whose V scale is more powers of two than this below the largest so far have their part of l summed apart
 
 __device__ inline float other_half(float x) {  // of lane ^ 32
@@ -318,10 +319,24 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
   const bool shaped = KIND != kPlain && (a.cap_log2 > 0.f || a.lowered);
   if (KIND == kPlain ? __builtin_expect(!masked, 1) : !masked && !shaped) return;
   if (KIND != kPlain && a.cap_log2 > 0.f) {
-    // cap * tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap))
+    // cap * tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), which is off by 2^-22 or so of the cap, whatever x
     const float g = f * a.cap_in;
+    auto closed = [&](float y) { return fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y)), a.cap_log2); };
+    if (a.cap_log2 <= kLowCap) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[i] * g)), a.cap_log2);
+      for (int i = 0; i < 16; ++i) s[i] = closed(s[i] * g);
+    } else {
+      // where x is small beside a high cap: x * tanh(u) / u by its series in u = x / cap, off by 2^-28 at u = 1/8
+      constexpr float kUnit = 0.25f * kLn2 * kLn2, c1 = -kUnit / 3.f, c2 = 2.f * kUnit * kUnit / 15.f, c3 = -17.f * kUnit * kUnit * kUnit / 315.f;
+      float to = g;
+      asm volatile("" : "+v"(to));  // (or else all sixteen s * g are made ahead of the branch, and s has to be kept beside them)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = s[i] * to, w = y * y;  // y = 2 u log2(e)
+        s[i] = fabsf(y) < 0.25f * kLog2e ? s[i] * f * fmaf(fmaf(fmaf(c3, w, c2), w, c1), w, 1.f) : closed(y);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     f = 1.f;
   }
   if (KIND != kPlain && a.lowered) {

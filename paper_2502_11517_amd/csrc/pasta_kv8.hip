@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -305,7 +306,8 @@ extern "C" int32_t pasta_kv8_attend(pasta_kv8* h, const pasta_kv8_attend_args* a
   while ((1 << k.g_shift) < k.g.G) k.g_shift++;
   k.scale_log2 = std::fabs(c.softmax_scale) * kLog2e;
   k.negate = c.softmax_scale < 0.f;
-  if (a->logit_cap > 0.f) k.cap_log2 = a->logit_cap * kLog2e, k.cap_in = 2.f / a->logit_cap;
+  // (below a cap of 2^-63 everything is the cap or less: how steeply it gets there no longer matters)
+  if (a->logit_cap > 0.f) k.cap_log2 = std::fmax(std::fmin(a->logit_cap * kLog2e, FLT_MAX), FLT_MIN), k.cap_in = std::fmin(2.f / a->logit_cap, 0x1p64f);
   const int64_t at = (int64_t)c.n_phys_pages * c.n_kv_heads * h->g.blocks_per_page * a->layer;
   k.k = (const uint8_t*)c.k_codes + at * 16 * c.head_dim, k.v = (const uint8_t*)c.v_codes + at * 16 * c.head_dim;
   k.ks = c.k_scale + at, k.vs = c.v_scale + at;
