@@ -104,7 +104,7 @@ struct Rows {
   float slope;  // in log2 units
   int token;    // own place
   int first_token;  // the wave's first row's
-  int position;
+  uint32_t position;  // from -2^31 on
   uint64_t see;
   int by_tag;  // lane t: which of the wave's rows see tag t
   bool real;
@@ -127,7 +127,7 @@ __device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head
   r.slope = a.slopes[head * a.g.G + (s & (a.g.G - 1))];
   if constexpr (MARKS) {
     r.see = a.row_see[s >> a.g_shift];
-    r.position = a.row_position[s >> a.g_shift];
+    r.position = (uint32_t)a.row_position[s >> a.g_shift] ^ 0x80000000u;
   } else {
     r.see = 0, r.position = 0;
   }
@@ -282,19 +282,25 @@ struct Unmarked {
 };
 
 struct Marked {
-  Marks marks;
-  int position, by_tag;
+  int tag, by_tag;
+  uint32_t mark, position;  // of the token and of the row, from -2^31 on: two of them can be up to 2^32 - 1 apart
+  __device__ Marked(const Marks& m, uint32_t position, int by_tag)
+      : tag(m.tag), by_tag(by_tag), mark((uint32_t)m.position ^ 0x80000000u), position(position) {}
   template <class F>
   __device__ void distances(F f) const {
-    each<16>([&](auto i) { f(i.value, (float)(position - of_row<i.value>(marks.position))); });
+    each<16>([&](auto i) {
+      uint32_t far;
+      asm("v_sad_u32 %0, %1, %2, 0" : "=v"(far) : "v"(position), "v"(of_row<i.value>((int)mark)));
+      f(i.value, (float)far);
+    });
   }
   // Whether the tokens' positions go up by one from each to the next, as in a prompt; then how far the lane's first token is from its row.
   __device__ bool in_order(float& far) const {
-    const int first = of_row<0>(marks.position);
-    far = (float)(position - first);
-    return __all(marks.position - first == (int)(threadIdx.x & 15));
+    const uint32_t first = (uint32_t)of_row<0>((int)mark);
+    far = position >= first ? (float)(position - first) : -(float)(first - position);
+    return __all(mark - first == (threadIdx.x & 15) && first <= UINT32_MAX - 15);
   }
-  __device__ int rows() const { return __builtin_amdgcn_ds_bpermute((marks.tag & 63) * 4, by_tag); }  // that see the lane's token
+  __device__ int rows() const { return __builtin_amdgcn_ds_bpermute((tag & 63) * 4, by_tag); }  // that see the lane's token
 };
 
 // f(i, whether the lane's row sees token i of its block: -1 or 0), from the rows that see the lane's token.
@@ -351,7 +357,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
         for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], f, -slope * fabsf(far - (float)i));
       }
     } else {
-      source.distances([&](int i, float far) { s[i] = fmaf(s[i], f, -slope * fabsf(far)); });
+      source.distances([&](int i, float far) { s[i] = fmaf(s[i], f, -slope * far); });
     }
     f = 1.f;
   }
