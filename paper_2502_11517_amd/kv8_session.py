@@ -6,7 +6,8 @@ what its parent saw then, and does not see what the parent writes later.  A join
 has joined, everything written so far becomes a prefix that all of its rows see, and its tags are free again.
 
 A step is begin() with the threads that write a row, then layer() for every layer; nothing in it depends on values on the device, so a step of the same
-threads can be captured into a graph and replayed, each replay one token further (run this file for an example).
+threads can be captured into a graph and replayed, each replay one token further (run this file for an example).  Between replays other steps may be
+begun, of other requests too; the captured one keeps its own rows, for which see again().
 """
 from __future__ import annotations
 
@@ -60,6 +61,7 @@ class Session:
         self.logit_cap = logit_cap
         self.requests = [_Request() for _ in range(max_requests)]
         self.handle = self._step = self._stream = None
+        self._captured = []  # steps that graphs read: their memory stays the session's
         self.bind(torch.cuda.current_stream(self.device))
 
     def bind(self, stream):
@@ -163,12 +165,17 @@ class Session:
 
     def _enter(self, step):
         self._step = step
+        if torch.cuda.is_current_stream_capturing():
+            self._captured.append(step)
         self.handle.slots(self.length, step["offsets"], step["n"], self.slot, self.length, self.free_count, self.free_count, row_tag=step["tag"],
                           row_position=step["position"])
         self.handle.plan(self.length, step["offsets"], step["n"], max_request_rows=step["most"], prefix_len=self.prefix_len, slot=self.slot)
 
     def again(self):
-        """The step's threads once more, each as many rows further as it has in the step: what a replayed graph does."""
+        """The step's threads once more, each as many rows further as it has in the step: what a replayed graph does.
+
+        Captured, the step goes on with rows, tags and positions of its own for as long as the session lives.  They are those of the capture: between
+        replays its threads neither fork nor join nor write rows by other calls.  What other requests do is free."""
         def go_on():
             self._step["position"].add_(self._step["stride"])
             self._enter(self._step)
