@@ -70,9 +70,13 @@ class Session:
         self.handle = kv8.PastaKv8(self.cfg, self.workspace, page_table=self.page_table, k_codes=self.k_codes, v_codes=self.v_codes,
                                    k_scale=self.k_scale, v_scale=self.v_scale, free_pages=self.free_pages, slot_tag=self.slot_tag,
                                    slot_position=self.slot_position, stream=stream.cuda_stream)
-        if self._step is not None:  # memory of the new stream's, that it may be given back behind its work
+        if self._step is not None:  # memory of the new stream's, that it may be given back behind its work; the old one's, not ahead of the copies
+            old = self._step
             with torch.cuda.stream(stream):
-                self._step = {k: v.clone() if torch.is_tensor(v) else v for k, v in self._step.items()}
+                self._step = {k: v.clone() if torch.is_tensor(v) else v for k, v in old.items()}
+            for v in old.values():
+                if torch.is_tensor(v):
+                    v.record_stream(stream)
 
     # ---- threads (host) ------------------------------------------------------------------------
     def _new_tag(self, request):

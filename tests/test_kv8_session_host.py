@@ -57,3 +57,31 @@ def test_a_captured_steps_memory_outlives_the_steps_that_follow(session, monkeyp
     session.handle.made.clear()
     gc.collect()
     assert between() is None and all(r() is not None for r in kept)
+
+
+def test_a_bound_steps_old_memory_waits_for_the_copies(session, monkeypatch):
+    """The copies are made on the new stream, and the allocator knows memory by the stream it was taken on."""
+    import contextlib
+
+    waits = []
+
+    class Recorded(torch.Tensor):
+        def record_stream(self, stream):
+            waits.append((self.data_ptr(), stream))
+
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
+    monkeypatch.setattr(kv8_session.kv8, "PastaKv8", lambda *args, **kw: Calls())
+    for name in ("cfg", "workspace", "page_table", "k_codes", "v_codes", "k_scale", "v_scale", "free_pages", "slot_tag", "slot_position"):
+        setattr(session, name, None)
+    t = session.open(0)
+    session.begin([t] * 4)
+    session._step = {k: v.as_subclass(Recorded) if torch.is_tensor(v) else v for k, v in session._step.items()}
+    old = [v.data_ptr() for v in session._step.values() if torch.is_tensor(v)]
+
+    class Stream:
+        cuda_stream = 7
+
+    new = Stream()
+    session.bind(new)
+    assert sorted(waits, key=lambda w: w[0]) == [(p, new) for p in sorted(old)] and len(old) == 5
+    assert not set(old) & {v.data_ptr() for v in session._step.values() if torch.is_tensor(v)}
