@@ -119,7 +119,7 @@ def cache_shapes(cfg: Config):
 
 
 def _p(t, dtypes=None, shape=None, what=""):
-    """Address of a tensor (or an address itself), after what can be checked of it: type, contiguity, number of values."""
+    """Address of a tensor (or an address itself), after what can be checked of it: type, contiguity, number of values, and that it is the GPU's."""
     if t is None or isinstance(t, int):
         return t
     if dtypes is not None and str(t.dtype) not in dtypes:
@@ -132,6 +132,8 @@ def _p(t, dtypes=None, shape=None, what=""):
             want *= n
         if t.numel() < want:
             raise ValueError(f"{what}: {tuple(t.shape)}, {tuple(shape)} is wanted")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: on {t.device}, device memory is wanted")
     return t.data_ptr()
 
 
@@ -141,8 +143,8 @@ _BYTES = {E4M3: ("torch.float8_e4m3fn", "torch.uint8"), INT8: ("torch.int8", "to
 
 
 class PastaKv8:
-    """One handle.  Buffers are device addresses (or torch tensors, which are then kept alive and checked for type, contiguity and
-    size) owned by the caller; those that no call needs may be left out.  `stream` is a hipStream_t as an int."""
+    """One handle.  Buffers are device addresses (or torch tensors, which are then kept alive and checked for type, contiguity,
+    size and device) owned by the caller; those that no call needs may be left out.  `stream` is a hipStream_t as an int."""
 
     def __init__(self, cfg: Config, workspace, *, page_table=None, k_codes=None, v_codes=None, k_scale=None, v_scale=None, free_pages=None,
                  slot_tag=None, slot_position=None, stream=0, workspace_bytes=None):
