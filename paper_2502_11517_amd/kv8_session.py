@@ -152,11 +152,11 @@ class Session:
         if where != sorted(where) or not all(t.alive for t in rows):
             raise ValueError("rows of living threads, requests ascending")
         count = [0] * len(self.requests)
-        ids = []
+        ids, after = [], {id(t): t.position for t in rows}
         for i, t in enumerate(rows):
             count[t.request] += 1
-            ids.append(t.position if positions is None else int(positions[i]))
-            t.position = ids[-1] + 1
+            ids.append(after[id(t)] if positions is None else int(positions[i]))
+            after[id(t)] = ids[-1] + 1
         offsets = [0]
         for k in count:
             offsets.append(offsets[-1] + k)
@@ -166,14 +166,16 @@ class Session:
         self._on_stream(lambda: self._enter(dict(
             n=n, most=max(count), offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8), see=dev(signed, torch.int64),
             position=dev(ids, torch.int32), stride=dev([times[id(t)] for t in rows], torch.int32))))
+        for t in rows:
+            t.position = after[id(t)]
 
     def _enter(self, step):
-        self._step = step
         if torch.cuda.is_current_stream_capturing():
             self._captured.append(step)
         self.handle.slots(self.length, step["offsets"], step["n"], self.slot, self.length, self.free_count, self.free_count, row_tag=step["tag"],
                           row_position=step["position"])
         self.handle.plan(self.length, step["offsets"], step["n"], max_request_rows=step["most"], prefix_len=self.prefix_len, slot=self.slot)
+        self._step = step
 
     def again(self):
         """The step's threads once more, each as many rows further as it has in the step: what a replayed graph does.

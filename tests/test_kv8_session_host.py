@@ -85,3 +85,20 @@ def test_a_bound_steps_old_memory_waits_for_the_copies(session, monkeypatch):
     session.bind(new)
     assert sorted(waits, key=lambda w: w[0]) == [(p, new) for p in sorted(old)] and len(old) == 5
     assert not set(old) & {v.data_ptr() for v in session._step.values() if torch.is_tensor(v)}
+
+
+@pytest.mark.parametrize("refuse", ["slots", "plan", "positions"])
+def test_a_step_that_is_not_accepted_moves_nothing_on(session, refuse):
+    t = session.open(0)
+    session.begin([t] * 5)
+    u = session.fork(t)
+    before = session._step
+    session.handle.refuse = refuse
+    with pytest.raises((kv8_session.kv8.PastaError, IndexError)):
+        session.begin([t, u, t, u], positions=[9, 9] if refuse == "positions" else None)
+    assert (t.position, u.position) == (5, 5) and session._step is before
+    session.handle.refuse = None
+    session.begin([t, u, t, u])
+    assert (t.position, u.position) == (7, 7) and session._step["position"].tolist() == [5, 5, 6, 6] and session._step["stride"].tolist() == [2] * 4
+    session.begin([u, t, u], positions=[40, 3, 50])
+    assert (t.position, u.position) == (4, 51)
