@@ -146,7 +146,10 @@ class Session:
 
     # ---- a step --------------------------------------------------------------------------------
     def begin(self, rows, positions=None):
-        """Places of a step's rows: `rows` names the thread of each, requests ascending (a thread may write several).  `positions`: their ids."""
+        """Places of a step's rows: `rows` names the thread of each, requests ascending (a thread may write several).  `positions`: their ids.
+
+        A request that the cache has no room for is refused on the device, which the host does not wait for: the positions of its threads go on as if it
+        had been served, until refused() sets them back."""
         n = len(rows)
         where = [t.request for t in rows]
         if where != sorted(where) or not all(t.alive for t in rows):
@@ -164,7 +167,7 @@ class Session:
         signed = [t.sees - (1 << 64) if t.sees >> 63 else t.sees for t in rows]
         times = Counter(id(t) for t in rows)
         self._on_stream(lambda: self._enter(dict(
-            n=n, most=max(count), offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8), see=dev(signed, torch.int64),
+            n=n, most=max(count), rows=list(rows), offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8), see=dev(signed, torch.int64),
             position=dev(ids, torch.int32), stride=dev([times[id(t)] for t in rows], torch.int32))))
         for t in rows:
             t.position = after[id(t)]
@@ -176,6 +179,7 @@ class Session:
                           row_position=step["position"])
         self.handle.plan(self.length, step["offsets"], step["n"], max_request_rows=step["most"], prefix_len=self.prefix_len, slot=self.slot)
         self._step = step
+        step["refused"] = None  # (not known)
 
     def again(self):
         """The step's threads once more, each as many rows further as it has in the step: what a replayed graph does.
@@ -186,6 +190,24 @@ class Session:
             self._step["position"].add_(self._step["stride"])
             self._enter(self._step)
         self._on_stream(go_on)
+
+    def refused(self):
+        """The requests that the last step begun, or gone on with by a call of again(), was refused for (waits for the device).  Their threads' next rows get
+        the ids of the refused ones."""
+        s = self._step
+        if s["refused"] is None:
+            with torch.cuda.stream(self._stream):
+                slot, ids = self.slot[:s["n"]].tolist(), s["position"].tolist()
+                first = {}
+                for i, t in enumerate(s["rows"]):
+                    first.setdefault(t.request, i)
+                s["refused"] = sorted(r for r, i in first.items() if slot[i] < 0)
+                for i in reversed(range(s["n"])):  # (of a thread's rows the first one's)
+                    t = s["rows"][i]
+                    if t.request in s["refused"]:
+                        t.position = ids[i]
+                        s["position"][i] -= s["stride"][i]  # (again() adds it)
+        return s["refused"]
 
     def advanced(self, rows, steps):
         """Tells the host that `steps` calls or replays of again() with these rows have been enqueued."""

@@ -70,3 +70,33 @@ def test_a_captured_step_keeps_its_rows_when_others_are_begun(n):
     for (o, e), (w, f) in zip(x, y):
         assert torch.equal(o, w) and torch.equal(e, f)
     assert torch.equal(a.length, b.length) and torch.equal(a.page_table, b.page_table) and a.length.tolist() == [60 + 13 * n, 4 + 9 * (1 + 4 + 7 + 10)]
+
+
+def test_a_refused_requests_rows_take_the_same_ids_when_there_is_room():
+    """Against a session that had the room from the start: places differ, positions and so the scores, which distance lowers, do not."""
+    runs = []
+    for pages in (5, 9):
+        torch.manual_seed(3)
+        s = Session(n_q_heads=2, n_kv_heads=2, head_dim=64, softmax_scale=0.125, max_requests=2, max_rows=128, n_phys_pages=pages, pages_per_request=8,
+                    slopes=[0.5, 0.125])
+        x = lambda n, h: torch.randn(n, h, 64, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+        a, b = s.open(0), s.open(1)
+
+        def step(rows):
+            s.begin(rows)
+            out, lse = torch.empty(len(rows), 2, 64, device="cuda", dtype=torch.bfloat16), torch.empty(len(rows), 2, device="cuda")
+            s.layer(0, x(len(rows), 2), x(len(rows), 2), x(len(rows), 2), out, lse)
+            return out, lse
+
+        step([a] * 48 + [b] * 20)
+        assert s.refused() == []
+        if pages == 5:
+            out, lse = step([b] * 30)
+            assert s.refused() == [1] and b.position == 20 and s.length.tolist() == [48, 20] and torch.isneginf(lse).all()
+            torch.manual_seed(4)
+            s.release(0)
+        torch.manual_seed(4)
+        runs.append(step([b] * 30))
+        assert s.refused() == [] and b.position == 50 and int(s.length[1]) == 50
+        runs.append(step([b]))
+    assert all(torch.equal(x, y) for i in (0, 1) for x, y in zip(runs[i], runs[i + 2]))

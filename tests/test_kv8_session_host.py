@@ -102,3 +102,22 @@ def test_a_step_that_is_not_accepted_moves_nothing_on(session, refuse):
     assert (t.position, u.position) == (7, 7) and session._step["position"].tolist() == [5, 5, 6, 6] and session._step["stride"].tolist() == [2] * 4
     session.begin([u, t, u], positions=[40, 3, 50])
     assert (t.position, u.position) == (4, 51)
+
+
+def test_positions_of_refused_requests_are_set_back(session):
+    a, b = session.open(0), session.open(1)
+    session.begin([a] * 2 + [b] * 3)
+    session.slot[:5] = torch.tensor([0, 1, 16, 17, 18])
+    assert session.refused() == [] and (a.position, b.position) == (2, 3)
+    kid = session.fork(b)
+    session.begin([a, b, kid, b, kid])
+    assert session._step["position"].tolist() == [2, 3, 3, 4, 4]
+    session.slot[:5] = torch.tensor([2, -1, -1, -1, -1])
+    assert (a.position, b.position, kid.position) == (3, 5, 5)
+    for _ in range(2):
+        assert session.refused() == [1] and (a.position, b.position, kid.position) == (3, 3, 3)
+    session.again()
+    session.advanced([a, b, kid, b, kid], 1)
+    assert session._step["position"].tolist() == [3, 3, 3, 4, 4] and (a.position, b.position, kid.position) == (4, 5, 5)
+    session.slot[:5] = torch.tensor([-1, 19, 20, 21, 22])
+    assert session.refused() == [0] and (a.position, b.position, kid.position) == (3, 5, 5)
