@@ -15,10 +15,10 @@
  *
  * Conventions are those of pasta_attn.h: status codes, nothing throws or aborts,
  * DEVICE pointers are the caller's, the library allocates no device memory, all
- * work is enqueued on the handle's stream.  The calls make no HIP call but kernel
- * launches, so all four may be captured into a graph.  A caller that uses a buffer
- * on another stream orders the two itself.  Calls on one handle are not
- * thread-safe.
+ * work is enqueued on the handle's stream, whose device has to be the current one.
+ * The calls make no HIP call but kernel launches, so all four may be captured into
+ * a graph.  A caller that uses a buffer on another stream orders the two itself.
+ * Calls on one handle are not thread-safe.
  *
  * DEVICE arrays cannot be checked on the host.  The kernels check what they read
  * from them before they use it as an address: lengths and offsets are clamped to

@@ -217,9 +217,10 @@ class Session:
     def layer(self, layer, k_new, v_new, q, out, lse=None):
         """Appends the step's rows of a layer, then attends: row i sees its own row too."""
         s = self._step
-        self.handle.append(layer, self.slot, k_new, v_new, n_rows=s["n"])
-        self.handle.attend(layer, q, out, lse=lse, logit_cap=self.logit_cap, slopes=self.slopes, row_see=s["see"],
-                           row_position=s["position"] if self.slopes is not None else None)
+        with torch.cuda.device(self.device):  # (a launch goes by the current device; the stream is the handle's)
+            self.handle.append(layer, self.slot, k_new, v_new, n_rows=s["n"])
+            self.handle.attend(layer, q, out, lse=lse, logit_cap=self.logit_cap, slopes=self.slopes, row_see=s["see"],
+                               row_position=s["position"] if self.slopes is not None else None)
 
 
 def main():

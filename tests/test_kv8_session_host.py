@@ -121,3 +121,21 @@ def test_positions_of_refused_requests_are_set_back(session):
     assert session._step["position"].tolist() == [3, 3, 3, 4, 4] and (a.position, b.position, kid.position) == (4, 5, 5)
     session.slot[:5] = torch.tensor([-1, 19, 20, 21, 22])
     assert session.refused() == [0] and (a.position, b.position, kid.position) == (3, 5, 5)
+
+
+def test_a_layers_launches_are_made_under_the_sessions_device(session, monkeypatch):
+    import contextlib
+
+    under = []
+
+    @contextlib.contextmanager
+    def device(d):
+        under.append(d)
+        yield
+        under.append(len(session.handle.made))
+
+    session.begin([session.open(0)])
+    session.handle.made.clear()
+    monkeypatch.setattr(torch.cuda, "device", device)
+    session.layer(0, None, None, None, None)
+    assert under == [session.device, 2] and [name for name, _, _ in session.handle.made] == ["append", "attend"]
