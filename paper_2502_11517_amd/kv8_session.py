@@ -99,6 +99,8 @@ class Session:
 
     def fork(self, parent: Thread, position=None) -> Thread:
         """A child that sees what `parent` sees now.  `position`: id of its first row (estimated ids may leave gaps); else it counts on."""
+        if not parent.alive:
+            raise ValueError("forks a living thread")
         r = self.requests[parent.request]
         free = TAGS - bin(r.used).count("1")
         if free < 2:
@@ -112,9 +114,12 @@ class Session:
     def join(self, thread: Thread, others):
         """`thread` sees from now on what `others` saw; they end.  Their rows stay where they are."""
         r = self.requests[thread.request]
+        others = list(others)
+        if not thread.alive or len({id(o) for o in others}) != len(others):
+            raise ValueError("joins living threads of one request, each once")
         for o in others:
             if o is thread or not o.alive or o.request != thread.request:
-                raise ValueError("joins living threads of one request")
+                raise ValueError("joins living threads of one request, each once")
         for o in others:
             thread.sees |= o.sees
             o.alive = False

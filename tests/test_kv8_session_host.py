@@ -139,3 +139,20 @@ def test_a_layers_launches_are_made_under_the_sessions_device(session, monkeypat
     monkeypatch.setattr(torch.cuda, "device", device)
     session.layer(0, None, None, None, None)
     assert under == [session.device, 2] and [name for name, _, _ in session.handle.made] == ["append", "attend"]
+
+
+def test_threads_that_have_ended_neither_join_nor_fork(session):
+    root = session.open(0)
+    a, b, c = (session.fork(root) for _ in range(3))
+    session.join(root, [a])
+    before = [(t.tag, t.sees, t.alive) for t in (root, a, b, c)], session.requests[0].used
+    for call in (lambda: session.join(a, [b, c]), lambda: session.join(a, [b, root, c]), lambda: session.join(root, [b, b]), lambda: session.join(root, [b, a]),
+                 lambda: session.join(b, [c, b]), lambda: session.fork(a)):
+        with pytest.raises(ValueError):
+            call()
+        assert before == ([(t.tag, t.sees, t.alive) for t in (root, a, b, c)], session.requests[0].used) and session.requests[0].threads == [root, b, c]
+    session.join(root, (t for t in (b, c)))  # anything that can be gone over once
+    assert not b.alive and not c.alive and session.requests[0].threads == [root] and session.requests[0].used == 1
+    session.release(0)
+    with pytest.raises(ValueError):
+        session.fork(root)
