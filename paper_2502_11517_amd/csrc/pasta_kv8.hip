@@ -12,6 +12,7 @@
 #include "k8_append.hpp"
 #include "k8_attend.hpp"
 #include "k8_plan.hpp"
+#include "k8_rules.hpp"
 #include "k8_slots.hpp"
 
 namespace {
@@ -219,12 +220,7 @@ extern "C" int32_t pasta_kv8_append(pasta_kv8* h, const pasta_kv8_append_args* a
   k.g = h->g, k.n_rows = a->n_rows, k.slot = a->slot, k.k_new = a->k_new, k.v_new = a->v_new;
   k.k = (uint8_t*)c.k_codes + at * 16 * c.head_dim, k.v = (uint8_t*)c.v_codes + at * 16 * c.head_dim;
   k.ks = c.k_scale + at, k.vs = c.v_scale + at;
-  // Rows to a work-group, a power of two: as many as leave some 1300 work-groups, but no more than a run has on the mean if every request's rows are
-  // neighbours.  (1000 rows of one request, a layer, by 1 / 4 / 16: 10.0 / 4.5 / 5.5 us, most groups without a run; 1500 requests of one row by 1 / 16: 22 / 45
-  // us, a group's runs one after the other.)
-  const int64_t runs = a->n_rows / 16 + 2 * (int64_t)std::min(c.max_requests, a->n_rows), tasks = (2 * c.n_kv_heads + 3) / 4;
-  k.group = 1;
-  while (k.group < 16 && k.group * 1333 < a->n_rows * tasks && 2 * k.group * runs <= a->n_rows + a->n_rows / 16) k.group *= 2;
+  k.group = k8::append_group(a->n_rows, c.n_kv_heads);
   const dim3 grid((a->n_rows + k.group - 1) / k.group, (2 * c.n_kv_heads + 3) / 4);
   hipStream_t s = (hipStream_t)c.hip_stream;
   if (c.codes == PASTA_KV8_E4M3)
