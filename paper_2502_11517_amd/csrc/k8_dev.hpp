@@ -7,6 +7,8 @@
 
 #include <utility>
 
+#include "k8_split.hpp"
+
 namespace k8 {
 
 constexpr int kBlock = 16;           // tokens under one scale
@@ -14,11 +16,7 @@ constexpr int kEMin = -100, kEMax = 119;
 constexpr int kRows = 32;            // stacked rows (query row x head of the kv head's group) of one wave
 constexpr int kWideRows = 64;        // ... of one work-group, in requests that have more than kManyRows
 constexpr int kManyRows = 128;
-constexpr int kChunkTokens = 128;    // pieces of a tile's tokens are multiples of this (32 for each wave) ...
-constexpr int kLeastTokens = 384;    // ... and no shorter than this, or
-constexpr int kLeastAlone = 256;     // than this where half as many work-groups as the chip holds do with pieces of
-constexpr int kAloneTokens = 1024;   // at most this
-constexpr int kWholeTokens = 768, kWholeWide = 512;  // where no request holds more, no tile is split (with tiles of 32 rows; of 64 rows, too)
+constexpr int kWholeTokens = 768, kWholeWide = 512;  // where the table has room for no more, no tile is split (with tiles of 32 rows; of 64 rows, too)
 constexpr int kTaggedRows = 64;      // with a prefix and at most so many rows in a step, a request's rows are taken to be streams with tags
 constexpr int kMostTokens = 1 << 27; // of a request: a plan's sums over 1024 tiles stay within 32 bits
 constexpr int kUnitBlocks = 64;      // blocks of a unit that are listed with it

@@ -3,12 +3,15 @@
 // Rows come in tiles of 32, or, in requests with more than 128 stacked rows, of 64 (a wave then turns its codes once for two groups; with fewer rows,
 // fewer and longer pieces of the tokens are worth more: 128 rows over 49k tokens 60 us a layer in tiles of 32, 87 of 64).  A tile's tokens go in even
 // pieces, and what they leave, partial rows, k8_merge joins.  How long pieces are:
-//   * One work-group a CU where pieces of up to 1024 tokens do with that, no shorter than 256.  Two on a CU take turns at its SIMDs and gain a tenth; 328 of
-//     them take as long as 512 would.  Eight rows over 10k tokens in 224 / 328 pieces: 14.2 / 17.5 us a layer; 22 rows over 30k 134 / 148 us a pass.
-//   * Else two, in pieces no shorter than 384 tokens.  The older one of a SIMD's two waves runs ahead, so the second half of the list stands in reverse:
+//   * One work-group a CU where pieces of up to 1024 tokens do with that, no more of them than pieces of 256 would be.  Two on a CU take turns at its
+//     SIMDs and gain a tenth; 328 of them take as long as 512 would.  Eight rows over 10k tokens in 224 / 328 pieces: 14.2 / 17.5 us a layer; 22 rows over
+//     30k 134 / 148 us a pass.
+//   * Else two, no more pieces than of 384 tokens.  The older one of a SIMD's two waves runs ahead, so the second half of the list stands in reverse:
 //     a CU that starts with a dear piece (behind the prefix, where tags are looked at) gets a plain one with it.
-//   * Tables that hold at most 768 tokens (512 with tiles of 64) are not split, which saves the launch of k8_merge: 0.6 us a layer less for 500 tokens; 1200
-//     would take 2.2 more.
+//   * Even pieces of chunks of 128 tokens: what goes in n can come out at half of these lengths, a chunk at least (769 tokens: 128, 256, 256, 129).
+//   * Where tables have room for at most 768 tokens (512 with tiles of 64) nothing is split, which saves the launch of k8_merge: two and eight rows over
+//     300 / 500 / 700 tokens, a layer, 8.2 and 9.6 / 8.7 and 10.9 / 11.5 us; 11.1 and 12.4 / 11.2 and 12.2 / 12.1 in wide tables, as a server's are (the
+//     table's width is all that the host knows of the lengths).
 // What it takes, 3 to 5 us a step for all layers, is the launch and its chain of reads and sums.
 #pragma once
 #include "k8_dev.hpp"
@@ -71,29 +74,17 @@ __device__ inline Unit tile_of(const PlanArgs& a, int r, const RequestTiles& q, 
 
 __device__ inline int chunks_of(int tokens) { return (tokens + kChunkTokens - 1) / kChunkTokens; }
 
-// What a tile's tokens cost, in halves of kChunkTokens plain ones: behind the prefix of a request with few rows, where every token's tag has to be looked
-// at, three for two.
-struct Cost {
-  int chunks, cheap;  // the first `cheap` of them plain
-  __device__ int all() const { return 3 * chunks - cheap; }
-  __device__ int chunk_at(int64_t cost) const { return (int)(cost <= 2 * cheap ? cost / 2 : cheap + (cost - 2 * cheap) / 3); }
-};
-
 __device__ inline Cost cost_of(const Unit& u, const RequestTiles& q) {
   const int chunks = chunks_of(u.hi);
   return Cost{chunks, q.prefix > 0 && q.n <= kTaggedRows ? min(q.prefix / kChunkTokens, chunks) : chunks};
 }
 
-// Into how many pieces of at most `most` (in Cost's units) a tile goes.
-__device__ inline int parts_of(const PlanArgs& a, int cost, int most) {
-  return a.whole ? 1 : max(1, (cost + most - 1) / most);
-}
+__device__ inline int parts_of(const PlanArgs& a, int cost, int most) { return a.whole ? 1 : pieces_of(cost, most); }
 
 __device__ inline Unit part_of(Unit u, const Cost& c, int k, int parts, int row_at) {
   if (parts == 1) return u.lo = 0, u.part = -1, u;
-  const int64_t all = c.all();
-  u.lo = c.chunk_at(all * k / parts) * kChunkTokens;
-  if (k + 1 < parts) u.hi = c.chunk_at(all * (k + 1) / parts) * kChunkTokens;
+  u.lo = piece_at(c, k, parts) * kChunkTokens;
+  if (k + 1 < parts) u.hi = piece_at(c, k + 1, parts) * kChunkTokens;
   u.part = row_at + k * u.n_rows;
   return u;
 }
