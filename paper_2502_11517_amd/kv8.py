@@ -170,10 +170,10 @@ class PastaKv8:
 
     # Each operator as a prepared call (marshalled once: f() -> status) and as a call that raises.
     def _prepared(self, name, args, keep):
-        fn, h, ref = getattr(self._lib, name), self._h, C.byref(args)
+        fn, ref = getattr(self._lib, name), C.byref(args)
 
-        def call(_keep=(args, keep, self)):
-            return fn(h, ref)
+        def call(_keep=(args, keep)):
+            return fn(self._h, ref)  # (destroyed meanwhile: None, which is E_STATE)
         call.operator = name
         return call
 

@@ -57,3 +57,23 @@ def test_a_calls_arguments(call, name):
     getattr(h, "prepare_" + call)(**good)
     with pytest.raises(ValueError, match=name + ".*device memory"):
         getattr(h, "prepare_" + call)(**{**good, name: torch.zeros(8 * 32 * 128, dtype=types[name])})
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_a_prepared_call_of_a_destroyed_handle_does_not_reach_its_memory(call, monkeypatch):
+    h = handle()
+    seen = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda handle, args: seen.append(handle) or kv8.E_STATE
+
+    monkeypatch.setattr(h, "_lib", Library())
+    prepared = getattr(h, "prepare_" + call)(**CALLS[call][0])
+    h._h = None  # what destroy() leaves
+    assert prepared() == kv8.E_STATE and seen == [None]
+    monkeypatch.undo()
+    h = handle()
+    prepared = getattr(h, "prepare_" + call)(**CALLS[call][0])
+    h.destroy()
+    assert prepared() == kv8.E_STATE
