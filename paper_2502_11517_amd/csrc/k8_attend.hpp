@@ -8,7 +8,7 @@
 //
 // Codes are whole fp16 numbers, so K and V enter the products exactly, and the scales, powers of two, stay outside of them: K's is a
 // factor of the score, V's a term of the exponent, the same for 16 tokens.  The maximum that keeps y_j within [0, 1] is that of what
-// enters the second product, row by row, so that its rounding to fp16, 2^-12 of each y_j, is small against the row's own result
+// enters the second product, row by row, so that its rounding to fp16, at most 2^-11 of each y_j, is small against the row's own result
 // whatever the blocks' scales; it is the only rounding that fp32 does not see, half a step of an fp16 output.
 //
 // Both products run transposed, S^T = K Q^T and O^T = V^T P^T, in 32x32x16 steps of a wave over 32 tokens x 32 stacked rows.  What row of
@@ -20,13 +20,13 @@
 // A work-group takes 32 or 64 stacked rows; its four waves split the tokens, each with codes of its own in registers, and meet once at the end.
 //
 // What bounds it (8 kv heads of 128; a layer):
-//   8 streams over 8k tokens, 21 MB        10.5 us: the ramp.  1.2 us to the first codes alone, 3.1 with the whole chip asking, 3.3 for the three pairs of a
+//   8 streams over 8k tokens, 21 MB        11.1 us: the ramp.  1.2 us to the first codes alone, 3.1 with the whole chip asking, 3.3 for the three pairs of a
 //                                          wave, 1.5 for the waves' meeting, 2.5 of launch; the bytes are 4.3 us at a large copy's 4.9 TB/s
-//   16 ragged requests, 95 MB              25.4 us, 3.8 TB/s: memory
-//   16 x 8 rows over 51k tokens, 100 MB    58 us: vector instructions, 21 a score (codes to fp16, exponentials, distances, tags); the four tiles of rows
+//   16 ragged requests, 95 MB              26.0 us, 3.7 TB/s: memory
+//   16 x 8 rows over 51k tokens, 100 MB    59 us: vector instructions, 21 a score (codes to fp16, exponentials, distances, tags); the four tiles of rows
 //                                          share codes through the L2 only, since two groups of rows with marks do not fit the registers
-//   2048 x 4 rows over 8k tokens, 309 GF   320 us, 965 TFLOP/s against 1190 of a large library product: vector instructions busy 63% of the time, matrix
-//                                          instructions 42%
+//   2048 x 4 rows over 8k tokens, 309 GF   322 to 354 us by the card, 870 to 960 TFLOP/s against 1190 to 1230 of a large library product: vector
+//                                          instructions busy 64% of the time, matrix instructions 43%
 // Tried and not taken: eight waves to a work-group (8 streams over 8k 123 -> 133 us a pass; 128 registers would be needed for four waves to a SIMD, and spill),
 // one copy of Q's operands for all waves (a barrier; 1 to 3% more), touching the codes of the step after next ahead of their turn (4 to 7% more), three
 // waves to a SIMD with 64 dims (spills), no priority for waves at the matrix pipe (nested forks over 35k 4% more).

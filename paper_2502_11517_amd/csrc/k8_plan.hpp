@@ -12,7 +12,7 @@
 //   * Where tables have room for at most 768 tokens (512 with tiles of 64) nothing is split, which saves the launch of k8_merge: two and eight rows over
 //     300 / 500 / 700 tokens, a layer, 8.2 and 9.6 / 8.7 and 10.9 / 11.5 us; 11.1 and 12.4 / 11.2 and 12.2 / 12.1 in wide tables, as a server's are (the
 //     table's width is all that the host knows of the lengths).
-// What it takes, 3 to 5 us a step for all layers, is the launch and its chain of reads and sums.
+// What it takes, 3 to 5 us a step for all layers, is the launch and its chain of reads and sums.  From 256 requests or tiles on (k8_plan_long) 10 to 13.
 #pragma once
 #include "k8_dev.hpp"
 

@@ -5,8 +5,9 @@
 // same for itself: the first writes what belongs to the requests, all of them return pages and place rows, in one launch.  A page that comes back
 // and is taken in the same step is looked up where it was, not on the stack.  Where lengths or the count are written in place that does not go (one work-group may write
 // what another has still to read), and with more requests than threads neither: one work-group then does the requests, and rows beyond kSlotsHere
-// follow in a second launch.  16 requests of up to eight rows 2.7 us, 512 requests with drafts taken back 5.4, 64 prompts with 259k rows 4.1 (3.7 MB):
-// launch, three reads behind one another, two sums over the requests and a search per row.
+// follow in a second launch.  16 requests of up to eight rows 2.7 us, 512 requests with drafts taken back 5.8, 64 prompts with 259k rows 4.4 (3.7 MB):
+// launch, three reads behind one another, two sums over the requests and a search per row.  In place, calls alone: the first 3.4 (3.5 apart), the second 6.8
+// and 5.3 in two launches (6.2), the third 3.6 and 6.1 (5.3), 64 requests of 64 rows 12.3 (4.4).  1500 requests of a row, either way: 12.4.
 #pragma once
 #include "k8_dev.hpp"
 
