@@ -10,8 +10,8 @@
 
 A code is a sign, two bits of exponent and one of mantissa: 0, 1/2, 1, 3/2, 2, 3, 4, 6.  A row of K has a power of two per kv head and 32 dims, a row of V
 one per kv head, both held as their exponent + 127 (255: not a number): the least 2^e, -100 <= e <= 119, with max|x| <= 7 * 2^e.  A block is 16 tokens of a
-kv head: K's codes lie as [D / 32][16 tokens][32 dims], V's as [D / 64][32 dims][2][16 tokens] (dim 64 X + 32 j + d at X, d, j), two to a byte, the first
-in its low half; scales as [16 tokens][D / 32] and [16 tokens].
+kv head: K's codes lie as [D / 32][16 tokens][32 dims], V's as [D][16 tokens], two to a byte, the first in its low half; scales as [16 tokens][D / 32] and
+[16 tokens].
 
 A case holds sizes and the seed of its history (who appended what, and so what a row sees); the seed of prepare() makes the values and the places of the
 pages.  Sizes are those of the repository's configurations and benchmark (8 kv heads of 128, 32 or 64 query heads, prefixes of 256 to 32768 tokens, 1 to 32
@@ -268,7 +268,7 @@ def _cache(c, pages, normal, fill):
     """Codes and scales of a cache; `fill`: written by earlier steps, else zeros under the least scale."""
     L, H, B, D = c["layers"], c["hkv"], c["page"] // BLOCK, c["d"]
     s = dict(k_codes=torch.zeros(L, pages, H, B, D // 32, BLOCK, 16, dtype=torch.uint8, device="cuda"),
-             v_codes=torch.zeros(L, pages, H, B, D // 64, 32, 2, 8, dtype=torch.uint8, device="cuda"),
+             v_codes=torch.zeros(L, pages, H, B, D, 8, dtype=torch.uint8, device="cuda"),
              k_scale=torch.full((L, pages, H, B, BLOCK, D // 32), E_MIN + 127, dtype=torch.uint8, device="cuda"),
              v_scale=torch.full((L, pages, H, B, BLOCK), E_MIN + 127, dtype=torch.uint8, device="cuda"))
     if fill:
@@ -280,7 +280,7 @@ def _cache(c, pages, normal, fill):
             s["k_scale"][l], s["v_scale"][l] = ks, vs
             kc = kc.unflatten(-1, (D // 32, 16, 2)).transpose(-4, -3)  # [.., D / 32, 16 tokens, 16, 2]
             s["k_codes"][l] = kc[..., 0] | kc[..., 1] << 4
-            vc = vc.transpose(-1, -2).unflatten(-2, (D // 64, 2, 32)).transpose(-3, -2).unflatten(-1, (8, 2))  # [.., D / 64, 32, 2, 8, 2]
+            vc = vc.transpose(-1, -2).unflatten(-1, (8, 2))  # [.., D, 8, 2]
             s["v_codes"][l] = vc[..., 0] | vc[..., 1] << 4
     return s
 
@@ -438,10 +438,9 @@ def _plain_append(s):
     s["k_codes"][:, page, :, b, :, t] = kc[..., 0] | kc[..., 1] << 4
     s["k_scale"][:, page, :, b, t] = ks
     s["v_scale"][:, page, :, b, t] = vs
-    vc = vc.unflatten(-1, (D // 64, 2, 32)).transpose(-1, -2)  # [n, L, H, D / 64, 32, 2]
     for half in range(2):  # two tokens share a byte
         mine = torch.arange(n, device=t.device)[t % 2 == half]
-        at = (slice(None), page[mine], slice(None), b[mine], slice(None), slice(None), slice(None), t[mine] // 2)
+        at = (slice(None), page[mine], slice(None), b[mine], slice(None), t[mine] // 2)
         was = s["v_codes"][at]
         s["v_codes"][at] = was & 0xF0 | vc[mine] if half == 0 else was & 0x0F | vc[mine] << 4
     return _plain_read(s)
@@ -452,9 +451,8 @@ def _plain_read(s):
     page, b, t = _places(s)
     k = s["k_codes"][:, page, :, b, :, t]  # [n, L, H, D / 32, 16]
     k = _values(torch.stack([k & 15, k >> 4], -1)).flatten(-2) * _scales(s["k_scale"][:, page, :, b, t])[..., None]
-    v = s["v_codes"][:, page, :, b, :, :, :, t // 2]  # [n, L, H, D / 64, 32, 2]
-    v = torch.where((t % 2 == 0).view(-1, 1, 1, 1, 1, 1), v & 15, v >> 4).transpose(-1, -2).flatten(-3)
-    v = _values(v) * _scales(s["v_scale"][:, page, :, b, t])[..., None]
+    v = s["v_codes"][:, page, :, b, :, t // 2]  # [n, L, H, D]
+    v = _values(torch.where((t % 2 == 0).view(-1, 1, 1, 1), v & 15, v >> 4)) * _scales(s["v_scale"][:, page, :, b, t])[..., None]
     td = s["k_out"].dtype
     return dict(k=k.flatten(-2).transpose(0, 1).to(td), v=v.transpose(0, 1).to(td))
 
@@ -464,7 +462,7 @@ def _natural(s, table):
     k, v = s["k_codes"][:, table], s["v_codes"][:, table]  # [L, R, W, H, B, ...]
     k = _values(torch.stack([k & 15, k >> 4], -1)).flatten(-2).transpose(-2, -3)  # [.., 16, D / 32, 32]
     k = (k * _scales(s["k_scale"][:, table])[..., None]).flatten(-2)
-    v = _values(torch.stack([v & 15, v >> 4], -1)).flatten(-2).transpose(-2, -3).flatten(-4, -2).transpose(-1, -2)  # [.., 16, D]
+    v = _values(torch.stack([v & 15, v >> 4], -1)).flatten(-2).transpose(-1, -2)  # [.., 16, D]
     v = v * _scales(s["v_scale"][:, table])[..., None]
     return k.transpose(2, 3).flatten(3, 5), v.transpose(2, 3).flatten(3, 5)
 
@@ -690,7 +688,7 @@ def _exact_read(s):
         for h in range(c["hkv"]):
             byte = kc[page[:, None], h, b[:, None], d // 32, t[:, None], d % 32 // 2]
             out["k"][l, :, h] = level[byte >> (d % 2 * 4) & 15] * 2.0 ** (ks[page[:, None], h, b[:, None], t[:, None], d // 32] - 127.0)
-            byte = vc[page[:, None], h, b[:, None], d // 64, d % 32, d % 64 // 32, t[:, None] // 2]
+            byte = vc[page[:, None], h, b[:, None], d, t[:, None] // 2]
             out["v"][l, :, h] = level[byte >> (t[:, None] % 2 * 4) & 15] * 2.0 ** (vs[page, h, b, t][:, None] - 127.0)
     return {k: torch.from_numpy(v) for k, v in out.items()}
 
@@ -725,7 +723,7 @@ def _exact_attend(s):
             for g in range(H):
                 byte = s["k_codes"][l][page_of, g, block_of, d // 32, w[:, None], d % 32 // 2].int()
                 kk = level[(byte >> (d % 2 * 4)) & 15] * 2.0 ** (s["k_scale"][l][page_of, g, block_of, w[:, None], d // 32].double() - 127.0)
-                byte = s["v_codes"][l][page_of, g, block_of, d // 64, d % 32, d % 64 // 32, w[:, None] // 2].int()
+                byte = s["v_codes"][l][page_of, g, block_of, d, w[:, None] // 2].int()
                 vv = level[(byte >> (w[:, None] % 2 * 4)) & 15] * 2.0 ** (s["v_scale"][l][pg, g, b, w][:, None].double() - 127.0)
                 kt = kk.t().contiguous()
                 for h in range(g * G, g * G + G):
