@@ -142,9 +142,65 @@ _ROWS = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16}
 _BYTES = {E4M3: ("torch.float8_e4m3fn", "torch.uint8"), INT8: ("torch.int8", "torch.uint8")}
 
 
-class PastaKv8:
+class _Handle:
+    """What the handles of the paged caches have in common: prepared calls, the attention's plan and the attention, their end."""
+
+    _prefix = None  # of the library's symbols
+
+    # Each operator as a prepared call (marshalled once: f() -> status) and as a call that raises.
+    def _prepared(self, name, args, keep):
+        fn, ref = getattr(self._lib, self._prefix + name), C.byref(args)
+
+        def call(_keep=(args, keep)):
+            return fn(self._h, ref)  # (destroyed meanwhile: None, which is E_STATE)
+        call.operator = self._prefix + name
+        return call
+
+    @staticmethod
+    def _now(call):
+        rc = call()
+        if rc != OK:
+            raise PastaError(rc, call.operator)
+
+    def prepare_plan(self, length, row_offsets, n_rows, *, max_request_rows=None, prefix_len=None, slot=None, n_requests=None):
+        R = n_requests if n_requests is not None else int(length.shape[0])
+        a = PlanArgs(C.sizeof(PlanArgs), 0, R, n_rows, n_rows if max_request_rows is None else max_request_rows, _p(length, _I32, (R,), "length"),
+                     _p(row_offsets, _I32, (R + 1,), "row_offsets"), _p(prefix_len, _I32, (R,), "prefix_len"), _p(slot, _I32, (n_rows,), "slot"))
+        return self._prepared("plan", a, (length, row_offsets, prefix_len, slot))
+
+    def prepare_attend(self, layer, q, out, *, lse=None, logit_cap=0.0, slopes=None, row_see=None, row_position=None, n_rows=None):
+        c = self.cfg
+        n = n_rows if n_rows is not None else int(q.shape[0])
+        shape = (n, c.n_q_heads, c.head_dim)
+        of = tuple(k for k, v in _ROWS.items() if v == c.dtype)
+        a = AttendArgs(C.sizeof(AttendArgs), 0, layer, n, logit_cap, _p(q, of, shape, "q"), _p(out, of, shape, "out"),
+                       _p(lse, _F32, (n, c.n_q_heads), "lse"), _p(slopes, _F32, (c.n_q_heads,), "slopes"),
+                       _p(row_see, ("torch.int64", "torch.uint64"), (n,), "row_see"), _p(row_position, _I32, (n,), "row_position"))
+        return self._prepared("attend", a, (q, out, lse, slopes, row_see, row_position))
+
+    def plan(self, *args, **kw):
+        self._now(self.prepare_plan(*args, **kw))
+
+    def attend(self, *args, **kw):
+        self._now(self.prepare_attend(*args, **kw))
+
+    def destroy(self):
+        if self._h is not None:
+            getattr(self._lib, self._prefix + "destroy")(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+class PastaKv8(_Handle):
     """One handle.  Buffers are device addresses (or torch tensors, which are then kept alive and checked for type, contiguity,
     size and device) owned by the caller; those that no call needs may be left out.  `stream` is a hipStream_t as an int."""
+
+    _prefix = "pasta_kv8_"
 
     def __init__(self, cfg: Config, workspace, *, page_table=None, k_codes=None, v_codes=None, k_scale=None, v_scale=None, free_pages=None,
                  slot_tag=None, slot_position=None, stream=0, workspace_bytes=None):
@@ -168,21 +224,6 @@ class PastaKv8:
             raise PastaError(rc, "pasta_kv8_create")
         self._h = h
 
-    # Each operator as a prepared call (marshalled once: f() -> status) and as a call that raises.
-    def _prepared(self, name, args, keep):
-        fn, ref = getattr(self._lib, name), C.byref(args)
-
-        def call(_keep=(args, keep)):
-            return fn(self._h, ref)  # (destroyed meanwhile: None, which is E_STATE)
-        call.operator = name
-        return call
-
-    @staticmethod
-    def _now(call):
-        rc = call()
-        if rc != OK:
-            raise PastaError(rc, call.operator)
-
     def prepare_slots(self, length, row_offsets, n_rows, slot, length_out, free_count, free_out, *, keep=None, row_tag=None, row_position=None,
                       n_requests=None):
         R = n_requests if n_requests is not None else int(length.shape[0])
@@ -190,7 +231,7 @@ class PastaKv8:
                       _p(row_offsets, _I32, (R + 1,), "row_offsets"), _p(row_tag, _U8, (n_rows,), "row_tag"),
                       _p(row_position, _I32, (n_rows,), "row_position"), _p(free_count, _I32, (1,), "free_count"), _p(slot, _I32, (n_rows,), "slot"),
                       _p(length_out, _I32, (R,), "length_out"), _p(free_out, _I32, (1,), "free_out"))
-        return self._prepared("pasta_kv8_slots", a, (length, row_offsets, slot, length_out, free_count, free_out, keep, row_tag, row_position))
+        return self._prepared("slots", a, (length, row_offsets, slot, length_out, free_count, free_out, keep, row_tag, row_position))
 
     def prepare_append(self, layer, slot, k_new, v_new, *, n_rows=None, dtype=None):
         n = n_rows if n_rows is not None else int(slot.shape[0])
@@ -200,43 +241,10 @@ class PastaKv8:
         of = tuple(k for k, v in _ROWS.items() if v == _DTYPES.get(dtype, dtype)) or None
         a = AppendArgs(C.sizeof(AppendArgs), 0, layer, n, _DTYPES.get(dtype, dtype), _p(slot, _I32, (n,), "slot"), _p(k_new, of, shape, "k_new"),
                        _p(v_new, of, shape, "v_new"))
-        return self._prepared("pasta_kv8_append", a, (slot, k_new, v_new))
-
-    def prepare_plan(self, length, row_offsets, n_rows, *, max_request_rows=None, prefix_len=None, slot=None, n_requests=None):
-        R = n_requests if n_requests is not None else int(length.shape[0])
-        a = PlanArgs(C.sizeof(PlanArgs), 0, R, n_rows, n_rows if max_request_rows is None else max_request_rows, _p(length, _I32, (R,), "length"),
-                     _p(row_offsets, _I32, (R + 1,), "row_offsets"), _p(prefix_len, _I32, (R,), "prefix_len"), _p(slot, _I32, (n_rows,), "slot"))
-        return self._prepared("pasta_kv8_plan", a, (length, row_offsets, prefix_len, slot))
-
-    def prepare_attend(self, layer, q, out, *, lse=None, logit_cap=0.0, slopes=None, row_see=None, row_position=None, n_rows=None):
-        c = self.cfg
-        n = n_rows if n_rows is not None else int(q.shape[0])
-        shape = (n, c.n_q_heads, c.head_dim)
-        of = tuple(k for k, v in _ROWS.items() if v == c.dtype)
-        a = AttendArgs(C.sizeof(AttendArgs), 0, layer, n, logit_cap, _p(q, of, shape, "q"), _p(out, of, shape, "out"),
-                       _p(lse, _F32, (n, c.n_q_heads), "lse"), _p(slopes, _F32, (c.n_q_heads,), "slopes"),
-                       _p(row_see, ("torch.int64", "torch.uint64"), (n,), "row_see"), _p(row_position, _I32, (n,), "row_position"))
-        return self._prepared("pasta_kv8_attend", a, (q, out, lse, slopes, row_see, row_position))
+        return self._prepared("append", a, (slot, k_new, v_new))
 
     def slots(self, *args, **kw):
         self._now(self.prepare_slots(*args, **kw))
 
     def append(self, *args, **kw):
         self._now(self.prepare_append(*args, **kw))
-
-    def plan(self, *args, **kw):
-        self._now(self.prepare_plan(*args, **kw))
-
-    def attend(self, *args, **kw):
-        self._now(self.prepare_attend(*args, **kw))
-
-    def destroy(self):
-        if self._h is not None:
-            self._lib.pasta_kv8_destroy(self._h)
-            self._h = None
-
-    def __del__(self):
-        try:
-            self.destroy()
-        except Exception:
-            pass
