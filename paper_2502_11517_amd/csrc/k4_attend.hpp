@@ -1,0 +1,520 @@
+// Attention over the 4-bit cache.
+//
+// Rows, units, marks and the hiding of scores are those of the 8-bit cache (k8_attend.hpp); codes and scales enter differently.  With f = |scale| * log2(e)
+// and 2^ev_j the scale of token j's V, all scores in log2 units:
+//
+//   t_j = f * (q . K_j)   (capped, lowered by distance)       m ~ max (t_j + ev_j)         y_j = 2^(t_j + ev - m)
+//   l   = 2^-ev sum y_j       O = sum y_j 2^(ev_j - ev) V4_j       out = O / l             lse = ln 2 * (m + log2 l)
+//
+// ev is the largest ev_j of 16 tokens.
+//   q . K   bf16 operands.  A code times its scale is a bf16 number, which one conversion gives of two codes: K's scales, one to a token and 32 dims, cost
+//           nothing.  bf16 rows of q enter as they are; fp16's 11 bits as two bf16 numbers, in two products.
+//   P . V   fp16 operands.  A token's V scale must stay outside of the product over tokens: a power of two up to 2^-8 below the block's largest, times which
+//           the weight, rounded to fp16 before that, stays as exact.  Where a block's scales are further apart, or one of them is further below the largest so
+//           far, or not a number, the step takes scores t_j + ev_j instead, token by token, and sums l from t_j apart (rare: V's rows of a model differ by
+//           a few powers of two).
+// Weights rounded to fp16, at most 2^-11 of each, are the only rounding that fp32 does not see.
+//
+// Products are transposed, S^T = K Q^T and O^T = V^T P^T, in 32x32x16 steps over 32 tokens x 32 stacked rows.  A lane's piece of K is 16 bytes, the 32 dims of
+// one token under one scale; its piece of V 16 bytes, two neighbouring dims of a block's 16 tokens, which go to two products' rows: the dims of a product are
+// every second of 64.  The scores that a lane gets (16 tokens of one block, one row) are its operand of the second product, as in the 8-bit cache.
+#pragma once
+#include "k4_dev.hpp"
+#include "k8_attend.hpp"
+
+namespace k4 {
+
+struct AttendArgs : k8::AttendArgs {
+  const uint8_t *k_scale, *v_scale;  // of the layer
+};
+
+constexpr int kNear = 8;      // powers of two between a block's V scales that its weights bear
+constexpr float kLift = 7.f;  // The base of the scores is set 2^7 below their maximum and follows when that is 2^15 ahead, which fp16 still holds: so its
+                              // smallest normal number is 2^-21 of the largest weight or less, times 2^kNear where that is one of a small V scale
+
+// A wave's rows of Q, as pieces of 8 dims: lane n and n + 32 hold row n, group 2x + half of the dims at 4x .. 4x + 3.
+template <int D, bool MARKS>
+__device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head, int first, Rows<D>& r, uint4v (&raw)[D / 16]) {
+  const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
+  r.real = first + n < u.n_rows;
+  const int s = u.s0 + (r.real ? first + n : 0);  // (a lane without a row computes the first one's, times 0)
+  const uint4v* p = (const uint4v*)((const uint16_t*)a.q + row_address(a, s, head) * D);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) raw[k] = p[(2 * (k >> 2) + half) * 4 + (k & 3)];
+  r.token = u.pos0 + ((first + n) >> a.g_shift);
+  r.first_token = u.pos0 + (first >> a.g_shift);
+  r.slope = a.slopes[head * a.g.G + (s & (a.g.G - 1))] * kLog2e;
+  if constexpr (MARKS) {
+    r.see = a.row_see[s >> a.g_shift];
+    r.position = (uint32_t)a.row_position[s >> a.g_shift] ^ 0x80000000u;
+  } else {
+    r.see = 0, r.position = 0;
+  }
+}
+
+// A piece of Q as operands: bf16's bits, or fp16's value as the sum of two bf16 numbers (8 bits and the rest, which is exact).
+template <int PARTS>
+__device__ inline void operands(const AttendArgs& a, bool real, const uint4v& raw, uint4v (&q)[PARTS]) {
+  if constexpr (PARTS == 1) {
+    const uint32_t sign = a.negate ? 0x80008000u : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[0][i] = real ? raw[i] ^ sign : 0u;
+  } else {
+    union { uint4v w; half8 h; } x{raw};
+    const float f = !real ? 0.f : a.negate ? -1.f : 1.f;
+    union { bf16x8 b; uint4v w; } high, low;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float y = real ? (float)x.h[i] * f : 0.f;
+      high.b[i] = (__bf16)y;
+      low.b[i] = (__bf16)(y - (float)high.b[i]);
+    }
+    q[0] = high.w, q[1] = low.w;
+  }
+}
+
+// 32 tokens whose codes and scales a lane holds its pieces of.
+template <int D>
+struct Codes {
+  uint4v k[D / 64], v[D / 64];
+  uint32_t ks;  // scales of the token of the lane's row of the first product, a byte to a group of dims
+  uint32_t vs;  // V's scales of tokens 2i, 2i + 1 of block lane >> 5, i = lane & 7
+};
+
+// Row m = 8a + 4h + b of the first product is token 4a + b of block h.
+template <int D>
+__device__ inline void load_k(const AttendArgs& a, int at0, int at1, Codes<D>& c) {
+  const int lane = threadIdx.x & 63, m = lane & 31, half = lane >> 5, token = (m >> 3) * 4 + (m & 3);
+  const int64_t at = max((m & 4) ? at1 : at0, 0), block = max(half ? at1 : at0, 0);
+  const uint8_t* from = a.k + at * kCodeBytes(D) + (half * kBlock + token) * 16;
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x) c.k[x] = *(const uint4v*)(from + x * 2 * kBlock * 16);
+  if constexpr (D == 128)
+    c.ks = *(const uint32_t*)(a.k_scale + (at * kBlock + token) * 4);
+  else
+    c.ks = *(const uint16_t*)(a.k_scale + (at * kBlock + token) * 2);
+  c.vs = *(const uint16_t*)(a.v_scale + block * kBlock + 2 * (lane & 7));
+}
+
+template <int D>
+__device__ inline void load_v(const AttendArgs& a, int at0, int at1, Codes<D>& c) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = max((lane & 32) ? at1 : at0, 0);
+  const uint8_t* from = a.v + at * kCodeBytes(D) + (lane & 31) * 16;
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x) c.v[x] = *(const uint4v*)(from + x * 512);
+}
+
+__device__ inline bf16x8 k_operand(uint32_t w, float scale) {
+  union { bf16x2 p[4]; bf16x8 v; } r;
+  r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  return r.v;
+}
+
+__device__ inline half8 v_operand(uint32_t w) {
+  union { half2v p[4]; half8 v; } r;
+  r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 0);
+  r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 1);
+  r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 2);
+  r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 3);
+  return r.v;
+}
+
+// What is known of a pair's tokens once their scales are there: lane i of each row of 16 lanes holds that of tokens 2i and 2i + 1 of its half's block.
+struct Scales {
+  float ev;      // largest exponent of the block's V scales (of none, the largest so far)
+  uint32_t low;  // 2^(ev_j - ev) of the two tokens, as fp16
+  uint32_t vs;   // their bytes; those that do not count are the block's largest
+  bool rare;     // for the wave: more than the above is needed
+  uint32_t knan; // which rows of the first product have a scale that is not a number
+};
+
+template <int D>
+__device__ inline Scales scales_of(const Codes<D>& c, int absent, int t0, int hi, int& most) {
+  Scales s;
+  const int lane = threadIdx.x & 63, base = t0 + 16 * (lane >> 5) + 2 * (lane & 7);
+  const int left = of_half(absent) ? 0 : min(max(hi - base, 0), 2);
+  const int b0 = c.vs & 255, b1 = c.vs >> 8 & 255;
+  const bool nan = (left > 0 && b0 == kNone) || (left > 1 && b1 == kNone);
+  int up = max(left > 0 && b0 != kNone ? b0 : 0, left > 1 && b1 != kNone ? b1 : 0);
+  int down = min(left > 0 && b0 != kNone ? b0 : kNone, left > 1 && b1 != kNone ? b1 : kNone);
+  up = max(up, __builtin_amdgcn_update_dpp(0, up, 0x124, 0xf, 0xf, false));  // row_ror: lanes i and i + 8 hold the same
+  down = min(down, __builtin_amdgcn_update_dpp(0, down, 0x124, 0xf, 0xf, false));
+  up = max(up, __builtin_amdgcn_update_dpp(0, up, 0x122, 0xf, 0xf, false));
+  down = min(down, __builtin_amdgcn_update_dpp(0, down, 0x122, 0xf, 0xf, false));
+  up = max(up, __builtin_amdgcn_update_dpp(0, up, 0x121, 0xf, 0xf, false));
+  down = min(down, __builtin_amdgcn_update_dpp(0, down, 0x121, 0xf, 0xf, false));
+  const auto both = __builtin_amdgcn_permlane32_swap((uint32_t)up, (uint32_t)up, false, false);
+  most = max(most, (int)max(both[0], both[1]));
+  const bool some = up > 0;
+  up = some ? up : most;
+  const int e0 = left > 0 && b0 != kNone ? b0 : up, e1 = left > 1 && b1 != kNone ? b1 : up;
+  s.ev = (float)(up - 127);
+  s.low = 0x3c003c00u - ((uint32_t)(up - e0) << 10) - ((uint32_t)(up - e1) << 26);
+  s.vs = (uint32_t)(nan && b0 == kNone && left > 0 ? kNone : e0) | (uint32_t)(nan && b1 == kNone && left > 1 ? kNone : e1) << 8;
+  s.rare = __any(nan || (some && (up - down > kNear || up < most - kScaleSpan)));
+  uint32_t knan;
+  if constexpr (D == 128) {
+    const uint32_t x = ~c.ks;  // a byte of 0 in x: 255 in ks
+    knan = (x - 0x01010101u) & ~x & 0x80808080u;
+  } else {
+    const uint32_t x = ~c.ks | 0xffff0000u;
+    knan = (x - 0x0101u) & ~x & 0x8080u;
+  }
+  s.knan = (uint32_t)__ballot(knan != 0);  // (both halves of the wave hold the same tokens' scales)
+  return s;
+}
+
+// Scores of tokens whose K reads as not a number: they are none, either.
+__device__ inline void spoil(uint32_t knan, float16v& s) {
+  if (__builtin_expect(knan == 0, 1)) return;
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (knan >> (8 * (i >> 2) + 4 * half + (i & 3)) & 1) s[i] = __builtin_nanf("");
+}
+
+// N pairs of blocks and G groups of 32 rows: their scores (times f) become the second product's operands.
+template <int D, int G, int N>
+__device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[G][N], Scales (&p)[N], half8 (&w)[G][N][2]) {
+  bool rare = false;
+#pragma unroll
+  for (int n = 0; n < N; ++n) rare |= p[n].rare;
+  float back[N], own_m[G][N], own_l[G][N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) back[n] = __builtin_amdgcn_exp2f(-p[n].ev);
+  if (__builtin_expect(rare, 0)) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        own_m[g][n] = -FLT_MAX, own_l[g][n] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[g][n][i] *= f[g][n], own_m[g][n] = fmaxf(own_m[g][n], s[g][n][i]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) own_l[g][n] += __builtin_amdgcn_exp2f(s[g][n][i] - own_m[g][n]);
+        f[g][n] = 1.f;
+      }
+      each<16>([&](auto i) {
+        const int byte = of_row<i.value / 2>((int)p[n].vs) >> (8 * (i.value & 1)) & 255;
+        const float e = byte == kNone ? p[n].ev : (float)(byte - 127);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          if (byte == kNone && s[g][n][i.value] != -INFINITY) z[g].bad = __builtin_nanf("");
+          s[g][n][i.value] += e;
+        }
+      });
+      p[n].ev = 0.f, p[n].low = 0x3c003c00u, back[n] = 0.f;
+    }
+  }
+  float m[G];
+  bool ahead = false;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    m[g] = -FLT_MAX;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float most = s[g][n][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) most = fmaxf(most, s[g][n][i]);
+      m[g] = fmaxf(m[g], fmaf(most, f[g][n], p[n].ev));
+    }
+    m[g] = fmaxf(m[g], other_half(m[g]));
+    ahead |= m[g] > z[g].m + (kSlack + kLift);
+  }
+  if (__builtin_expect(__any(ahead), 0)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float to = fmaxf(m[g] - kLift, z[g].m), h = root_exp2(z[g].m - to), alpha = h * h;
+      z[g].m = to;
+      z[g].l = z[g].l * h * h;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) z[g].o[i][k] *= alpha;
+    }
+  }
+  if (__builtin_expect(rare, 0)) {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const float h = root_exp2(own_m[g][n] - z[g].m);
+        z[g].l = fmaf(own_l[g][n] * h, h, z[g].l);
+      }
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    half2v low[8];
+    each<8>([&](auto i) {
+      union { int w; half2v h; } x{of_row<i.value>((int)p[n].low)};
+      low[i.value] = x.h;
+    });
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float off = p[n].ev - z[g].m;
+      float sum = 0.f;
+      float16v y;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        y[i] = __builtin_amdgcn_exp2f(fmaf(s[g][n][i], f[g][n], off));
+        sum += y[i];
+      }
+      z[g].l = fmaf(sum, back[n], z[g].l);
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const half2v h = __builtin_convertvector((float2v{y[i], y[i + 1]}), half2v) * low[i / 2];
+        w[g][n][i / 8][i % 8] = h[0], w[g][n][i / 8][i % 8 + 1] = h[1];
+      }
+    }
+  }
+}
+
+// One step of a wave: N pairs whose codes are in c, against G groups of 32 rows.  `ahead` is called when K may be overwritten, `behind` when V may.
+template <int D, int PARTS, int KIND, int G, int N, class Ahead, class Behind>
+__device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&r)[G], const bf16x8* q, State<D> (&z)[G], Codes<D> (&c)[N],
+                            const int (&absent)[N], const Marks (&marks)[N], const int (&t0)[N], int& most, Ahead ahead, Behind behind) {
+  float16v s[G][N];
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[g][n][i] = 0.f;
+  const int half = (threadIdx.x >> 5) & 1;
+  // A wave at the matrix pipe goes first: else the older of a SIMD's two runs ahead, and the younger ends alone.
+  __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x) {
+    float scale[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) scale[n] = __uint_as_float((c[n].ks >> (8 * (2 * x + half)) & 255u) << 23);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      bf16x8 codes[N];
+#pragma unroll
+      for (int n = 0; n < N; ++n) codes[n] = k_operand(c[n].k[x][y], scale[n]);
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+          const bf16x8 row = q[((g * PARTS + part) * (D / 16) + 4 * x + y) * 64 + (threadIdx.x & 63)];
+#pragma unroll
+          for (int n = 0; n < N; ++n) s[g][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes[n], row, s[g][n], 0, 0, 0);
+        }
+    }
+  }
+  __builtin_amdgcn_s_setprio(0);
+  Marks m[N];
+  Scales p[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) m[n] = marks[n], p[n] = scales_of<D>(c[n], absent[n], t0[n], u.hi, most);
+  ahead();
+  float f[G][N];
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      spoil(p[n].knan, s[g][n]);
+      f[g][n] = a.scale_log2;
+      const Pair pair{1.f, 0.f, absent[n], 0, 0};
+      if constexpr (KIND == kMarked)
+        finish_scores<KIND>(a, u.prefix, u.hi, t0[n], pair, Marked{m[n], r[g].position, r[g].by_tag}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
+      else
+        finish_scores<KIND>(a, u.prefix, u.hi, t0[n], pair, Unmarked{}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
+    }
+  half8 w[G][N][2];
+  k4::soften<D, G, N>(z, s, f, p, w);
+  __builtin_amdgcn_s_setprio(1);
+  __builtin_amdgcn_sched_barrier(0);  // (V's codes are turned as they are needed: all at once they take 64 registers more)
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {
+        const half8 codes = v_operand(c[n].v[x / 2][2 * (x & 1) + y]);
+#pragma unroll
+        for (int g = 0; g < G; ++g) z[g].o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, w[g][n][y], z[g].o[x], 0, 0, 0);
+      }
+  __builtin_amdgcn_s_setprio(0);
+  behind();
+}
+
+// A unit of G groups of 32 rows.  Every wave takes a quarter of the tokens, pairs wave, wave + 4, ...; the four meet at the end.  Two pairs at a time, so that a
+// softmax's way through its lanes is taken once for 64 tokens; with two groups and 128 dims there are registers for one.  Q's operands lie in LDS, a copy for
+// each wave (where its output goes later).
+template <int D, int PARTS, int KIND, int G>
+__device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
+  constexpr bool MARKS = KIND == kMarked;
+  constexpr int N = G == 1 || D == 64 ? 2 : 1;
+  static_assert(G * PARTS * (D / 16) * 64 * 16 <= kRows * kPitch<D> * 4, "Q's operands lie where the output goes");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 31, half = lane >> 5;
+  const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's
+  uint4v* q = (uint4v*)(lds + wave * kRows * kPitch<D>);
+  Rows<D> r[G];
+  State<D> z[G];
+  Blocks b;
+  uint64_t gone;
+  int most = kEMin + 127;  // largest byte of V's scales so far
+  Codes<D> c[N];
+  Marks marks[N] = {};
+  auto token = [&](int i) { return u.lo + (wave + 4 * i) * 32; };  // first of the wave's i-th pair
+  auto find = [&](int i) { find_blocks(a, u.request, head, token(i + (lane >> 1)) + (lane & 1) * 16, u.hi, b), gone = __ballot(b.at < 0); };
+  auto k_ahead = [&](int i, int to) {
+    const int x = 2 * (i & 31);
+    load_k<D>(a, __builtin_amdgcn_readlane(b.at, x), __builtin_amdgcn_readlane(b.at, x + 1), c[to]);
+  };
+  auto v_ahead = [&](int i, int to) {
+    const int x = 2 * (i & 31);
+    load_v<D>(a, __builtin_amdgcn_readlane(b.at, x), __builtin_amdgcn_readlane(b.at, x + 1), c[to]);
+  };
+  auto absent_of = [&](int i) { return (int)(gone >> (2 * (i & 31))) & 3; };
+  {
+    // Everything is asked for before anything is waited for: loads come back in their order.  (Where the wave has fewer than N pairs, block 0 is read in
+    // their place.)
+    uint4v raw[D / 16];
+    k4::request_rows<D, MARKS>(a, u, head, 0, r[0], raw);
+    __builtin_amdgcn_sched_barrier(0);
+    if (u.hi - u.lo <= kUnitBlocks * kBlock)
+      on_block(a, 2 * (wave + 4 * (lane >> 1)) + (lane & 1) < kUnitBlocks ? listed : -1, head, b), gone = __ballot(b.at < 0);
+    else
+      find(0);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if constexpr (MARKS) marks[n] = load_marks(a, b, n);
+#pragma unroll
+    for (int n = 0; n < N; ++n) k_ahead(n, n);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v_ahead(n, n);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (g) k4::request_rows<D, MARKS>(a, u, head, g * kRows, r[g], raw);
+      if constexpr (MARKS) r[g].by_tag = rows_by_tag(r[g].see, a.g_shift);
+#pragma unroll
+      for (int y = 0; y < D / 16; ++y) {
+        uint4v x[PARTS];
+        operands<PARTS>(a, r[g].real, raw[y], x);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) q[((g * PARTS + part) * (D / 16) + y) * 64 + lane] = x[part];
+      }
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) start(z[g]);
+  int i = 0;
+  for (; i + N - 1 < n_pairs; i += N) {
+    int t0[N], absent[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) t0[n] = token(i + n), absent[n] = absent_of(i + n);
+    k4::step<D, PARTS, KIND, G, N>(a, u, r, (const bf16x8*)q, z, c, absent, marks, t0, most,
+      [&] {
+        if (i + N >= n_pairs) return;
+        if (((i + N) & 31) == 0) find(i + N);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if constexpr (MARKS) marks[n] = load_marks(a, b, (i + N + n) & 31);
+#pragma unroll
+        for (int n = 0; n < N; ++n) k_ahead(i + N + n, n);
+      },
+      [&] {
+        if (i + N >= n_pairs) return;
+#pragma unroll
+        for (int n = 0; n < N; ++n) v_ahead(i + N + n, n);
+      });
+  }
+  if constexpr (N == 2) {
+    if (i < n_pairs) {
+      const int t0[1] = {token(i)}, absent[1] = {absent_of(i)};
+      const Marks last[1] = {marks[0]};
+      k4::step<D, PARTS, KIND, G, 1>(a, u, r, (const bf16x8*)q, z, *(Codes<D>(*)[1]) & c, absent, last, t0, most, [] {}, [] {});
+    }
+  }
+  // the four waves meet, group after group
+  float* s_o = lds;                                         // [4][32][kPitch]
+  float2v* s_ml = (float2v*)(lds + 4 * kRows * kPitch<D>);  // [4][32]
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    if (g && u.n_rows <= g * kRows) break;
+    const float l = z[g].l + other_half(z[g].l);
+    poison(z[g]);
+    if (g) __syncthreads();
+    if (half == 0) s_ml[wave * kRows + row] = float2v{z[g].m, l};
+    if (r[g].real) {
+      // o[2X + j][4y + b] is dim 64 X + 2 (8y + 4 half + b) + j
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int k = 0; k < 4; k += 2)
+            *(float4v*)(s_o + (wave * kRows + row) * kPitch<D> + 64 * x + 2 * (8 * y + 4 * half + k)) =
+                float4v{z[g].o[2 * x][4 * y + k], z[g].o[2 * x + 1][4 * y + k], z[g].o[2 * x][4 * y + k + 1], z[g].o[2 * x + 1][4 * y + k + 1]};
+    }
+    __syncthreads();
+    // a thread takes the same four dims of several rows; what lies in LDS is read for rows that there are not, too
+    constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;
+    const int i0 = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4, rows = min(u.n_rows - g * kRows, kRows);
+#pragma unroll
+    for (int j = 0; j < kRows / kAtOnce; ++j) {
+      const int i = i0 + j * kAtOnce;
+      float2v ml[4];
+      float4v part[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) ml[w] = s_ml[w * kRows + i], part[w] = *(const float4v*)(s_o + (w * kRows + i) * kPitch<D> + d);
+      const float m = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
+      float all = 0.f;
+      float4v o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float h = root_exp2(ml[w][0] - m);
+        all = fmaf(ml[w][1] * h, h, all);
+        o += part[w] * (h * h);
+      }
+      if (i >= rows) continue;
+      if (u.part < 0) {
+        const int64_t to = row_address(a, u.s0 + g * kRows + i, head);
+        store_out(a, to * D + d, o * inverse_of(all));
+        if (a.lse && d == 0) a.lse[to] = lse_of(m, all);
+      } else {
+        const int64_t to = (int64_t)(u.part + g * kRows + i) * a.g.Hkv + head;
+        *(float4v*)(a.part_acc + to * D + d) = o;
+        if (d == 0) a.part_ml[to] = float2v{m, all};
+      }
+    }
+  }
+}
+
+// A work-group (blockIdx.y) takes each of a tile's two groups.
+template <int D, int PARTS, int KIND>
+constexpr bool kApart = true;
+
+template <int D, int PARTS, bool MANY, int KIND>
+__global__ __launch_bounds__(256, 2) void k4_attend(AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) float lds[4 * kRows * kPitch<D> + 4 * kRows * 2];
+  const int head = blockIdx.x % a.g.Hkv, unit = blockIdx.x / a.g.Hkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Unit u = a.units[unit];
+  // the lane's block, asked for together with the unit: pairs are dealt out to the four waves
+  const int listed = a.unit_blocks[unit * kUnitBlocks + min(2 * (wave + 4 * (lane >> 1)) + (lane & 1), kUnitBlocks - 1)];
+  asm volatile("" ::"s"(u.request), "s"(u.s0), "s"(u.pos0), "s"(u.lo), "s"(u.hi), "s"(u.prefix), "s"(u.part));  // (one load, ahead of the branch)
+  if constexpr (MANY && kApart<D, PARTS, KIND>) {
+    const int first = blockIdx.y * kRows;
+    u.s0 += first, u.n_rows = min(u.n_rows - first, kRows), u.pos0 += first >> a.g_shift;
+    if (u.part >= 0) u.part += first;
+  }
+  if (u.n_rows <= 0) return;
+  if constexpr (MANY && !kApart<D, PARTS, KIND>) {
+    if (u.n_rows > kRows)
+      k4::attend_unit<D, PARTS, KIND, 2>(a, u, listed, head, lds);
+    else
+      k4::attend_unit<D, PARTS, KIND, 1>(a, u, listed, head, lds);
+  } else {
+    k4::attend_unit<D, PARTS, KIND, 1>(a, u, listed, head, lds);
+  }
+}
+
+}  // namespace k4

@@ -1,0 +1,247 @@
+// New rows of one layer into the 4-bit cache, and rows back out of it.
+//
+// A wave takes a run, at most 16 neighbouring rows that lie in neighbouring slots of one block, of one kv head, K or V.  A row's scales depend on that row
+// alone, so nothing that was written before is rounded again.
+//   K  a lane has a quarter of a token's dims: with D = 128 those of one scale, with 64 half of them
+//   V  a lane has D / 64 neighbouring dims of all 16 tokens, whose codes lie together; a token's magnitudes are compared across the wave.  Codes of two
+//      tokens share a byte, so those of the block's other tokens are read and put back.
+#pragma once
+#include "k4_dev.hpp"
+#include "k8_append.hpp"
+
+namespace k4 {
+
+struct RowArgs {
+  Geometry g;
+  int n_rows, group;  // rows that a work-group looks at
+  const int* slot;
+  int64_t k_stride, v_stride;    // of the rows, in values
+  const void *k_new, *v_new;     // into the cache
+  void *k_out, *v_out;           // out of it
+  uint8_t *k, *v, *ks, *vs;
+};
+
+// f(first row, rows, token of the first, block) for every run that begins within the work-group's rows.
+template <class F>
+__device__ inline void each_run(const RowArgs& a, int head, F f) {
+  const int lane = threadIdx.x & 63, n_slots = a.g.n_pages << a.g.page_shift;
+  const int first = blockIdx.x * a.group, last = min(first + a.group, a.n_rows);
+  // lane k: the slot of row first + k - 1; a run that begins within the group ends within 16 more rows
+  const int row = first + lane - 1;
+  const int mine = lane <= a.group + kBlock && row >= 0 && row < a.n_rows ? a.slot[row] : -1;
+  int i = first;
+  while (i < last) {
+    const int at = i - first + 1, prev = __builtin_amdgcn_readlane(mine, at - 1), slot = __builtin_amdgcn_readlane(mine, at);
+    if (slot < 0 || slot >= n_slots) {
+      ++i;
+      continue;
+    }
+    const bool goes_on = lane >= at && mine == slot + lane - at && (mine >> 4) == (slot >> 4);
+    const int n = __builtin_ctzll(~(__ballot(goes_on) >> at));
+    if (!(prev >= 0 && slot == prev + 1 && (slot & 15))) {  // the run begins here
+      const int page = slot >> a.g.page_shift, b = (slot & (a.g.page_tokens - 1)) >> 4;
+      f(i, n, slot & 15, ((int64_t)page * a.g.Hkv + head) * a.g.blocks_per_page + b);
+    }
+    i += n;
+  }
+}
+
+template <int D, int IN>
+__device__ inline void append_k(const RowArgs& a, int row, int n, int offset, int head, int64_t block) {
+  constexpr int N = D / 4;
+  const int lane = threadIdx.x & 63, i = lane >> 2, part = lane & 3, token = offset + i;
+  float x[N];
+  load_row<IN, N>(a.k_new, (int64_t)(row + min(i, n - 1)) * a.k_stride + head * D + part * N, x);
+  uint32_t amax = magnitude(x, 0);
+  if constexpr (D == 64) amax = max(amax, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0xb1, 0xf, 0xf, false));  // of lane ^ 1
+  const int byte = scale_byte(amax);
+  const float inverse = inverse_scale(byte);
+  uint32_t w[N / 8];
+#pragma unroll
+  for (int j = 0; j < N; ++j) x[j] = byte == kNone ? 0.f : x[j] * inverse;
+#pragma unroll
+  for (int j = 0; j < N / 8; ++j) w[j] = encode8(x + 8 * j);
+  if (i >= n) return;
+  const int dim = part * N;
+  uint8_t* to = a.k + block * kCodeBytes(D) + (dim / kGroup * kBlock + token) * 16 + dim % kGroup / 2;
+  if constexpr (D == 128) {
+    *(uint4v*)to = uint4v{w[0], w[1], w[2], w[3]};
+    a.ks[(block * kBlock + token) * 4 + part] = (uint8_t)byte;
+  } else {
+    *(uint2v*)to = uint2v{w[0], w[1]};
+    if ((part & 1) == 0) a.ks[(block * kBlock + token) * 2 + part / 2] = (uint8_t)byte;
+  }
+}
+
+// Bytes 0 .. 7 of a dim's codes, whose tokens lie in [from, from + n): 255 in each half of them.
+__device__ inline uint2v tokens_mask(int from, int n) {
+  const uint64_t all = ~0ull;
+  const uint64_t m = (all >> (64 - 4 * n)) << (4 * from);  // 1 <= n, from + n <= 16
+  return uint2v{(uint32_t)m, (uint32_t)(m >> 32)};
+}
+
+template <int D, int IN>
+__device__ inline void append_v(const RowArgs& a, int row, int n, int offset, int head, int64_t block) {
+  constexpr int N = D / 64;
+  const int lane = threadIdx.x & 63;
+  uint2v* codes = (uint2v*)(a.v + block * kCodeBytes(D)) + lane * N;
+  float x[kBlock][N];
+  // Places without a row get the nearest one's and are dropped below: loads under branches wait for one another.
+#pragma unroll
+  for (int t = 0; t < kBlock; ++t) load_row<IN, N>(a.v_new, (int64_t)(row + min(max(t - offset, 0), n - 1)) * a.v_stride + head * D + lane * N, x[t]);
+  uint2v old[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) old[j] = uint2v{0, 0};
+  if (n < kBlock)
+#pragma unroll
+    for (int j = 0; j < N; ++j) old[j] = codes[j];
+  int byte = 0;  // lane t: of token t
+#pragma unroll
+  for (int t = 0; t < kBlock; ++t) {
+    if (t < offset || t >= offset + n) continue;  // (the same for the whole wave)
+    const int b = scale_byte(wave_max(magnitude(x[t], 0)));
+    const float inverse = inverse_scale(b);
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[t][j] = b == kNone ? 0.f : x[t][j] * inverse;
+    byte = lane == t ? b : byte;
+  }
+  const uint2v mine = tokens_mask(offset, n);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    uint2v w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = x[8 * i + k][j];
+      w[i] = (encode8(y) & mine[i]) | (old[j][i] & ~mine[i]);
+    }
+    codes[j] = w;
+  }
+  if (lane >= offset && lane < offset + n) a.vs[block * kBlock + lane] = (uint8_t)byte;
+}
+
+template <int D, int IN>
+__global__ __launch_bounds__(256) void k4_append(RowArgs a) {
+  const int task = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = task >> 1;
+  if (head >= a.g.Hkv) return;
+  each_run(a, head, [&](int row, int n, int offset, int64_t block) {
+    if (task & 1)
+      append_v<D, IN>(a, row, n, offset, head, block);
+    else
+      append_k<D, IN>(a, row, n, offset, head, block);
+  });
+}
+
+// N neighbouring values of a row.
+template <int OUT, int N>
+__device__ inline void store_row(void* base, int64_t at, const float (&x)[N]) {
+  if constexpr (OUT == kF32) {
+    float* p = (float*)base + at;
+    if constexpr (N >= 4) {
+      for (int i = 0; i < N; i += 4) *(float4v*)(p + i) = float4v{x[i], x[i + 1], x[i + 2], x[i + 3]};
+    } else if constexpr (N == 2) {
+      *(float2v*)p = float2v{x[0], x[1]};
+    } else {
+      *p = x[0];
+    }
+  } else {
+    // bf16 holds every code times a power of two: its upper half is the value, not a number included
+    uint16_t b[N];
+    for (int i = 0; i < N; ++i) {
+      if constexpr (OUT == kBf16) {
+        b[i] = (uint16_t)(__float_as_uint(x[i]) >> 16);
+      } else {
+        union { _Float16 h; uint16_t u; } c{(_Float16)x[i]};
+        b[i] = c.u;
+      }
+    }
+    uint16_t* p = (uint16_t*)base + at;
+    if constexpr (N >= 8) {
+      for (int i = 0; i < N; i += 8) {
+        uint4v w;
+        for (int k = 0; k < 4; ++k) w[k] = b[i + 2 * k] | (uint32_t)b[i + 2 * k + 1] << 16;
+        *(uint4v*)(p + i) = w;
+      }
+    } else if constexpr (N == 2) {
+      *(uint32_t*)p = b[0] | (uint32_t)b[1] << 16;
+    } else {
+      *p = b[0];
+    }
+  }
+}
+
+__device__ inline float scale_of(int byte) {  // (2^-127 is a subnormal number of fp32)
+  return byte == kNone ? __builtin_nanf("") : __uint_as_float(byte ? (uint32_t)byte << 23 : 0x400000u);
+}
+
+template <int D, int OUT>
+__device__ inline void read_k(const RowArgs& a, int row, int n, int offset, int head, int64_t block) {
+  constexpr int N = D / 4;
+  const int lane = threadIdx.x & 63, i = min(lane >> 2, n - 1), part = lane & 3, dim = part * N;
+  const uint8_t* from = a.k + block * kCodeBytes(D) + (dim / kGroup * kBlock + offset + i) * 16 + dim % kGroup / 2;
+  uint32_t w[N / 8];
+  if constexpr (D == 128) {
+    const uint4v t = *(const uint4v*)from;
+    for (int j = 0; j < 4; ++j) w[j] = t[j];
+  } else {
+    const uint2v t = *(const uint2v*)from;
+    w[0] = t[0], w[1] = t[1];
+  }
+  const float scale = scale_of(a.ks[(block * kBlock + offset + i) * (D / kGroup) + dim / kGroup]);
+  if ((lane >> 2) >= n) return;
+  float x[N];
+#pragma unroll
+  for (int j = 0; j < N / 8; ++j) {
+    float y[8];
+    decode8(w[j], y);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[8 * j + k] = y[k] * scale;
+  }
+  store_row<OUT, N>(a.k_out, (int64_t)(row + i) * a.k_stride + head * D + dim, x);
+}
+
+template <int D, int OUT>
+__device__ inline void read_v(const RowArgs& a, int row, int n, int offset, int head, int64_t block) {
+  constexpr int N = D / 64;
+  const int lane = threadIdx.x & 63;
+  const uint2v* codes = (const uint2v*)(a.v + block * kCodeBytes(D)) + lane * N;
+  uint2v w[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) w[j] = codes[j];
+  const int bytes = a.vs[block * kBlock + (lane & 15)];
+  float x[kBlock][N];
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float y[8];
+      decode8(w[j][i], y);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[8 * i + k][j] = y[k];
+    }
+#pragma unroll
+  for (int t = 0; t < kBlock; ++t) {
+    if (t < offset || t >= offset + n) continue;  // (the same for the whole wave)
+    const float scale = scale_of(__builtin_amdgcn_readlane(bytes, t));
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[t][j] *= scale;
+    store_row<OUT, N>(a.v_out, (int64_t)(row + t - offset) * a.v_stride + head * D + lane * N, x[t]);
+  }
+}
+
+// Tasks: kv heads times K and V, or one of them where only that is wanted.
+template <int D, int OUT>
+__global__ __launch_bounds__(256) void k4_read(RowArgs a) {
+  const bool both = a.k_out && a.v_out;
+  const int task = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = both ? task >> 1 : task;
+  if (head >= a.g.Hkv) return;
+  each_run(a, head, [&](int row, int n, int offset, int64_t block) {
+    if (both ? task & 1 : !a.k_out)
+      read_v<D, OUT>(a, row, n, offset, head, block);
+    else
+      read_k<D, OUT>(a, row, n, offset, head, block);
+  });
+}
+
+}  // namespace k4
