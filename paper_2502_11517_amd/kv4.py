@@ -9,7 +9,7 @@ import os
 import subprocess
 
 from .binding import BF16, E_CAPACITY, E_DEVICE, E_INVAL, E_NOMEM, E_STATE, F32, HIPCC_FLAGS, OK, PastaError  # noqa: F401
-from .kv8 import _DTYPES, _I32, _ROWS, _U8, BLOCK, F16, AttendArgs, PlanArgs, _Handle, _p  # noqa: F401
+from .kv8 import _DTYPES, _I32, _ROWS, _U8, BLOCK, F16, AttendArgs, PlanArgs, _Attention, _p  # noqa: F401
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = os.path.join(_HERE, "libpasta_kv4.so")
@@ -100,7 +100,7 @@ def cache_shapes(cfg: Config):
             (*block, BLOCK))
 
 
-class PastaKv4(_Handle):
+class PastaKv4(_Attention):
     """One handle.  Buffers are device addresses (or torch tensors, which are then kept alive and checked for type, contiguity,
     size and device) owned by the caller; those that no call needs may be left out.  `stream` is a hipStream_t as an int."""
 

@@ -143,7 +143,7 @@ _BYTES = {E4M3: ("torch.float8_e4m3fn", "torch.uint8"), INT8: ("torch.int8", "to
 
 
 class _Handle:
-    """What the handles of the paged caches have in common: prepared calls, the attention's plan and the attention, their end."""
+    """What handles have in common: prepared calls and their end."""
 
     _prefix = None  # of the library's symbols
 
@@ -161,6 +161,21 @@ class _Handle:
         rc = call()
         if rc != OK:
             raise PastaError(rc, call.operator)
+
+    def destroy(self):
+        if self._h is not None:
+            getattr(self._lib, self._prefix + "destroy")(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+class _Attention(_Handle):
+    """Plan and attention, alike for every paged cache."""
 
     def prepare_plan(self, length, row_offsets, n_rows, *, max_request_rows=None, prefix_len=None, slot=None, n_requests=None):
         R = n_requests if n_requests is not None else int(length.shape[0])
@@ -184,19 +199,8 @@ class _Handle:
     def attend(self, *args, **kw):
         self._now(self.prepare_attend(*args, **kw))
 
-    def destroy(self):
-        if self._h is not None:
-            getattr(self._lib, self._prefix + "destroy")(self._h)
-            self._h = None
 
-    def __del__(self):
-        try:
-            self.destroy()
-        except Exception:
-            pass
-
-
-class PastaKv8(_Handle):
+class PastaKv8(_Attention):
     """One handle.  Buffers are device addresses (or torch tensors, which are then kept alive and checked for type, contiguity,
     size and device) owned by the caller; those that no call needs may be left out.  `stream` is a hipStream_t as an int."""
 
