@@ -8,7 +8,7 @@
 //
 // ev is the largest ev_j of 16 tokens.
 //   q . K   bf16 operands.  A code times its scale is a bf16 number, which one conversion gives of two codes: K's scales, one to a token and 32 dims, cost
-//           nothing.  bf16 rows of q enter as they are; fp16's 11 bits as two bf16 numbers, in two products.
+//           nothing (and 255 among them gives numbers that are none).  bf16 rows of q enter as they are; fp16's 11 bits as two bf16 numbers, in two products.
 //   P . V   fp16 operands.  A token's V scale must stay outside of the product over tokens: a power of two up to 2^-8 below the block's largest, times which
 //           the weight, rounded to fp16 before that, stays as exact.  Where a block's scales are further apart, or one of them is further below the largest so
 //           far, or not a number, the step takes scores t_j + ev_j instead, token by token, and sums l from t_j apart (rare: V's rows of a model differ by
@@ -37,7 +37,7 @@ template <int D, bool MARKS>
 __device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head, int first, Rows<D>& r, uint4v (&raw)[D / 16]) {
   const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
   r.real = first + n < u.n_rows;
-  const int s = u.s0 + (r.real ? first + n : 0);  // (a lane without a row computes the first one's, times 0)
+  const int s = u.s0 + (r.real ? first + n : 0);  // (a lane without a row computes the first one's, and nobody looks)
   const uint4v* p = (const uint4v*)((const uint16_t*)a.q + row_address(a, s, head) * D);
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) raw[k] = p[(2 * (k >> 2) + half) * 4 + (k & 3)];
@@ -54,22 +54,23 @@ __device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head
 
 // A piece of Q as operands: bf16's bits, or fp16's value as the sum of two bf16 numbers (8 bits and the rest, which is exact).
 template <int PARTS>
-__device__ inline void operands(const AttendArgs& a, bool real, const uint4v& raw, uint4v (&q)[PARTS]) {
+__device__ inline void operands(bool negate, const uint4v& raw, uint4v (&q)[PARTS]) {
   if constexpr (PARTS == 1) {
-    const uint32_t sign = a.negate ? 0x80008000u : 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q[0][i] = real ? raw[i] ^ sign : 0u;
+    q[0] = raw;
   } else {
     union { uint4v w; half8 h; } x{raw};
-    const float f = !real ? 0.f : a.negate ? -1.f : 1.f;
     union { bf16x8 b; uint4v w; } high, low;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float y = real ? (float)x.h[i] * f : 0.f;
+      const float y = (float)x.h[i];
       high.b[i] = (__bf16)y;
       low.b[i] = (__bf16)(y - (float)high.b[i]);
     }
     q[0] = high.w, q[1] = low.w;
+  }
+  if (__builtin_expect(negate, 0)) {  // (the same for all lanes)
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) q[p] ^= uint4v{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
   }
 }
 
@@ -129,52 +130,40 @@ struct Scales {
   uint32_t low;  // 2^(ev_j - ev) of the two tokens, as fp16
   uint32_t vs;   // their bytes; those that do not count are the block's largest
   bool rare;     // for the wave: more than the above is needed
-  uint32_t knan; // which rows of the first product have a scale that is not a number
 };
+
+__device__ inline int row_largest(int x) {  // of a row of 16 lanes, of which i and i + 8 hold the same
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xf, 0xf, false));  // row_ror
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xf, 0xf, false));
+  return max(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, false));
+}
 
 template <int D>
 __device__ inline Scales scales_of(const Codes<D>& c, int absent, int t0, int hi, int& most) {
   Scales s;
-  const int lane = threadIdx.x & 63, base = t0 + 16 * (lane >> 5) + 2 * (lane & 7);
-  const int left = of_half(absent) ? 0 : min(max(hi - base, 0), 2);
-  const int b0 = c.vs & 255, b1 = c.vs >> 8 & 255;
-  const bool nan = (left > 0 && b0 == kNone) || (left > 1 && b1 == kNone);
-  int up = max(left > 0 && b0 != kNone ? b0 : 0, left > 1 && b1 != kNone ? b1 : 0);
-  int down = min(left > 0 && b0 != kNone ? b0 : kNone, left > 1 && b1 != kNone ? b1 : kNone);
-  up = max(up, __builtin_amdgcn_update_dpp(0, up, 0x124, 0xf, 0xf, false));  // row_ror: lanes i and i + 8 hold the same
-  down = min(down, __builtin_amdgcn_update_dpp(0, down, 0x124, 0xf, 0xf, false));
-  up = max(up, __builtin_amdgcn_update_dpp(0, up, 0x122, 0xf, 0xf, false));
-  down = min(down, __builtin_amdgcn_update_dpp(0, down, 0x122, 0xf, 0xf, false));
-  up = max(up, __builtin_amdgcn_update_dpp(0, up, 0x121, 0xf, 0xf, false));
-  down = min(down, __builtin_amdgcn_update_dpp(0, down, 0x121, 0xf, 0xf, false));
-  const auto both = __builtin_amdgcn_permlane32_swap((uint32_t)up, (uint32_t)up, false, false);
-  most = max(most, (int)max(both[0], both[1]));
-  const bool some = up > 0;
-  up = some ? up : most;
-  const int e0 = left > 0 && b0 != kNone ? b0 : up, e1 = left > 1 && b1 != kNone ? b1 : up;
-  s.ev = (float)(up - 127);
-  s.low = 0x3c003c00u - ((uint32_t)(up - e0) << 10) - ((uint32_t)(up - e1) << 26);
-  s.vs = (uint32_t)(nan && b0 == kNone && left > 0 ? kNone : e0) | (uint32_t)(nan && b1 == kNone && left > 1 ? kNone : e1) << 8;
-  s.rare = __any(nan || (some && (up - down > kNear || up < most - kScaleSpan)));
-  uint32_t knan;
-  if constexpr (D == 128) {
-    const uint32_t x = ~c.ks;  // a byte of 0 in x: 255 in ks
-    knan = (x - 0x01010101u) & ~x & 0x80808080u;
+  int b0 = c.vs & 255, b1 = c.vs >> 8;
+  bool some = true, nan = false;
+  int up = row_largest(max(b0, b1));
+  const bool cut = t0 + 32 > hi || absent, all = !__any(up == kNone) && !cut;  // (the same for the whole wave)
+  if (__builtin_expect(!all, 0)) {  // tokens that there are not, or whose V is not a number, are left out: they get the largest of the others
+    const int left = of_half(absent) ? 0 : min(max(hi - (t0 + 16 * (int)(threadIdx.x >> 5 & 1) + 2 * (int)(threadIdx.x & 7)), 0), 2);
+    const bool n0 = left > 0 && b0 == kNone, n1 = left > 1 && b1 == kNone;
+    up = row_largest(max(left > 0 && !n0 ? b0 : 0, left > 1 && !n1 ? b1 : 0));
+    some = up > 0, nan = n0 || n1;
+    const auto both = __builtin_amdgcn_permlane32_swap((uint32_t)up, (uint32_t)up, false, false);
+    most = max(most, (int)max(both[0], both[1]));
+    up = some ? up : most;
+    s.vs = (uint32_t)(n0 || left < 1 ? (n0 ? kNone : up) : b0) | (uint32_t)(n1 || left < 2 ? (n1 ? kNone : up) : b1) << 8;
+    b0 = left < 1 || n0 ? up : b0, b1 = left < 2 || n1 ? up : b1;
   } else {
-    const uint32_t x = ~c.ks | 0xffff0000u;
-    knan = (x - 0x0101u) & ~x & 0x8080u;
+    const auto both = __builtin_amdgcn_permlane32_swap((uint32_t)up, (uint32_t)up, false, false);
+    most = max(most, (int)max(both[0], both[1]));
+    s.vs = c.vs;
   }
-  s.knan = (uint32_t)__ballot(knan != 0);  // (both halves of the wave hold the same tokens' scales)
+  s.ev = (float)(up - 127);
+  s.low = 0x3c003c00u - ((uint32_t)(up - b0) << 10) - ((uint32_t)(up - b1) << 26);
+  s.rare = __any(nan || max(up - b0, up - b1) > kNear || (some && up < most - kScaleSpan));
   return s;
-}
-
-// Scores of tokens whose K reads as not a number: they are none, either.
-__device__ inline void spoil(uint32_t knan, float16v& s) {
-  if (__builtin_expect(knan == 0, 1)) return;
-  const int half = (threadIdx.x >> 5) & 1;
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (knan >> (8 * (i >> 2) + 4 * half + (i & 3)) & 1) s[i] = __builtin_nanf("");
 }
 
 // N pairs of blocks and G groups of 32 rows: their scores (times f) become the second product's operands.
@@ -195,7 +184,10 @@ __device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[g][n][i] *= f[g][n], own_m[g][n] = fmaxf(own_m[g][n], s[g][n][i]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) own_l[g][n] += __builtin_amdgcn_exp2f(s[g][n][i] - own_m[g][n]);
+        for (int i = 0; i < 16; ++i) {
+          own_l[g][n] += __builtin_amdgcn_exp2f(s[g][n][i] - own_m[g][n]);
+          __builtin_amdgcn_sched_barrier(0);  // (one after the other, or registers run out)
+        }
         f[g][n] = 1.f;
       }
       each<16>([&](auto i) {
@@ -203,9 +195,11 @@ __device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[
         const float e = byte == kNone ? p[n].ev : (float)(byte - 127);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          if (byte == kNone && s[g][n][i.value] != -INFINITY) z[g].bad = __builtin_nanf("");
+          const int seen = byte == kNone && s[g][n][i.value] != -INFINITY ? 0x7fc00000 : 0;  // (without a branch)
+          z[g].bad = __uint_as_float(__float_as_uint(z[g].bad) | seen);
           s[g][n][i.value] += e;
         }
+        __builtin_amdgcn_sched_barrier(0);
       });
       p[n].ev = 0.f, p[n].low = 0x3c003c00u, back[n] = 0.f;
     }
@@ -229,8 +223,10 @@ __device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const float to = fmaxf(m[g] - kLift, z[g].m), h = root_exp2(z[g].m - to), alpha = h * h;
+      const bool fresh = z[g].m == -FLT_MAX;  // (nothing so far)
       z[g].m = to;
       z[g].l = z[g].l * h * h;
+      if (__all(fresh)) continue;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -248,28 +244,22 @@ __device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    half2v low[8];
+    float off[G], sum[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) off[g] = p[n].ev - z[g].m, sum[g] = 0.f;
     each<8>([&](auto i) {
-      union { int w; half2v h; } x{of_row<i.value>((int)p[n].low)};
-      low[i.value] = x.h;
+      union { int w; half2v h; } low{of_row<i.value>((int)p[n].low)};
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const float y0 = __builtin_amdgcn_exp2f(fmaf(s[g][n][2 * i.value], f[g][n], off[g]));
+        const float y1 = __builtin_amdgcn_exp2f(fmaf(s[g][n][2 * i.value + 1], f[g][n], off[g]));
+        sum[g] += y0, sum[g] += y1;
+        const half2v h = __builtin_convertvector((float2v{y0, y1}), half2v) * low.h;
+        w[g][n][i.value / 4][2 * i.value % 8] = h[0], w[g][n][i.value / 4][2 * i.value % 8 + 1] = h[1];
+      }
     });
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const float off = p[n].ev - z[g].m;
-      float sum = 0.f;
-      float16v y;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        y[i] = __builtin_amdgcn_exp2f(fmaf(s[g][n][i], f[g][n], off));
-        sum += y[i];
-      }
-      z[g].l = fmaf(sum, back[n], z[g].l);
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const half2v h = __builtin_convertvector((float2v{y[i], y[i + 1]}), half2v) * low[i / 2];
-        w[g][n][i / 8][i % 8] = h[0], w[g][n][i / 8][i % 8 + 1] = h[1];
-      }
-    }
+    for (int g = 0; g < G; ++g) z[g].l = fmaf(sum[g], back[n], z[g].l);
   }
 }
 
@@ -318,7 +308,6 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
   for (int g = 0; g < G; ++g)
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      spoil(p[n].knan, s[g][n]);
       f[g][n] = a.scale_log2;
       const Pair pair{1.f, 0.f, absent[n], 0, 0};
       if constexpr (KIND == kMarked)
@@ -398,7 +387,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
 #pragma unroll
       for (int y = 0; y < D / 16; ++y) {
         uint4v x[PARTS];
-        operands<PARTS>(a, r[g].real, raw[y], x);
+        operands<PARTS>(a.negate, raw[y], x);
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) q[((g * PARTS + part) * (D / 16) + y) * 64 + lane] = x[part];
       }
@@ -489,9 +478,9 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
   }
 }
 
-// A work-group (blockIdx.y) takes each of a tile's two groups.
+// Two groups at a time do not fit the registers with 128 dims and scores that are capped, lowered or hidden by tags, nor LDS with two parts of Q: then a work-group (blockIdx.y) takes each.
 template <int D, int PARTS, int KIND>
-constexpr bool kApart = true;
+constexpr bool kApart = PARTS == 2 || (D == 128 && KIND != kPlain);
 
 template <int D, int PARTS, bool MANY, int KIND>
 __global__ __launch_bounds__(256, 2) void k4_attend(AttendArgs a) {
