@@ -423,9 +423,12 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
       k4::step<D, PARTS, KIND, G, 1>(a, u, r, (const bf16x8*)q, z, *(Codes<D>(*)[1]) & c, absent, last, t0, most, [] {}, [] {});
     }
   }
-  // the four waves meet, group after group
-  float* s_o = lds;                                         // [4][32][kPitch]
+  // The four waves meet, group after group.  Each gives three quarters of its output to the others and joins the fourth with theirs: quarter y of a lane's
+  // is o[..][4y .. 4y + 3], of each 64 dims the eight from 16 y + 8 half on, which go through LDS as they lie in the registers.
+  constexpr int kPieces = D / 32;  // float4s of a quarter
+  float4v* s_o = (float4v*)lds;    // [4] waves, kPitch * kRows floats apart: [4] quarters [kPieces][64]
   float2v* s_ml = (float2v*)(lds + 4 * kRows * kPitch<D>);  // [4][32]
+  auto at = [&](int w, int y, int k) { return w * (kRows * kPitch<D> / 4) + (y * kPieces + k) * 64 + lane; };
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     if (g && u.n_rows <= g * kRows) break;
@@ -433,47 +436,61 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
     poison(z[g]);
     if (g) __syncthreads();
     if (half == 0) s_ml[wave * kRows + row] = float2v{z[g].m, l};
-    if (r[g].real) {
-      // o[2X + j][4y + b] is dim 64 X + 2 (8y + 4 half + b) + j
+    // o[2X + j][4y + b] is dim 64 X + 2 (8y + 4 half + b) + j
+    auto piece = [&](int y, int k) {
+      const int x = k / 2, b = 2 * (k % 2);
+      return float4v{z[g].o[2 * x][4 * y + b], z[g].o[2 * x + 1][4 * y + b], z[g].o[2 * x][4 * y + b + 1], z[g].o[2 * x + 1][4 * y + b + 1]};
+    };
+    float4v own[kPieces];
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x)
+    for (int y = 0; y < 4; ++y)
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-#pragma unroll
-          for (int k = 0; k < 4; k += 2)
-            *(float4v*)(s_o + (wave * kRows + row) * kPitch<D> + 64 * x + 2 * (8 * y + 4 * half + k)) =
-                float4v{z[g].o[2 * x][4 * y + k], z[g].o[2 * x + 1][4 * y + k], z[g].o[2 * x][4 * y + k + 1], z[g].o[2 * x + 1][4 * y + k + 1]};
-    }
+      for (int k = 0; k < kPieces; ++k) {
+        if (y == wave) own[k] = piece(y, k);  // (the same for the whole wave)
+        else s_o[at(wave, y, k)] = piece(y, k);
+      }
     __syncthreads();
-    // a thread takes the same four dims of several rows; what lies in LDS is read for rows that there are not, too
-    constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;
-    const int i0 = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4, rows = min(u.n_rows - g * kRows, kRows);
+    float2v ml[4];
+    float4v part[3][kPieces];
 #pragma unroll
-    for (int j = 0; j < kRows / kAtOnce; ++j) {
-      const int i = i0 + j * kAtOnce;
-      float2v ml[4];
-      float4v part[4];
+    for (int w = 0; w < 4; ++w) ml[w] = s_ml[w * kRows + row];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) ml[w] = s_ml[w * kRows + i], part[w] = *(const float4v*)(s_o + (w * kRows + i) * kPitch<D> + d);
-      const float m = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
-      float all = 0.f;
-      float4v o{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < 3; ++i)
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float h = root_exp2(ml[w][0] - m);
-        all = fmaf(ml[w][1] * h, h, all);
-        o += part[w] * (h * h);
+      for (int k = 0; k < kPieces; ++k) part[i][k] = s_o[at(i + (i >= wave), wave, k)];
+    const float m = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0]));
+    float all = 0.f, factor[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float h = root_exp2(ml[w][0] - m);
+      all = fmaf(ml[w][1] * h, h, all);
+      factor[w] = h * h;
+    }
+    const float mine = wave < 2 ? (wave == 0 ? factor[0] : factor[1]) : (wave == 2 ? factor[2] : factor[3]);
+    if (!r[g].real) continue;
+    const int s = u.s0 + g * kRows + row, first = 16 * wave + 8 * half;
+    const int64_t to = u.part < 0 ? row_address(a, s, head) : (int64_t)(u.part + g * kRows + row) * a.g.Hkv + head;
+    const float inverse = inverse_of(all);
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) {
+      float4v o[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        o[k] = own[2 * x + k] * mine;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) o[k] += part[i][2 * x + k] * (i >= wave ? factor[i + 1] : factor[i]);
       }
-      if (i >= rows) continue;
       if (u.part < 0) {
-        const int64_t to = row_address(a, u.s0 + g * kRows + i, head);
-        store_out(a, to * D + d, o * inverse_of(all));
-        if (a.lse && d == 0) a.lse[to] = lse_of(m, all);
+        store_out(a, to * D + 64 * x + first, o[0] * inverse);
+        store_out(a, to * D + 64 * x + first + 4, o[1] * inverse);
       } else {
-        const int64_t to = (int64_t)(u.part + g * kRows + i) * a.g.Hkv + head;
-        *(float4v*)(a.part_acc + to * D + d) = o;
-        if (d == 0) a.part_ml[to] = float2v{m, all};
+        float4v* p = (float4v*)(a.part_acc + to * D + 64 * x + first);
+        p[0] = o[0], p[1] = o[1];
       }
+    }
+    if (wave == 0 && half == 0) {
+      if (u.part >= 0) a.part_ml[to] = float2v{m, all};
+      else if (a.lse) a.lse[to] = lse_of(m, all);
     }
   }
 }
