@@ -2,7 +2,7 @@
 //
 // A wave takes a run, at most 16 neighbouring rows that lie in neighbouring slots of one block, of one kv head, K or V.  A row's scales depend on that row
 // alone, so nothing that was written before is rounded again.
-//   K  a lane has a quarter of a token's dims: with D = 128 those of one scale, with 64 half of them
+//   K  a lane has 8 dims of a token, four neighbouring ones those under one scale
 //   V  a lane has D / 64 neighbouring dims of all 16 tokens, whose codes lie together; a token's magnitudes are compared across the wave.  Codes of two
 //      tokens share a byte, so those of the block's other tokens are read and put back.
 #pragma once
@@ -46,30 +46,38 @@ __device__ inline void each_run(const RowArgs& a, int head, F f) {
   }
 }
 
+// K: a lane takes 8 dims of a token, D / 8 lanes a token; 512 / D tokens at a time.
+template <int D>
+struct KLane {
+  static constexpr int kAtOnce = 512 / D, kTurns = kBlock / kAtOnce;
+  int token, dim;
+  __device__ KLane() : token((int)(threadIdx.x & 63) / (D / 8)), dim((int)(threadIdx.x & 63) % (D / 8) * 8) {}
+  __device__ int64_t codes(int64_t block, int t) const { return block * kCodeBytes(D) + (dim / kGroup * kBlock + t) * 16 + dim % kGroup / 2; }
+  __device__ int64_t scale(int64_t block, int t) const { return (block * kBlock + t) * (D / kGroup) + dim / kGroup; }
+};
+
 template <int D, int IN>
 __device__ inline void append_k(const RowArgs& a, int row, int n, int offset, int head, int64_t block) {
-  constexpr int N = D / 4;
-  const int lane = threadIdx.x & 63, i = lane >> 2, part = lane & 3, token = offset + i;
-  float x[N];
-  load_row<IN, N>(a.k_new, (int64_t)(row + min(i, n - 1)) * a.k_stride + head * D + part * N, x);
-  uint32_t amax = magnitude(x, 0);
-  if constexpr (D == 64) amax = max(amax, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0xb1, 0xf, 0xf, false));  // of lane ^ 1
-  const int byte = scale_byte(amax);
-  const float inverse = inverse_scale(byte);
-  uint32_t w[N / 8];
+  using L = KLane<D>;
+  const L l;
+  float x[L::kTurns][8];
+  // Places without a row get the nearest one's and are dropped below: loads under branches wait for one another.
 #pragma unroll
-  for (int j = 0; j < N; ++j) x[j] = byte == kNone ? 0.f : x[j] * inverse;
+  for (int j = 0; j < L::kTurns; ++j)
+    load_row<IN, 8>(a.k_new, (int64_t)(row + min(l.token + j * L::kAtOnce, n - 1)) * a.k_stride + head * D + l.dim, x[j]);
 #pragma unroll
-  for (int j = 0; j < N / 8; ++j) w[j] = encode8(x + 8 * j);
-  if (i >= n) return;
-  const int dim = part * N;
-  uint8_t* to = a.k + block * kCodeBytes(D) + (dim / kGroup * kBlock + token) * 16 + dim % kGroup / 2;
-  if constexpr (D == 128) {
-    *(uint4v*)to = uint4v{w[0], w[1], w[2], w[3]};
-    a.ks[(block * kBlock + token) * 4 + part] = (uint8_t)byte;
-  } else {
-    *(uint2v*)to = uint2v{w[0], w[1]};
-    if ((part & 1) == 0) a.ks[(block * kBlock + token) * 2 + part / 2] = (uint8_t)byte;
+  for (int j = 0; j < L::kTurns; ++j) {
+    uint32_t amax = magnitude(x[j], 0);
+    amax = max(amax, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0xb1, 0xf, 0xf, false));  // of lane ^ 1
+    amax = max(amax, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0x4e, 0xf, 0xf, false));  // of lane ^ 2
+    const int byte = scale_byte(amax), i = l.token + j * L::kAtOnce;
+    const float inverse = inverse_scale(byte);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[j][k] = byte == kNone ? 0.f : x[j][k] * inverse;
+    const uint32_t w = encode8(x[j]);
+    if (i >= n) continue;
+    *(uint32_t*)(a.k + l.codes(block, offset + i)) = w;
+    if (l.dim % kGroup == 0) a.ks[l.scale(block, offset + i)] = (uint8_t)byte;
   }
 }
 
@@ -171,34 +179,27 @@ __device__ inline void store_row(void* base, int64_t at, const float (&x)[N]) {
   }
 }
 
-__device__ inline float scale_of(int byte) {  // (2^-127 is a subnormal number of fp32)
-  return byte == kNone ? __builtin_nanf("") : __uint_as_float(byte ? (uint32_t)byte << 23 : 0x400000u);
-}
+// A scale's byte as the conversions of codes take it: they go by the exponent alone, 0 is 2^-127 and 255 makes everything not a number.
+__device__ inline float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 
 template <int D, int OUT>
 __device__ inline void read_k(const RowArgs& a, int row, int n, int offset, int head, int64_t block) {
-  constexpr int N = D / 4;
-  const int lane = threadIdx.x & 63, i = min(lane >> 2, n - 1), part = lane & 3, dim = part * N;
-  const uint8_t* from = a.k + block * kCodeBytes(D) + (dim / kGroup * kBlock + offset + i) * 16 + dim % kGroup / 2;
-  uint32_t w[N / 8];
-  if constexpr (D == 128) {
-    const uint4v t = *(const uint4v*)from;
-    for (int j = 0; j < 4; ++j) w[j] = t[j];
-  } else {
-    const uint2v t = *(const uint2v*)from;
-    w[0] = t[0], w[1] = t[1];
-  }
-  const float scale = scale_of(a.ks[(block * kBlock + offset + i) * (D / kGroup) + dim / kGroup]);
-  if ((lane >> 2) >= n) return;
-  float x[N];
+  using L = KLane<D>;
+  const L l;
+  uint32_t w[L::kTurns];
+  int byte[L::kTurns];
 #pragma unroll
-  for (int j = 0; j < N / 8; ++j) {
-    float y[8];
-    decode8(w[j], y);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[8 * j + k] = y[k] * scale;
+  for (int j = 0; j < L::kTurns; ++j) {
+    const int t = offset + min(l.token + j * L::kAtOnce, n - 1);
+    w[j] = *(const uint32_t*)(a.k + l.codes(block, t)), byte[j] = a.ks[l.scale(block, t)];
   }
-  store_row<OUT, N>(a.k_out, (int64_t)(row + i) * a.k_stride + head * D + dim, x);
+#pragma unroll
+  for (int j = 0; j < L::kTurns; ++j) {
+    const int i = l.token + j * L::kAtOnce;
+    float x[8];
+    decode8(w[j], scale_of(byte[j]), x);
+    if (i < n) store_row<OUT, 8>(a.k_out, (int64_t)(row + i) * a.k_stride + head * D + l.dim, x);
+  }
 }
 
 template <int D, int OUT>
@@ -216,14 +217,15 @@ __device__ inline void read_v(const RowArgs& a, int row, int n, int offset, int 
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       float y[8];
-      decode8(w[j][i], y);
+      decode8(w[j][i], 1.f, y);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[8 * i + k][j] = y[k];
     }
 #pragma unroll
   for (int t = 0; t < kBlock; ++t) {
     if (t < offset || t >= offset + n) continue;  // (the same for the whole wave)
-    const float scale = scale_of(__builtin_amdgcn_readlane(bytes, t));
+    const int byte = __builtin_amdgcn_readlane(bytes, t);
+    const float scale = byte == kNone ? __builtin_nanf("") : byte ? scale_of(byte) : 0x1p-127f;
 #pragma unroll
     for (int j = 0; j < N; ++j) x[t][j] *= scale;
     store_row<OUT, N>(a.v_out, (int64_t)(row + t - offset) * a.v_stride + head * D + lane * N, x[t]);

@@ -20,7 +20,8 @@ constexpr int kMaxVocab = 1 << 22, kWholeVocab = 16 * 8 * 256;  // the latter: 1
 struct pasta_rows {
   uint64_t magic = kMagic;
   pasta_rows_config cfg{};
-  rows::Sums* sums = nullptr;
+  double* sums = nullptr;
+  int2* verdicts = nullptr;
 };
 
 namespace {
@@ -31,7 +32,9 @@ int32_t launched() { return hipGetLastError() == hipSuccess ? PASTA_OK : PASTA_E
 
 int segments_of(int vocab) { return vocab > kWholeVocab ? (vocab + rows::kSegment - 1) / rows::kSegment : 0; }
 
-uint64_t workspace_of(const pasta_rows_config& c) { return (uint64_t)segments_of(c.vocab) * c.max_sequences * sizeof(rows::Sums); }
+// Sums of every sequence's segments, then what became of its drafts.
+uint64_t sums_of(const pasta_rows_config& c) { return (uint64_t)segments_of(c.vocab) * c.max_sequences; }
+uint64_t workspace_of(const pasta_rows_config& c) { return segments_of(c.vocab) ? sums_of(c) * sizeof(double) + c.max_sequences * sizeof(int2) : 0; }
 
 int32_t check(const pasta_rows_config* c) {
   if (!c || c->struct_size != sizeof(*c) || c->max_rows < 1) return PASTA_E_INVAL;
@@ -88,7 +91,7 @@ extern "C" int32_t pasta_rows_create(pasta_rows_config* cfg, pasta_rows** out) {
   pasta_rows* h = new (std::nothrow) pasta_rows();
   if (!h) return PASTA_E_NOMEM;
   h->cfg = *cfg;
-  h->sums = (rows::Sums*)cfg->workspace;
+  h->sums = (double*)cfg->workspace, h->verdicts = (int2*)(h->sums + sums_of(*cfg));
   *out = h;
   return PASTA_OK;
 }
@@ -120,12 +123,17 @@ extern "C" int32_t pasta_rows_rotate(pasta_rows* h, const pasta_rows_rotate_args
   const bool wide = (k.interleaved ? c.rope_dims : k.planes) % unit == 0;  // (head_dim is whole 16-byte pieces, and then so is what stays)
   k.pieces = wide ? (k.interleaved ? c.rope_dims : k.planes) / unit + stays / unit : k.planes + stays;
   k.at_once = 256 / k.pieces;
-  const dim3 grid((unsigned)a->n_rows, (unsigned)((k.n_heads + k.at_once - 1) / k.at_once));
+  // Two rows to a work-group where that leaves 2048 of them and more, since more has to be on its way then (8192 rows of 32 + 8 heads, interleaved / half: 36 /
+  // 38 us instead of 43 / 40; 2048 rows 8.7 and 8.9; of 1024 rows 6.0 and 5.6; four rows to a work-group are no better).
+  const unsigned parts = (unsigned)((k.n_heads + k.at_once - 1) / k.at_once);
+  auto launch = [&](auto type, auto wide, auto rows) {
+    const dim3 grid((unsigned)(((int64_t)a->n_rows + rows.value - 1) / rows.value), parts);
+    rows::rows_rotate<type.value, wide.value, rows.value><<<grid, 256, 0, (hipStream_t)c.hip_stream>>>(k);
+  };
   by_type(a->dtype, [&](auto type) {
-    if (wide)
-      rows::rows_rotate<type.value, true><<<grid, 256, 0, (hipStream_t)c.hip_stream>>>(k);
-    else
-      rows::rows_rotate<type.value, false><<<grid, 256, 0, (hipStream_t)c.hip_stream>>>(k);
+    if (!wide) launch(type, std::false_type{}, std::integral_constant<int, 1>{});
+    else if ((int64_t)a->n_rows * parts < 4096) launch(type, std::true_type{}, std::integral_constant<int, 1>{});
+    else launch(type, std::true_type{}, std::integral_constant<int, 2>{});
   });
   return launched();
 }
@@ -153,7 +161,7 @@ extern "C" int32_t pasta_rows_verify(pasta_rows* h, const pasta_rows_verify_args
   k.n_sequences = a->n_sequences, k.n_rows = a->n_rows, k.vocab = c.vocab;
   k.row_offsets = a->row_offsets, k.token = a->token, k.target = a->target, k.draft = a->draft, k.draw = a->draw, k.last_draw = a->last_draw;
   k.length = a->length, k.row_position = a->row_position, k.accepted = a->accepted, k.next_token = a->next_token, k.keep = a->keep;
-  k.position_out = a->position_out, k.sums = h->sums;
+  k.position_out = a->position_out, k.sums = h->sums, k.verdicts = h->verdicts;
   hipStream_t s = (hipStream_t)c.hip_stream;
   by_type(a->dtype, [&](auto type) {
     if (k.segments) {

@@ -81,64 +81,75 @@ __device__ inline void turn_of(double revolutions, float& c, float& s) {
 }
 
 // WIDE: every piece of a head is 16 bytes, of one kind: half-split planes (then the piece is two, half the turned dims apart), interleaved ones, or dims that
-// stay.  Else a piece is one plane or one dim that stays: rope_dims that are not whole 16-byte pieces.
-template <int TYPE, bool WIDE>
+// stay.  Else a piece is one plane or one dim that stays: rope_dims that are not whole 16-byte pieces.  A work-group turns ROWS rows.
+template <int TYPE, bool WIDE, int ROWS>
 __global__ __launch_bounds__(256) void rows_rotate(RotateArgs a) {
-  __shared__ float s_cos[kMaxDim / 2], s_sin[kMaxDim / 2];
+  __shared__ float s_cos[ROWS][kMaxDim / 2], s_sin[ROWS][kMaxDim / 2];
   using T = std::conditional_t<TYPE == kF32, uint32_t, uint16_t>;
   constexpr int N = WIDE ? Piece<TYPE>::N : 1;
-  const int row = blockIdx.x, slot = threadIdx.x / a.pieces, piece = threadIdx.x - slot * a.pieces;
+  const int row = blockIdx.x * ROWS, n_rows = min(ROWS, a.n_rows - row), slot = threadIdx.x / a.pieces, piece = threadIdx.x - slot * a.pieces;
   const int head = blockIdx.y * a.at_once + slot;
   const bool mine = slot < a.at_once && head < a.n_heads;
   const Side& side = head < a.n_q ? a.q : a.k;
   const int64_t at = (int64_t)(head < a.n_q ? head : head - a.n_q) * a.D;
   const char* in = (const char*)side.in + (row * side.in_stride + at) * sizeof(T);
   char* out = (char*)side.out + (row * side.out_stride + at) * sizeof(T);
+  const int64_t in_step = side.in_stride * sizeof(T), out_step = side.out_stride * sizeof(T);
   // pieces of a head: the turned ones, then those that stay
   const int turned = a.interleaved && WIDE ? 2 * a.planes / N : a.planes / N;
   const bool turns = piece < turned;
   const int first = turns ? (a.interleaved ? (WIDE ? piece * N : 2 * piece) : piece * N) : 2 * a.planes + (piece - turned) * N;
   const int second = a.interleaved ? first + 1 : first + a.planes;  // of a half-split plane, or of one alone
-  Piece<TYPE> x, y;
+  Piece<TYPE> x[ROWS], y[ROWS];
   if (mine) {
-    if constexpr (WIDE) {
-      x.load(in, first);
-      if (turns && !a.interleaved) y.load(in, second);
-    } else {
-      x.x[0] = to_float<TYPE>(((const T*)in)[first]);
-      if (turns) y.x[0] = to_float<TYPE>(((const T*)in)[second]);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const char* from = in + min(r, n_rows - 1) * in_step;  // (no branches around loads: they would wait for one another)
+      if constexpr (WIDE) {
+        x[r].load(from, first);
+        if (turns && !a.interleaved) y[r].load(from, second);
+      } else {
+        x[r].x[0] = to_float<TYPE>(((const T*)from)[first]);
+        if (turns) y[r].x[0] = to_float<TYPE>(((const T*)from)[second]);
+      }
     }
   }
-  if ((int)threadIdx.x < a.planes) {
+  for (int i = threadIdx.x; i < n_rows * a.planes; i += 256) {
     constexpr double kTurn = 0.15915494309189533577;  // 1 / (2 pi)
+    const int r = ROWS == 1 ? 0 : i / a.planes, f = i - r * a.planes;
     float c, s;
-    turn_of<TYPE>((double)a.position[row] * (a.frequency[threadIdx.x] * kTurn), c, s);
-    s_cos[threadIdx.x] = c * a.magnitude, s_sin[threadIdx.x] = s * a.direction;
+    turn_of<TYPE>((double)a.position[row + r] * (a.frequency[f] * kTurn), c, s);
+    s_cos[r][f] = c * a.magnitude, s_sin[r][f] = s * a.direction;
   }
   __syncthreads();
   if (!mine || (!turns && in == out)) return;
-  if constexpr (WIDE) {
-    if (turns && a.interleaved) {
-      for (int i = 0; i < N; i += 2) {
-        const float c = s_cos[(first + i) / 2], s = s_sin[(first + i) / 2], u = x.x[i], v = x.x[i + 1];
-        x.x[i] = u * c - v * s, x.x[i + 1] = v * c + u * s;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (r >= n_rows) break;
+    char* to = out + r * out_step;
+    if constexpr (WIDE) {
+      if (turns && a.interleaved) {
+        for (int i = 0; i < N; i += 2) {
+          const float c = s_cos[r][(first + i) / 2], s = s_sin[r][(first + i) / 2], u = x[r].x[i], v = x[r].x[i + 1];
+          x[r].x[i] = u * c - v * s, x[r].x[i + 1] = v * c + u * s;
+        }
+      } else if (turns) {
+        for (int i = 0; i < N; ++i) {
+          const float c = s_cos[r][first + i], s = s_sin[r][first + i], u = x[r].x[i], v = y[r].x[i];
+          x[r].x[i] = u * c - v * s, y[r].x[i] = v * c + u * s;
+        }
+        y[r].store(to, second);
       }
-    } else if (turns) {
-      for (int i = 0; i < N; ++i) {
-        const float c = s_cos[first + i], s = s_sin[first + i], u = x.x[i], v = y.x[i];
-        x.x[i] = u * c - v * s, y.x[i] = v * c + u * s;
+      x[r].store(to, first);
+    } else {
+      float u = x[r].x[0];
+      if (turns) {
+        const float c = s_cos[r][piece], s = s_sin[r][piece], v = y[r].x[0];
+        ((T*)to)[second] = (T)from_float<TYPE>(v * c + u * s);
+        u = u * c - v * s;
       }
-      y.store(out, second);
+      ((T*)to)[first] = (T)from_float<TYPE>(u);
     }
-    x.store(out, first);
-  } else {
-    float u = x.x[0];
-    if (turns) {
-      const float c = s_cos[piece], s = s_sin[piece], v = y.x[0];
-      ((T*)out)[second] = (T)from_float<TYPE>(v * c + u * s);
-      u = u * c - v * s;
-    }
-    ((T*)out)[first] = (T)from_float<TYPE>(u);
   }
 }
 

@@ -20,12 +20,10 @@ struct VerifyArgs {
   const float *draw, *last_draw;
   const int *length, *row_position;
   int *accepted, *next_token, *keep, *position_out;
-  struct Sums* sums;  // workspace: [sequence][segment]
+  double* sums;     // workspace: [sequence][segment]
+  int2* verdicts;   // workspace: [sequence] accepted, rejected
 };
 
-struct Sums {
-  double rest, all;  // of max(p - q, 0), of p
-};
 
 constexpr int kSegment = 1024;  // tokens of a wave, where a sequence takes many
 
@@ -72,22 +70,29 @@ __device__ inline void four(const void* base, int64_t row, int at, int n, float 
   }
 }
 
-__device__ inline double weight(double x) { return x > 0.0 && x < __builtin_inf() ? x : 0.0; }
+// What the target has beyond the draft's distribution; 0 for a NaN, too (the larger of a NaN and 0 is 0).
+__device__ inline double weight(float p, float q) { return fmax((double)p - (double)q, 0.0); }
 
 // What becomes of a sequence's drafts; every lane of the wave knows.
 struct Verdict {
   int first, rows, accepted;
   int rejected;  // the token that was, -1: none
+  __device__ bool left() const { return accepted + 1 < rows; }  // a draft was rejected: what the target has beyond the draft's distribution is left
 };
 
-template <int TYPE>
-__device__ inline Verdict judge(const VerifyArgs& a, int s) {
-  const int lane = threadIdx.x & 63;
+__device__ inline Verdict rows_of(const VerifyArgs& a, int s) {
   const int end = min(max(a.row_offsets[a.n_sequences], 0), a.n_rows);
   Verdict v;
   v.first = min(max(a.row_offsets[s], 0), end);
   v.rows = min(max(a.row_offsets[s + 1], v.first), end) - v.first;
   v.accepted = max(v.rows - 1, 0), v.rejected = -1;
+  return v;
+}
+
+template <int TYPE>
+__device__ inline Verdict judge(const VerifyArgs& a, int s) {
+  const int lane = threadIdx.x & 63;
+  Verdict v = rows_of(a, s);
   for (int i0 = 1; i0 < v.rows; i0 += 64) {
     const int i = i0 + lane, row = v.first + min(i, v.rows - 1);
     const int t = a.token[row];
@@ -109,23 +114,43 @@ __device__ inline Verdict judge(const VerifyArgs& a, int s) {
 // A wave's segment: weights of 4 * LOADS tokens in every lane.
 template <int TYPE, int LOADS>
 struct Segment {
-  float p[LOADS][4], q[LOADS][4];
+  float p[LOADS][4], q[LOADS][4];  // q: 0 where the target alone counts, +inf where nothing is to count
 
   __device__ void load(const VerifyArgs& a, const Verdict& v, int from) {
     const int lane = threadIdx.x & 63;
     const int64_t row = v.first + v.accepted;
-    const bool both = a.draft && v.accepted + 1 < v.rows;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) four<TYPE>(a.target, row * a.target_stride, from + j * 256 + lane * 4, a.vocab, p[j]);
-    if (both) {
+    if (a.draft && v.left()) {
 #pragma unroll
       for (int j = 0; j < LOADS; ++j) four<TYPE>(a.draft, (row + 1) * a.draft_stride, from + j * 256 + lane * 4, a.vocab, q[j]);
     } else {
 #pragma unroll
       for (int j = 0; j < LOADS; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[j][i] = !a.draft && from + j * 256 + lane * 4 + i == v.rejected ? __builtin_inff() : 0.f;
+        for (int i = 0; i < 4; ++i) q[j][i] = !a.draft && v.left() && from + j * 256 + lane * 4 + i == v.rejected ? __builtin_inff() : 0.f;
     }
+  }
+
+  // Infinite weights count as 0: they are taken out here, and the sums need not look for them.
+  __device__ void hold() {
+    float most = 0.f, least = 0.f;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, p[j][i]), least = fminf(least, q[j][i]);
+    if (__builtin_expect(!__any(most == __builtin_inff() || least == -__builtin_inff()), 1)) return;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[j][i] = p[j][i] == __builtin_inff() ? 0.f : p[j][i], q[j][i] = q[j][i] == -__builtin_inff() ? __builtin_inff() : q[j][i];
+  }
+
+  __device__ void target_alone() {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[j][i] = 0.f;
   }
 
   // Weights are computed anew behind this: kept, as fp64, they take twice the registers that there are.
@@ -136,46 +161,52 @@ struct Segment {
       for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(p[j][i]), "+v"(q[j][i]));
   }
 
-  __device__ double at(bool rest, int j, int i) const { return rest ? weight((double)p[j][i] - (double)q[j][i]) : weight((double)p[j][i]); }
+  __device__ double lane_sum(int j) const { return (weight(p[j][0], q[j][0]) + weight(p[j][1], q[j][1])) + (weight(p[j][2], q[j][2]) + weight(p[j][3], q[j][3])); }
 
-  __device__ double lane_sum(bool rest, int j) const { return (at(rest, j, 0) + at(rest, j, 1)) + (at(rest, j, 2) + at(rest, j, 3)); }
-
-  __device__ Sums sums() const {  // of the wave, in every lane
-    Sums s{0.0, 0.0};
+  __device__ double sum() const {  // of the wave, in every lane
+    double s = 0.0;
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) s.rest += lane_sum(true, j), s.all += lane_sum(false, j);
-    return Sums{of_lane(upto(s.rest), 63), of_lane(upto(s.all), 63)};
+    for (int j = 0; j < LOADS; ++j) s += lane_sum(j);
+    return of_lane(upto(s), 63);
   }
 
   // The first token whose sum, from `before` on, is above `mark`; where rounding leaves none, the last that has a weight.
-  __device__ int find(bool rest, double before, double mark, int from) const {
+  __device__ int find(double before, double mark, int from) const {
     const int lane = threadIdx.x & 63;
-    int found = -1, last = -1;
+    double up[LOADS];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) up[j] = upto(lane_sum(j));
+    int at = 0;  // which 256 tokens
+    double base = before;
+    bool found = false;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const double mine = lane_sum(rest, j), up = before + upto(mine);
-      double here = up - mine;
-      int hit = -1, some = -1;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const double w = at(rest, j, i);
-        here += w;
-        if (w > 0.0) some = i;
-        if (hit < 0 && w > 0.0 && here > mark) hit = i;
-      }
-      if (hit < 0 && some >= 0 && up > mark) hit = some;  // (its own sum was rounded otherwise)
-      const uint64_t hits = __ballot(hit >= 0), any = __ballot(some >= 0);
-      if (found < 0 && hits) {
-        const int k = __builtin_ctzll(hits);
-        found = from + j * 256 + k * 4 + __builtin_amdgcn_readlane(hit, k);
-      }
-      if (any) {
-        const int k = 63 - __builtin_clzll(any);
-        last = from + j * 256 + k * 4 + __builtin_amdgcn_readlane(some, k);
-      }
-      before = of_lane(up, 63);
+      const double all = of_lane(up[j], 63);
+      if (!found && all > 0.0) at = j, base = before, found = before + all > mark;  // (the same for all lanes)
+      before += all;
     }
-    return found >= 0 ? found : last;
+    float x[4], y[4];
+    double mine = 0.0;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+      if (j == at) {
+        mine = base + up[j];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = p[j][i], y[i] = q[j][i];
+      }
+    double here = mine - ((weight(x[0], y[0]) + weight(x[1], y[1])) + (weight(x[2], y[2]) + weight(x[3], y[3])));
+    int hit = -1, some = -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const double w = weight(x[i], y[i]);
+      here += w;
+      if (w > 0.0) some = i;
+      if (hit < 0 && w > 0.0 && here > mark) hit = i;
+    }
+    if (hit < 0 && some >= 0 && mine > mark) hit = some;  // (its own sum was rounded otherwise)
+    const uint64_t hits = __ballot(hit >= 0), any = __ballot(some >= 0);
+    const int k = hits ? __builtin_ctzll(hits) : any ? 63 - __builtin_clzll(any) : 0;
+    return from + at * 256 + k * 4 + max(__builtin_amdgcn_readlane(hits ? hit : some, k), 0);
   }
 };
 
@@ -197,94 +228,124 @@ __device__ inline double mark_of(const VerifyArgs& a, int s, double total) {
 // A sequence a work-group, the whole vocabulary in its registers.
 template <int TYPE, int LOADS>
 __global__ __launch_bounds__(1024) void rows_verify_whole(VerifyArgs a) {
-  __shared__ Sums s_sums[16];
+  __shared__ double s_sum[2][16];
   const int s = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), from = wave * LOADS * 256;
   const Verdict v = judge<TYPE>(a, s);
-  put_down(a, s, v);
-  if (v.rows == 0) return;
+  if (v.rows == 0) return put_down(a, s, v);
   Segment<TYPE, LOADS> g;
   g.load(a, v, from);
-  const Sums own = g.sums();
-  g.forget();
-  if ((threadIdx.x & 63) == 0) s_sums[wave] = own;
-  __syncthreads();
-  Sums total{0.0, 0.0}, before{0.0, 0.0};
-  for (int w = 0; w < (int)blockDim.x >> 6; ++w) {
-    if (w == wave) before = total;
-    total.rest += s_sums[w].rest, total.all += s_sums[w].all;
+  put_down(a, s, v);
+  double own, total, before;
+  g.hold();
+  for (int turn = 0; turn < 2; ++turn) {  // where nothing is left of p - q, p alone
+    own = g.sum();
+    g.forget();
+    if ((threadIdx.x & 63) == 0) s_sum[turn][wave] = own;
+    __syncthreads();
+    total = before = 0.0;
+    for (int w = 0; w < (int)blockDim.x >> 6; ++w) {
+      if (w == wave) before = total;
+      total += s_sum[turn][w];
+    }
+    if (total > 0.0 || !v.left()) break;
+    g.target_alone();
   }
-  const bool rest = v.accepted + 1 < v.rows && total.rest > 0.0;
-  const double mark = mark_of(a, s, rest ? total.rest : total.all);
-  if (!(total.all > 0.0) && !rest) {
+  if (!(total > 0.0)) {
     if (threadIdx.x == 0) a.next_token[s] = -1;
     return;
   }
-  const double lower = rest ? before.rest : before.all, mine = rest ? own.rest : own.all;
-  if (lower <= mark && lower + mine > mark) {  // (one wave, since sums go up by the same additions everywhere)
-    const int t = g.find(rest, lower, mark, from);
+  const double mark = mark_of(a, s, total);
+  if (before <= mark && before + own > mark) {  // (one wave, since sums go up by the same additions everywhere)
+    const int t = g.find(before, mark, from);
     if ((threadIdx.x & 63) == 0) a.next_token[s] = t;
   }
 }
 
-// Sums of the segments; four of a sequence to a work-group.
+// Sums of the segments; four of a sequence to a work-group.  What is judged goes to the next launch.
 template <int TYPE>
 __global__ __launch_bounds__(256) void rows_verify_sums(VerifyArgs a) {
   const int s = blockIdx.y, segment = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (segment >= a.segments) return;
   const Verdict v = judge<TYPE>(a, s);
+  if (segment == 0 && (threadIdx.x & 63) == 0) a.verdicts[s] = int2{v.accepted, v.rejected};
   if (v.rows == 0) return;
   Segment<TYPE, kSegment / 256> g;
   g.load(a, v, segment * kSegment);
-  const Sums own = g.sums();
+  g.hold();
+  const double own = g.sum();
   if ((threadIdx.x & 63) == 0) a.sums[(int64_t)s * a.segments + segment] = own;
 }
 
 // The segment that the draw falls into, and the token; a sequence a work-group.
 template <int TYPE>
 __global__ __launch_bounds__(256) void rows_verify_pick(VerifyArgs a) {
-  __shared__ Sums s_sums[4];
+  __shared__ double s_sum[4];
   const int s = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Sums* sums = a.sums + (int64_t)s * a.segments;
-  const Verdict v = judge<TYPE>(a, s);
+  double* sums = a.sums + (int64_t)s * a.segments;
+  const int each = (a.segments + 255) / 256, from = min((int)threadIdx.x * each, a.segments), to = min(from + each, a.segments);  // this thread's
+  const double first = from < to ? sums[from] : 0.0;  // (asked for at once; of a sequence without rows it is nothing)
+  const int2 known = a.verdicts[s];
+  Verdict v = rows_of(a, s);
+  v.accepted = known.x, v.rejected = known.y;
   put_down(a, s, v);
   if (v.rows == 0) return;
-  const int each = (a.segments + 255) / 256, from = min((int)threadIdx.x * each, a.segments), to = min(from + each, a.segments);  // this thread's
-  Sums own{0.0, 0.0};
-  for (int i = from; i < to; ++i) own.rest += sums[i].rest, own.all += sums[i].all;
-  const Sums up{upto(own.rest), upto(own.all)};
-  if (lane == 63) s_sums[wave] = up;
-  __syncthreads();
-  Sums total{0.0, 0.0}, before{0.0, 0.0};
-  for (int w = 0; w < 4; ++w) {
-    if (w == wave) before = total;
-    total.rest += s_sums[w].rest, total.all += s_sums[w].all;
+  Segment<TYPE, kSegment / 256> g;
+  bool alone = false;  // nothing is left of p - q: p alone
+  double own = first;
+  for (int i = from + 1; i < to; ++i) own += sums[i];
+  double up, total, before;
+  auto add = [&] {
+    up = upto(own);
+    if (lane == 63) s_sum[wave] = up;
+    __syncthreads();
+    total = before = 0.0;
+    for (int w = 0; w < 4; ++w) {
+      if (w == wave) before = total;
+      total += s_sum[w];
+    }
+  };
+  add();
+  if (!(total > 0.0) && v.left()) {
+    alone = true;
+    for (int i = wave; i < a.segments; i += 4) {
+      g.load(a, v, i * kSegment);
+      g.hold();
+      g.target_alone();
+      const double x = g.sum();
+      if (lane == 0) sums[i] = x;
+    }
+    __syncthreads();
+    own = 0.0;
+    for (int i = from; i < to; ++i) own += sums[i];
+    add();
   }
-  const bool rest = v.accepted + 1 < v.rows && total.rest > 0.0;
-  const double mark = mark_of(a, s, rest ? total.rest : total.all);
-  if (!(total.all > 0.0) && !rest) {
+  if (!(total > 0.0)) {
     if (threadIdx.x == 0) a.next_token[s] = -1;
     return;
   }
   // the wave, the thread in it, the segment of that: each the first one whose sum is above the mark
-  const double lower = rest ? before.rest : before.all, upper = lower + (rest ? s_sums[wave].rest : s_sums[wave].all);
-  if (!(lower <= mark && upper > mark)) return;
-  const double end = lower + (rest ? up.rest : up.all);
-  const bool some = (rest ? own.rest : own.all) > 0.0;
+  const double mark = mark_of(a, s, total);
+  if (!(before <= mark && before + s_sum[wave] > mark)) return;
+  const double end = before + up;
+  const bool some = own > 0.0;
   const uint64_t any = __ballot(some), past = __ballot(some && end > mark);  // (lanes' sums are rounded each in its own way)
   const int k = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
-  double here = k ? of_lane(end, k - 1) : lower;
-  const int first = __builtin_amdgcn_readlane(from, k), last = __builtin_amdgcn_readlane(to, k);
-  int segment = -1;
+  double here = k ? of_lane(end, k - 1) : before;
+  const int begin = __builtin_amdgcn_readlane(from, k), stop = __builtin_amdgcn_readlane(to, k);
+  int segment = begin;
   double base = here;
-  for (int i = first; i < last; ++i) {
-    const double w = rest ? sums[i].rest : sums[i].all;
-    if (w > 0.0) segment = i, base = here;
-    here += w;
-    if (here > mark && w > 0.0) break;
+  if (each > 1) {
+    for (int i = begin; i < stop; ++i) {
+      const double w = sums[i];
+      if (w > 0.0) segment = i, base = here;
+      here += w;
+      if (here > mark && w > 0.0) break;
+    }
   }
-  Segment<TYPE, kSegment / 256> g;
   g.load(a, v, segment * kSegment);
-  const int t = g.find(rest, base, mark, segment * kSegment);
+  g.hold();
+  if (alone) g.target_alone();
+  const int t = g.find(base, mark, segment * kSegment);
   if (lane == 0) a.next_token[s] = t;
 }
 

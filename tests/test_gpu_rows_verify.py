@@ -194,6 +194,21 @@ def test_weights_that_do_not_count(V):
     assert got[1][0] == -1 and got[1][1] == -1 and got[1][2] % 3 == 2 and got[1][4] == V - 1
 
 
+@pytest.mark.parametrize("V", [300, 20000, 40000])
+def test_infinite_weights_beside_finite_ones(V):
+    """Of p, of the draft's distribution (below p everywhere else, and nowhere), and where p alone is left."""
+    c = Case(26, V, [2, 2, 2])
+    t = c.token[[1, 3, 5]].long()
+    c.target[[0, 2, 4], t] = 0.0  # (rejected)
+    c.target[0, 7], c.draft[1, 11], c.draft[1, 12] = float("inf"), -float("inf"), float("inf")
+    c.draft[3] = 2.0
+    c.draft[3, 5] = -float("inf")
+    c.draft[3, t[1]] = 1.0
+    c.draft[5] = float("nan")
+    c.draft[5, t[2]] = 1.0
+    assert (c.check()[0] == 0).all()
+
+
 @pytest.mark.parametrize("V", [300, 40000])
 def test_draws_outside_of_their_range(V):
     c = Case(19, V, [1] * 6 + [2] * 3)

@@ -64,7 +64,7 @@ def test_workspaces_and_addresses():
     assert rows.query_workspace_bytes(rows.make_config(**ROPE)) == 0
     assert rows.query_workspace_bytes(rows.make_config(**{**VERIFY, "vocab": 32768})) == 0
     size = rows.query_workspace_bytes(rows.make_config(**VERIFY))
-    assert size == 16 * 98 * 16
+    assert size == 16 * (98 * 8 + 8)
     for ws, n, code in ((FAKE, size - 1, rows.E_CAPACITY), (FAKE + 16, size, rows.E_INVAL)):
         with pytest.raises(rows.PastaError) as e:
             rows.PastaRows(rows.make_config(**VERIFY), ws, workspace_bytes=n)
