@@ -52,7 +52,7 @@ struct Planned {
 // units, which a launch goes over one by one: 256 work-groups that find nothing cost 1.5 us; a tile is split only into pieces of more than half a chunk
 // on the mean, so that at most twice max(capacity, 1) of them are partial).
 template <class Config>
-Bounds bounds(const Config& c, int64_t n_rows, int64_t n_requests, bool wide, bool whole) {
+Bounds bounds(const Config& c, int64_t n_rows, int64_t n_requests, bool wide, bool whole, int least_alone) {
   const int64_t G = c.n_q_heads / c.n_kv_heads, stacked = n_rows * G;
   Bounds b;
   b.capacity = kUnitsAtOnce / c.n_kv_heads;
@@ -61,7 +61,7 @@ Bounds bounds(const Config& c, int64_t n_rows, int64_t n_requests, bool wide, bo
   if (wide) b.tiles = std::min(b.tiles, (stacked + (n_requests + 1) * (kWideRows - 1)) / kWideRows + 2 * (n_requests + 1));
   if (b.tiles > stacked) b.tiles = stacked;
   const int64_t chunks = ((int64_t)c.pages_per_request * c.page_tokens + kChunkTokens - 1) / kChunkTokens;
-  b.units = std::min(std::max(b.capacity, std::max(b.capacity / 2, (int64_t)1) + b.tiles), b.tiles * ((3 * chunks + 3) / 4));
+  b.units = std::min(std::max(b.capacity, std::max(b.capacity / 2, (int64_t)1) + b.tiles), b.tiles * (least_alone < kLeastAlone ? chunks : (3 * chunks + 3) / 4));
   if (whole) b.units = b.tiles;
   int64_t rows = wide ? kWideRows : kRows;
   b.merge_rows = rows < stacked ? rows : stacked;
@@ -71,6 +71,7 @@ Bounds bounds(const Config& c, int64_t n_rows, int64_t n_requests, bool wide, bo
 
 // What a plan keeps in the workspace.
 struct PlanSpace {
+  int least_alone = kLeastAlone;  // (of the cache: the least length of pieces where a CU has one)
   int* tiles_upto = nullptr;
   Unit* units = nullptr;
   int* unit_blocks = nullptr;
@@ -80,8 +81,8 @@ struct PlanSpace {
 
   template <class Config, class Take>
   void lay_out(const Config& c, Take take) {
-    Bounds b = bounds(c, c.max_rows, c.max_requests, false, false);
-    if ((int64_t)c.max_rows * (c.n_q_heads / c.n_kv_heads) > kManyRows) b.part_rows = bounds(c, c.max_rows, c.max_requests, true, false).part_rows;
+    Bounds b = bounds(c, c.max_rows, c.max_requests, false, false, least_alone);
+    if ((int64_t)c.max_rows * (c.n_q_heads / c.n_kv_heads) > kManyRows) b.part_rows = bounds(c, c.max_rows, c.max_requests, true, false, least_alone).part_rows;
     take(tiles_upto, c.max_requests + 1);
     take(units, b.units);
     take(unit_blocks, b.units * kUnitBlocks);
@@ -111,9 +112,9 @@ bool launch_plan(const Config& c, const Geometry& g, const PlanSpace& space, con
   plan.wide = most * g.G > kManyRows;
   // where every tile is that short, splitting it costs more (a launch, partial rows) than it saves
   plan.whole = (int64_t)c.pages_per_request * c.page_tokens <= (plan.wide ? kWholeWide : kWholeTokens);
-  plan.most = bounds(c, a.n_rows, a.n_requests, plan.wide, plan.whole);
+  plan.most = bounds(c, a.n_rows, a.n_requests, plan.wide, plan.whole, space.least_alone);
   PlanArgs k{};
-  k.g = g, k.n_requests = a.n_requests, k.n_rows = a.n_rows, k.wide = plan.wide, k.whole = plan.whole, k.capacity = (int)plan.most.capacity;
+  k.g = g, k.n_requests = a.n_requests, k.n_rows = a.n_rows, k.wide = plan.wide, k.whole = plan.whole, k.capacity = (int)plan.most.capacity, k.least_alone = space.least_alone;
   k.max_units = (int)plan.most.units, k.max_tiles = (int)plan.most.tiles, k.max_part_rows = (int)plan.most.part_rows;
   k.length = a.n_requests ? a.length : a.row_offsets;  // (read, not used, without a request)
   k.row_offsets = a.row_offsets, k.prefix_len = a.prefix_len, k.slot = a.slot;

@@ -24,6 +24,7 @@ struct PlanArgs {
   int wide;       // requests with more than kManyRows stacked rows take tiles of 64
   int whole;      // no tile is split
   int capacity;   // units that the chip takes at once
+  int least_alone;  // kLeastAlone, or that of another cache
   int max_units, max_tiles, max_part_rows;
   const int *length, *row_offsets, *prefix_len, *slot, *table;
   Unit* units;
@@ -140,8 +141,9 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
   }
   __syncthreads();
   const bool alone = 2 * n_tiles <= a.capacity && s_chunk[1] * (kChunkTokens / 2) <= kAloneTokens;
-  const int chunk = alone ? max(s_chunk[1], 2 * kLeastAlone / kChunkTokens) : max(s_chunk[0], 2 * kLeastTokens / kChunkTokens);
-  const int parts = tid < n_tiles ? parts_of(a, own, chunk) : 0;
+  const int chunk = alone ? max(s_chunk[1], 2 * a.least_alone / kChunkTokens) : max(s_chunk[0], 2 * kLeastTokens / kChunkTokens);
+  int parts = tid < n_tiles ? parts_of(a, own, chunk) : 0;
+  if (chunk < 2 * kLeastAlone / kChunkTokens) parts = min(parts, most_pieces(cost));
   const int rows = parts > 1 ? parts * u.n_rows : 0;
   int2v all;
   const int2v upto_here = group_scan<NT>(int2v{parts, rows}, s_tmp, all);
