@@ -103,6 +103,10 @@ int32_t pasta_rows_rotate(pasta_rows *h, const pasta_rows_rotate_args *a);
  *   position_out[i] = row_position[i] + 1 + a for the sequence's rows: their positions in
  *   the next step.  It may be row_position.
  *
+ * slot (optional): the rows' places, as pasta_kv8_slots gave them.  A sequence whose first
+ * row has none was refused: a is 0, next_token -1, keep[s] = length[s], and its
+ * positions stay.
+ *
  * Rows behind row_offsets[n_sequences] are left alone.  Strides are at least vocab, in values.
  * Needs the workspace.  Errors: E_INVAL, E_CAPACITY, E_DEVICE, E_STATE.          */
 typedef struct {
@@ -111,6 +115,7 @@ typedef struct {
   int32_t dtype;                  /* of the probabilities: PASTA_F32 | PASTA_BF16 | PASTA_F16 */
   const int32_t *row_offsets;     /* DEVICE [n_sequences + 1] */
   const int32_t *token;           /* DEVICE [n_rows] */
+  const int32_t *slot;            /* DEVICE [n_rows], or NULL */
   const void *target;             /* DEVICE [n_rows][vocab] */
   const void *draft;              /* DEVICE [n_rows][vocab], or NULL */
   int64_t target_stride, draft_stride; /* in values; 0: vocab */

@@ -153,13 +153,13 @@ extern "C" int32_t pasta_rows_verify(pasta_rows* h, const pasta_rows_verify_args
   if (!a->keep != !a->length || !a->position_out != !a->row_position) return PASTA_E_INVAL;
   if (a->n_sequences == 0) return PASTA_OK;
   if (!a->row_offsets || !a->accepted || !a->next_token || !a->last_draw || (a->n_rows && (!a->token || !a->target || !a->draw))) return PASTA_E_INVAL;
-  const void* words[] = {a->row_offsets, a->token, a->draw, a->last_draw, a->length, a->row_position, a->accepted, a->next_token, a->keep, a->position_out};
+  const void* words[] = {a->row_offsets, a->token, a->slot, a->draw, a->last_draw, a->length, a->row_position, a->accepted, a->next_token, a->keep, a->position_out};
   for (const void* p : words)
     if (!aligned(p, 4)) return PASTA_E_INVAL;
   const uintptr_t size = a->dtype == PASTA_F32 ? 4 : 2;
   if (!aligned(a->target, size) || !aligned(a->draft, size)) return PASTA_E_INVAL;
   k.n_sequences = a->n_sequences, k.n_rows = a->n_rows, k.vocab = c.vocab;
-  k.row_offsets = a->row_offsets, k.token = a->token, k.target = a->target, k.draft = a->draft, k.draw = a->draw, k.last_draw = a->last_draw;
+  k.row_offsets = a->row_offsets, k.token = a->token, k.slot = a->slot, k.target = a->target, k.draft = a->draft, k.draw = a->draw, k.last_draw = a->last_draw;
   k.length = a->length, k.row_position = a->row_position, k.accepted = a->accepted, k.next_token = a->next_token, k.keep = a->keep;
   k.position_out = a->position_out, k.sums = h->sums, k.verdicts = h->verdicts;
   hipStream_t s = (hipStream_t)c.hip_stream;

@@ -14,7 +14,7 @@ namespace rows {
 
 struct VerifyArgs {
   int n_sequences, n_rows, vocab, segments;
-  const int *row_offsets, *token;
+  const int *row_offsets, *token, *slot;
   const void *target, *draft;
   int64_t target_stride, draft_stride;
   const float *draw, *last_draw;
@@ -76,6 +76,7 @@ __device__ inline double weight(float p, float q) { return fmax((double)p - (dou
 // What becomes of a sequence's drafts; every lane of the wave knows.
 struct Verdict {
   int first, rows, accepted;
+  int refused;   // rows of a sequence that has no place for them, whose `rows` are then 0
   int rejected;  // the token that was, -1: none
   __device__ bool left() const { return accepted + 1 < rows; }  // a draft was rejected: what the target has beyond the draft's distribution is left
 };
@@ -85,6 +86,8 @@ __device__ inline Verdict rows_of(const VerifyArgs& a, int s) {
   Verdict v;
   v.first = min(max(a.row_offsets[s], 0), end);
   v.rows = min(max(a.row_offsets[s + 1], v.first), end) - v.first;
+  v.refused = a.slot && v.rows && a.slot[v.first] < 0 ? v.rows : 0;
+  if (v.refused) v.rows = 0;
   v.accepted = max(v.rows - 1, 0), v.rejected = -1;
   return v;
 }
@@ -218,7 +221,8 @@ __device__ inline void put_down(const VerifyArgs& a, int s, const Verdict& v) {
     if (v.rows == 0) a.next_token[s] = -1;
   }
   if (a.position_out)
-    for (int i = threadIdx.x; i < v.rows; i += blockDim.x) a.position_out[v.first + i] = a.row_position[v.first + i] + 1 + v.accepted;
+    for (int i = threadIdx.x; i < v.rows + v.refused; i += blockDim.x)
+      a.position_out[v.first + i] = a.row_position[v.first + i] + (v.refused ? 0 : 1 + v.accepted);
 }
 
 __device__ inline double mark_of(const VerifyArgs& a, int s, double total) {

@@ -1,4 +1,4 @@
-"""Asynchronous decoding over the 8-bit paged cache: its operators together, as a model's forward pass calls them.
+"""Asynchronous decoding over the 8-bit or 4-bit paged cache: the operators together, as a model's forward pass calls them.
 
 A Session owns the device buffers of a batch of requests and, on the host, which thread of a request sees which.  Rows carry the
 tag of the thread that wrote them; a thread is the set of tags that it sees.  A fork gives both the child and the parent a new tag: the child goes on from
@@ -8,6 +8,9 @@ has joined, everything written so far becomes a prefix that all of its rows see,
 A step is begin() with the threads that write a row, then layer() for every layer; nothing in it depends on values on the device, so a step of the same
 threads can be captured into a graph and replayed, each replay one token further (run this file for an example).  Between replays other steps may be
 begun, of other requests too; the captured one keeps its own rows, for which see again().
+
+With rope, layer() turns q and k by the rows' position ids on their way.  With vocab, a step's rows may be drafts: verify() holds them to the target's
+probabilities, and the next begin() or again() takes back those that were not accepted, in a replayed graph as well.
 """
 from __future__ import annotations
 
@@ -16,7 +19,7 @@ from dataclasses import dataclass, field
 
 import torch
 
-from . import kv8
+from . import kv4, kv8, rows
 
 TAGS = 64
 
@@ -37,17 +40,41 @@ class _Request:
 
 
 class Session:
+    cache = None  # the handle of the 4-bit cache; the 8-bit cache's does everything itself
+    places = places_workspace = None  # configuration and workspace of the handle that gives places to the 4-bit cache's rows
+    rows_cfg = rows_workspace = rows = keep = None  # of rope and drafts
+    _verified = _unsettled = False  # drafts wait to be taken back; threads do not know their positions
+
     def __init__(self, *, codes="e4m3", dtype="bf16", n_q_heads, n_kv_heads, head_dim, softmax_scale, n_layers=1, max_requests=1, max_rows=256,
-                 page_tokens=16, n_phys_pages, pages_per_request, slopes=None, logit_cap=0.0, device="cuda:0"):
+                 page_tokens=16, n_phys_pages, pages_per_request, slopes=None, logit_cap=0.0, rope=None, vocab=0, device="cuda:0"):
+        """`codes`: e4m3, int8 or e2m1 (4 bits).  `rope`: arguments of rows.make_config that begin with rope_.  `vocab`: of drafts that are to be verified."""
         self.device = torch.device(device)
-        self.cfg = cfg = kv8.make_config(codes, dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale, n_layers=n_layers, max_requests=max_requests,
-                                         max_rows=max_rows, page_tokens=page_tokens, n_phys_pages=n_phys_pages, pages_per_request=pages_per_request)
-        i32 = dict(dtype=torch.int32, device=self.device)
-        k_shape, v_shape, s_shape = kv8.cache_shapes(cfg)
-        # uninitialised on purpose: what has not been written is never read
-        self.k_codes = torch.empty(k_shape, dtype=torch.uint8, device=self.device)
-        self.v_codes = torch.empty(v_shape, dtype=torch.uint8, device=self.device)
-        self.k_scale, self.v_scale = torch.empty(s_shape, device=self.device), torch.empty(s_shape, device=self.device)
+        sizes = dict(n_layers=n_layers, max_requests=max_requests, max_rows=max_rows, page_tokens=page_tokens, n_phys_pages=n_phys_pages,
+                     pages_per_request=pages_per_request)
+        i32, u8 = dict(dtype=torch.int32, device=self.device), dict(dtype=torch.uint8, device=self.device)
+        # codes and scales are uninitialised on purpose: what has not been written is never read
+        if codes == "e2m1":
+            self.cfg = cfg = kv4.make_config(dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale, **sizes)
+            self.k_codes, self.v_codes, self.k_scale, self.v_scale = (torch.empty(s, **u8) for s in kv4.cache_shapes(cfg))
+            self.places = kv8.make_config("e4m3", dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale, **{**sizes, "n_layers": 1})
+            self.places_workspace = torch.empty(kv8.query_workspace_bytes(self.places), **u8)
+        else:
+            self.cfg = cfg = kv8.make_config(codes, dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale, **sizes)
+            k_shape, v_shape, s_shape = kv8.cache_shapes(cfg)
+            self.k_codes, self.v_codes = torch.empty(k_shape, **u8), torch.empty(v_shape, **u8)
+            self.k_scale, self.v_scale = torch.empty(s_shape, device=self.device), torch.empty(s_shape, device=self.device)
+        if rope is not None or vocab:
+            turns = {}
+            if rope is not None:
+                td = {kv8.BF16: torch.bfloat16, kv8.F16: torch.float16}[cfg.dtype]
+                self._q, self._k = (torch.empty(max_rows, h, head_dim, dtype=td, device=self.device) for h in (n_q_heads, n_kv_heads))
+                f = torch.as_tensor(rope["rope_frequency"], dtype=torch.float64).to(self.device)
+                turns = dict(n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, **{**rope, "rope_frequency": f})
+            self.rows_cfg = rows.make_config(max_rows=max_rows, vocab=vocab, max_sequences=max_requests if vocab else 0, **turns)
+            self.rows_workspace = torch.empty(rows.query_workspace_bytes(self.rows_cfg), **u8)
+        if vocab:
+            self.keep = torch.zeros(max_requests, **i32)
+            self.accepted, self.next_token = torch.zeros(max_requests, **i32), torch.full((max_requests,), -1, **i32)
         self.page_table = torch.full((max_requests, pages_per_request), -1, **i32)
         self.free_pages = torch.arange(n_phys_pages - 1, -1, -1, **i32)
         self.free_count = torch.full((1,), n_phys_pages, **i32)
@@ -56,7 +83,7 @@ class Session:
         slots = n_phys_pages * page_tokens
         self.slot_tag, self.slot_position = torch.zeros(slots, dtype=torch.uint8, device=self.device), torch.zeros(slots, **i32)
         self.slot = torch.full((max_rows,), -1, **i32)
-        self.workspace = torch.empty(kv8.query_workspace_bytes(cfg), dtype=torch.uint8, device=self.device)
+        self.workspace = torch.empty((kv4 if codes == "e2m1" else kv8).query_workspace_bytes(cfg), **u8)
         self.slopes = None if slopes is None else torch.as_tensor(slopes, dtype=torch.float32, device=self.device)
         self.logit_cap = logit_cap
         self.requests = [_Request() for _ in range(max_requests)]
@@ -67,9 +94,15 @@ class Session:
     def bind(self, stream):
         """Work of later calls goes to this stream; the caller orders it behind what was enqueued before.  A step that had begun goes on with again()."""
         self._stream = stream
-        self.handle = kv8.PastaKv8(self.cfg, self.workspace, page_table=self.page_table, k_codes=self.k_codes, v_codes=self.v_codes,
-                                   k_scale=self.k_scale, v_scale=self.v_scale, free_pages=self.free_pages, slot_tag=self.slot_tag,
-                                   slot_position=self.slot_position, stream=stream.cuda_stream)
+        shared = dict(page_table=self.page_table, slot_tag=self.slot_tag, slot_position=self.slot_position, stream=stream.cuda_stream)
+        held = dict(k_codes=self.k_codes, v_codes=self.v_codes, k_scale=self.k_scale, v_scale=self.v_scale)
+        if self.places is not None:
+            self.handle = kv8.PastaKv8(self.places, self.places_workspace, free_pages=self.free_pages, **shared)
+            self.cache = kv4.PastaKv4(self.cfg, self.workspace, **held, **shared)
+        else:
+            self.handle = kv8.PastaKv8(self.cfg, self.workspace, free_pages=self.free_pages, **held, **shared)
+        if self.rows_cfg is not None:
+            self.rows = rows.PastaRows(self.rows_cfg, self.rows_workspace, stream=stream.cuda_stream)
         if self._step is not None:  # memory of the new stream's, that it may be given back behind its work; the old one's, not ahead of the copies
             old = self._step
             with torch.cuda.stream(stream):
@@ -101,6 +134,7 @@ class Session:
         """A child that sees what `parent` sees now.  `position`: id of its first row (estimated ids may leave gaps); else it counts on."""
         if not parent.alive:
             raise ValueError("forks a living thread")
+        self._must_be_settled()
         r = self.requests[parent.request]
         free = TAGS - bin(r.used).count("1")
         if free < 2:
@@ -120,6 +154,7 @@ class Session:
         for o in others:
             if o is thread or not o.alive or o.request != thread.request:
                 raise ValueError("joins living threads of one request, each once")
+        self._must_be_settled()
         for o in others:
             thread.sees |= o.sees
             o.alive = False
@@ -127,10 +162,12 @@ class Session:
         if len(r.threads) == 1:
             # everything written is seen: a prefix, as long as the device says (a step may have been refused), and the tags are free again
             r.used, thread.tag, thread.sees = 1, 0, 1
+            self._take_back()
             self._on_stream(lambda: self.prefix_len[thread.request].copy_(self.length[thread.request]))
 
     def release(self, request):
         """Ends the request's threads and gives its pages back."""
+        self._take_back()
         r = self.requests[request]
         for t in r.threads:
             t.alive = False
@@ -145,6 +182,17 @@ class Session:
                               self.free_count, keep=keep)
         self._on_stream(give_back)
 
+    def _take_back(self):
+        """Drafts that were not accepted, ahead of the next step."""
+        if self._verified:
+            self._on_stream(lambda: self.handle.slots(self.length, torch.zeros(len(self.requests) + 1, dtype=torch.int32, device=self.device), 0, None,
+                                                      self.length, self.free_count, self.free_count, keep=self.keep))
+            self._verified = False
+
+    def _must_be_settled(self):
+        if self._unsettled:
+            raise RuntimeError("a verified step's threads do not know their positions: settle() first")
+
     def _on_stream(self, what):
         with torch.cuda.stream(self._stream):
             what()
@@ -155,6 +203,7 @@ class Session:
 
         A request that the cache has no room for is refused on the device, which the host does not wait for: the positions of its threads go on as if it
         had been served, until refused() sets them back."""
+        self._must_be_settled()
         n = len(rows)
         where = [t.request for t in rows]
         if where != sorted(where) or not all(t.alive for t in rows):
@@ -180,9 +229,11 @@ class Session:
     def _enter(self, step):
         if torch.cuda.is_current_stream_capturing():
             self._captured.append(step)
+        drafts = dict(keep=self.keep) if self._verified else {}
         self.handle.slots(self.length, step["offsets"], step["n"], self.slot, self.length, self.free_count, self.free_count, row_tag=step["tag"],
-                          row_position=step["position"])
-        self.handle.plan(self.length, step["offsets"], step["n"], max_request_rows=step["most"], prefix_len=self.prefix_len, slot=self.slot)
+                          row_position=step["position"], **drafts)
+        step["kept"], self._verified = bool(drafts), False
+        (self.cache or self.handle).plan(self.length, step["offsets"], step["n"], max_request_rows=step["most"], prefix_len=self.prefix_len, slot=self.slot)
         self._step = step
         step["refused"] = None  # (not known)
 
@@ -192,7 +243,8 @@ class Session:
         Captured, the step goes on with rows, tags and positions of its own for as long as the session lives.  They are those of the capture: between
         replays its threads neither fork nor join nor write rows by other calls.  What other requests do is free."""
         def go_on():
-            self._step["position"].add_(self._step["stride"])
+            if not self._verified:  # (verify() has moved positions on)
+                self._step["position"].add_(self._step["stride"])
             self._enter(self._step)
         self._on_stream(go_on)
 
@@ -211,7 +263,8 @@ class Session:
                     t = s["rows"][i]
                     if t.request in s["refused"]:
                         t.position = ids[i]
-                        s["position"][i] -= s["stride"][i]  # (again() adds it)
+                        if not self._verified:
+                            s["position"][i] -= s["stride"][i]  # (again() adds it)
         return s["refused"]
 
     def advanced(self, rows, steps):
@@ -220,12 +273,46 @@ class Session:
             t.position += steps
 
     def layer(self, layer, k_new, v_new, q, out, lse=None):
-        """Appends the step's rows of a layer, then attends: row i sees its own row too."""
-        s = self._step
+        """Appends the step's rows of a layer, then attends: row i sees its own row too.  With rope, q and k come as they are, and are turned here."""
+        s, cache = self._step, self.cache or self.handle
         with torch.cuda.device(self.device):  # (a launch goes by the current device; the stream is the handle's)
-            self.handle.append(layer, self.slot, k_new, v_new, n_rows=s["n"])
-            self.handle.attend(layer, q, out, lse=lse, logit_cap=self.logit_cap, slopes=self.slopes, row_see=s["see"],
+            if self.rows is not None and self.rows_cfg.rope_dims:
+                n = s["n"]
+                self.rows.rotate(s["position"], q, self._q[:n], k_new, self._k[:n], n_rows=n)
+                q, k_new = self._q[:n], self._k[:n]
+            cache.append(layer, self.slot, k_new, v_new, n_rows=s["n"])
+            cache.attend(layer, q, out, lse=lse, logit_cap=self.logit_cap, slopes=self.slopes, row_see=s["see"],
                                row_position=s["position"] if self.slopes is not None else None)
+
+
+    def verify(self, token, target, draw, last_draw, draft=None):
+        """Holds the step's rows to the target's probabilities: of each request's rows, those of one thread, the first is its last token and the others drafts.
+        token, draw [n]; target, draft [n, vocab]; last_draw [max_requests].  Returns (accepted, next token) of every request, on the device, until the next call.
+
+        The next begin() or again() takes back what was not accepted.  again() goes on behind the accepted rows without the host; begin(), fork() and join()
+        want settle() first.  A captured step that ends with verify() begins behind a verified one."""
+        s = self._step
+        owner = {}
+        for t in s["rows"]:
+            if owner.setdefault(t.request, t) is not t:
+                raise ValueError(f"request {t.request}: rows of several threads are no drafts")
+        if torch.cuda.is_current_stream_capturing() and not s["kept"]:
+            raise RuntimeError("a captured step that ends with verify() has to begin behind a verified one, or its replays would keep all drafts")
+        with torch.cuda.device(self.device):
+            self.rows.verify(s["offsets"], token, target, draw, last_draw, self.accepted, self.next_token, draft=draft, length=self.length, keep=self.keep,
+                             row_position=s["position"], position_out=s["position"], slot=self.slot, n_sequences=len(self.requests), n_rows=s["n"])
+        self._verified = self._unsettled = True
+        return self.accepted, self.next_token
+
+    def settle(self):
+        """Waits for the device, after verify() or replays that end with it, and tells the step's threads their positions.  Returns the requests' accepted drafts."""
+        if self._unsettled:
+            with torch.cuda.stream(self._stream):
+                ids = self._step["position"].tolist()
+            for i in reversed(range(self._step["n"])):  # (of a thread's rows the first one's)
+                self._step["rows"][i].position = ids[i]
+            self._unsettled = False
+        return self.accepted.tolist()
 
 
 def main():

@@ -56,7 +56,7 @@ class RotateArgs(C.Structure):
 class VerifyArgs(C.Structure):
     _fields_ = [
         ("struct_size", C.c_uint32), ("flags", C.c_uint32), ("n_sequences", C.c_int32), ("n_rows", C.c_int32), ("dtype", C.c_int32),
-        ("row_offsets", C.c_void_p), ("token", C.c_void_p), ("target", C.c_void_p), ("draft", C.c_void_p), ("target_stride", C.c_int64),
+        ("row_offsets", C.c_void_p), ("token", C.c_void_p), ("slot", C.c_void_p), ("target", C.c_void_p), ("draft", C.c_void_p), ("target_stride", C.c_int64),
         ("draft_stride", C.c_int64), ("draw", C.c_void_p), ("last_draw", C.c_void_p), ("length", C.c_void_p), ("row_position", C.c_void_p),
         ("accepted", C.c_void_p), ("next_token", C.c_void_p), ("keep", C.c_void_p), ("position_out", C.c_void_p),
     ]
@@ -170,16 +170,16 @@ class PastaRows(_Handle):
         return self._prepared("rotate", a, (position, q, q_out, k, k_out))
 
     def prepare_verify(self, row_offsets, token, target, draw, last_draw, accepted, next_token, *, draft=None, length=None, keep=None, row_position=None,
-                       position_out=None, n_sequences=None, n_rows=None, dtype=None):
+                       position_out=None, slot=None, n_sequences=None, n_rows=None, dtype=None):
         S = n_sequences if n_sequences is not None else int(row_offsets.shape[0]) - 1
         n = n_rows if n_rows is not None else int(token.shape[0])
         dtype, of = _row_type(dtype, target)
         (p, ps), (q, qs) = self._distributions(target, n, of, "target"), self._distributions(draft, n, of, "draft")
         i32 = lambda x, k, what: _p(x, _I32, (k,), what)  # noqa: E731
-        a = VerifyArgs(C.sizeof(VerifyArgs), 0, S, n, dtype, i32(row_offsets, S + 1, "row_offsets"), i32(token, n, "token"), p, q, ps, qs,
+        a = VerifyArgs(C.sizeof(VerifyArgs), 0, S, n, dtype, i32(row_offsets, S + 1, "row_offsets"), i32(token, n, "token"), i32(slot, n, "slot"), p, q, ps, qs,
                        _p(draw, _F32, (n,), "draw"), _p(last_draw, _F32, (S,), "last_draw"), i32(length, S, "length"), i32(row_position, n, "row_position"),
                        i32(accepted, S, "accepted"), i32(next_token, S, "next_token"), i32(keep, S, "keep"), i32(position_out, n, "position_out"))
-        return self._prepared("verify", a, (row_offsets, token, target, draw, last_draw, accepted, next_token, draft, length, keep, row_position, position_out))
+        return self._prepared("verify", a, (row_offsets, token, target, draw, last_draw, accepted, next_token, draft, length, keep, row_position, position_out, slot))
 
     def _distributions(self, x, n, of, what):
         """(address, values between rows) of a tensor [n, vocab or more]."""

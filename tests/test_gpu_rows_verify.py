@@ -228,6 +228,27 @@ def test_a_few_tokens_hold_everything(V):
     c.check()
 
 
+@pytest.mark.parametrize("V", [300, 40000])
+def test_sequences_that_were_refused_stay_as_they_are(V):
+    c = Case(27, V, [4, 3, 1, 5])
+    want = c.want()
+    slot = torch.arange(c.n, dtype=torch.int32, device="cuda")
+    slot[4:7], slot[7], slot[10] = -1, -1, -1  # (the last one: not a first row, which alone counts)
+    cfg = rows.make_config(vocab=V, max_sequences=4, max_rows=c.n)
+    ws = torch.empty(rows.query_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    acc, nxt, keep, pos = c.out(4), c.out(4), c.out(4), c.out(c.n)
+    h = rows.PastaRows(cfg, ws, stream=torch.cuda.current_stream().cuda_stream)
+    h.verify(torch.from_numpy(c.offs).cuda(), c.token, c.target, c.draw, c.last, acc, nxt, draft=c.draft, length=c.length, keep=keep, row_position=c.position,
+             position_out=pos, slot=slot)
+    torch.cuda.synchronize()
+    length, position = c.length.cpu().numpy(), c.position.cpu().numpy()
+    for s in (1, 2):
+        want[0][s], want[1][s], want[2][s] = 0, -1, length[s]
+        want[3][c.offs[s]:c.offs[s + 1]] = position[c.offs[s]:c.offs[s + 1]]
+    for got, w in zip((acc, nxt, keep, pos), want):
+        assert np.array_equal(got.cpu().numpy(), w)
+
+
 def test_offsets_that_are_wrong_stay_inside_the_arrays():
     for V in (300, 40000):
         c = Case(21, V, [3, 3, 3])

@@ -98,12 +98,12 @@ def test_verify_refusals():
                      (dict(target=None), rows.E_INVAL), (dict(draw=None), rows.E_INVAL), (dict(last_draw=None), rows.E_INVAL), (dict(accepted=None), rows.E_INVAL),
                      (dict(next_token=None), rows.E_INVAL), (dict(length=None), rows.E_INVAL), (dict(keep=None), rows.E_INVAL),
                      (dict(row_position=None), rows.E_INVAL), (dict(position_out=None), rows.E_INVAL), (dict(target=FAKE + 2), rows.E_INVAL),
-                     (dict(draft=FAKE + 1, dtype="bf16"), rows.E_INVAL), (dict(accepted=FAKE + 2), rows.E_INVAL), (dict(n_sequences=0), rows.OK)):
+                     (dict(draft=FAKE + 1, dtype="bf16"), rows.E_INVAL), (dict(accepted=FAKE + 2), rows.E_INVAL), (dict(slot=FAKE + 1), rows.E_INVAL), (dict(n_sequences=0), rows.OK)):
         assert h.prepare_verify(**{**good, **kw})() == code, kw
     assert verifies(workspace=None).prepare_verify(**good)() == rows.E_INVAL
     assert rotates().prepare_verify(**good)() == rows.E_INVAL  # a handle for rotate
     for field, value in (("target_stride", 99999), ("draft_stride", -100000), ("target_stride", 1 << 41)):
-        a = rows.VerifyArgs(C.sizeof(rows.VerifyArgs), 0, 4, 9, rows.F32, *[FAKE] * 4, 0, 0, *[FAKE] * 8)
+        a = rows.VerifyArgs(C.sizeof(rows.VerifyArgs), 0, 4, 9, rows.F32, *[FAKE] * 5, 0, 0, *[FAKE] * 8)
         setattr(a, field, value)
         assert rows.load_library().pasta_rows_verify(h._h, C.byref(a)) == rows.E_INVAL, field
 
