@@ -122,7 +122,8 @@ int32_t pasta_kv4_read(pasta_kv4 *h, const pasta_kv4_read_args *a);
  * one whose V does, too (out, not lse).  K enters the products exactly; q does, too; the
  * softmax weights, each times its token's V scale and in units of the row's largest such product,
  * enter the product with V as fp16: what is 2^-25 of the largest or less adds to the sums,
- * but nothing to out.  q . K has to stay within fp32's range.                    */
+ * but nothing to out.  Scores are held in fp32, which tells those beyond 2^22 in magnitude
+ * no longer apart: there a row's weights, and with them out and lse, can be anything.  */
 int32_t pasta_kv4_plan(pasta_kv4 *h, const pasta_kv8_plan_args *a);
 int32_t pasta_kv4_attend(pasta_kv4 *h, const pasta_kv8_attend_args *a);
 

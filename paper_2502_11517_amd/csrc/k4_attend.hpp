@@ -7,8 +7,9 @@
 //   l   = 2^-ev sum y_j       O = sum y_j 2^(ev_j - ev) V4_j       out = O / l             lse = ln 2 * (m + log2 l)
 //
 // ev is the largest ev_j of 16 tokens.
-//   q . K   bf16 operands.  A code times its scale is a bf16 number, which one conversion gives of two codes: K's scales, one to a token and 32 dims, cost
-//           nothing (and 255 among them gives numbers that are none).  bf16 rows of q enter as they are; fp16's 11 bits as two bf16 numbers, in two products.
+//   q . K   operands of q's type, which enters as it is.  A code times its scale is a bf16 number, which one conversion gives of two codes: K's scales, one to a
+//           token and 32 dims, cost nothing (and 255 among them gives numbers that are none).  In fp16 it is one, too, in units of a power of two from which the
+//           scales are at most 2^13 away; a wave goes by that of its first token, and where scales are further away a pair's products are taken window by window.
 //   P . V   fp16 operands.  A token's V scale must stay outside of the product over tokens: a power of two up to 2^-8 below the block's largest, times which
 //           the weight, rounded to fp16 before that, stays as exact.  Where a block's scales are further apart, or one of them is further below the largest so
 //           far, or not a number, the step takes scores t_j + ev_j instead, token by token, and sums l from t_j apart (rare: V's rows of a model differ by
@@ -52,28 +53,6 @@ __device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head
   }
 }
 
-// A piece of Q as operands: bf16's bits, or fp16's value as the sum of two bf16 numbers (8 bits and the rest, which is exact).
-template <int PARTS>
-__device__ inline void operands(bool negate, const uint4v& raw, uint4v (&q)[PARTS]) {
-  if constexpr (PARTS == 1) {
-    q[0] = raw;
-  } else {
-    union { uint4v w; half8 h; } x{raw};
-    union { bf16x8 b; uint4v w; } high, low;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float y = (float)x.h[i];
-      high.b[i] = (__bf16)y;
-      low.b[i] = (__bf16)(y - (float)high.b[i]);
-    }
-    q[0] = high.w, q[1] = low.w;
-  }
-  if (__builtin_expect(negate, 0)) {  // (the same for all lanes)
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) q[p] ^= uint4v{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
-  }
-}
-
 // 32 tokens whose codes and scales a lane holds its pieces of.
 template <int D>
 struct Codes {
@@ -106,13 +85,51 @@ __device__ inline void load_v(const AttendArgs& a, int at0, int at1, Codes<D>& c
   for (int x = 0; x < D / 64; ++x) c.v[x] = *(const uint4v*)(from + x * 512);
 }
 
-__device__ inline bf16x8 k_operand(uint32_t w, float scale) {
-  union { bf16x2 p[4]; bf16x8 v; } r;
-  r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
-  r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
-  r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
-  r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
-  return r.v;
+// Eight codes of K under their scale (or that in other units), as an operand.
+template <bool F16>
+__device__ inline uint4v k_operand(uint32_t w, float scale) {
+  if constexpr (F16) {
+    union { half2v p[4]; uint4v v; } r;
+    r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0);
+    r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1);
+    r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2);
+    r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
+    return r.v;
+  } else {
+    union { bf16x2 p[4]; uint4v v; } r;
+    r.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+    r.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+    r.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+    r.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+    return r.v;
+  }
+}
+
+__device__ inline float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
+template <bool F16>
+__device__ inline float16v product(const uint4v& k, const uint4v& q, const float16v& s) {
+  union { uint4v w; half8 h; bf16x8 b; } x{k}, y{q};
+  if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(x.h, y.h, s, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b, y.b, s, 0, 0, 0);
+}
+
+// fp16's window of K's scales: a code times 2^-13 .. 2^13 is a normal fp16 number.  (Down to 2^-23 it is one, too, but of those sums of products keep fewer bits:
+// scores of 2^-23 were ten times as far off.)  `unit` is the byte of the scale that is 1.
+constexpr int kAside = 13;
+__device__ inline float unit_scale(int unit) { return pow2f(unit - 127); }
+
+// Whether all scales of the lane's token lie in the window.
+template <int D>
+__device__ inline bool in_window(uint32_t ks, int unit) {
+  using short2v = __attribute__((ext_vector_type(2))) unsigned short;
+  union { uint32_t w; short2v v; } even, odd, low, high;
+  even.w = ks & 0x00ff00ffu, odd.w = D == 128 ? ks >> 8 & 0x00ff00ffu : ks >> 8;
+  if constexpr (D == 64) even.w |= even.w << 16, odd.w |= odd.w << 16;  // (two scales)
+  low.w = (uint32_t)(unit - kAside) * 0x10001u, high.w = (uint32_t)(unit + kAside) * 0x10001u;
+  const short2v most = __builtin_elementwise_max(even.v, odd.v), least = __builtin_elementwise_min(even.v, odd.v);
+  union { short2v v; uint32_t w; } off{__builtin_elementwise_sub_sat(most, high.v) | __builtin_elementwise_sub_sat(low.v, least)};
+  return off.w == 0;
 }
 
 __device__ inline half8 v_operand(uint32_t w) {
@@ -263,9 +280,50 @@ __device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[
   }
 }
 
+// Scores of a pair whose K scales do not share a window, fp16: window by window, the smallest first, in units that go up with them (what gets lost so is 2^-126 of
+// the next one's).  Returns the last one's unit.
+template <int D, int G, int N>
+__device__ inline int windows(const Codes<D>& c, bool there, const uint4v* q, float16v (&s)[G][N], int n) {
+  constexpr int kWide = 2 * kAside, kWindows = 256 / kWide + 1;
+  const int half = (threadIdx.x >> 5) & 1;
+  int byte[D / 64], unit = -1;
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x) byte[x] = there ? (int)(c.ks >> (8 * (2 * x + half)) & 255u) : 127;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[g][n][i] = 0.f;
+#pragma unroll 1
+  for (int w = 0; w < kWindows; ++w) {
+    bool some = w == kWindows - 1 && unit < 0;
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) some |= byte[x] != kNone && byte[x] / kWide == w;
+    if (!__any(some)) continue;
+    const int next = kWide * w + kAside;
+    const float down = unit < 0 ? 1.f : pow2f(max(unit - next, -126));
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[g][n][i] *= down;
+    unit = next;
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) {
+      const bool mine = byte[x] == kNone || byte[x] / kWide == w;  // (not a number: in every window)
+      const float scale = __uint_as_float(byte[x] == kNone ? 0x7f800000u : (uint32_t)((mine ? byte[x] - next : 0) + 127) << 23);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const uint4v codes = k_operand<true>(mine ? c.k[x][y] : 0u, scale);
+#pragma unroll
+        for (int g = 0; g < G; ++g) s[g][n] = product<true>(codes, q[(g * (D / 16) + 4 * x + y) * 64 + (threadIdx.x & 63)], s[g][n]);
+      }
+    }
+  }
+  return unit;
+}
+
 // One step of a wave: N pairs whose codes are in c, against G groups of 32 rows.  `ahead` is called when K may be overwritten, `behind` when V may.
-template <int D, int PARTS, int KIND, int G, int N, class Ahead, class Behind>
-__device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&r)[G], const bf16x8* q, State<D> (&z)[G], Codes<D> (&c)[N],
+template <int D, bool F16, int KIND, int G, int N, class Ahead, class Behind>
+__device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&r)[G], const uint4v* q, int unit, State<D> (&z)[G], Codes<D> (&c)[N],
                             const int (&absent)[N], const Marks (&marks)[N], const int (&t0)[N], int& most, Ahead ahead, Behind behind) {
   float16v s[G][N];
 #pragma unroll
@@ -281,34 +339,50 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
   for (int x = 0; x < D / 64; ++x) {
     float scale[N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) scale[n] = __uint_as_float((c[n].ks >> (8 * (2 * x + half)) & 255u) << 23);
+    for (int n = 0; n < N; ++n) {
+      const uint32_t bits = (c[n].ks >> (8 * (2 * x + half)) & 255u) << 23;
+      scale[n] = __uint_as_float(F16 ? bits + ((uint32_t)(127 - unit) << 23) : bits);
+    }
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
-      bf16x8 codes[N];
+      uint4v codes[N];
 #pragma unroll
-      for (int n = 0; n < N; ++n) codes[n] = k_operand(c[n].k[x][y], scale[n]);
+      for (int n = 0; n < N; ++n) codes[n] = k_operand<F16>(c[n].k[x][y], scale[n]);
 #pragma unroll
-      for (int g = 0; g < G; ++g)
+      for (int g = 0; g < G; ++g) {
+        const uint4v row = q[(g * (D / 16) + 4 * x + y) * 64 + (threadIdx.x & 63)];
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
-          const bf16x8 row = q[((g * PARTS + part) * (D / 16) + 4 * x + y) * 64 + (threadIdx.x & 63)];
-#pragma unroll
-          for (int n = 0; n < N; ++n) s[g][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(codes[n], row, s[g][n], 0, 0, 0);
-        }
+        for (int n = 0; n < N; ++n) s[g][n] = product<F16>(codes[n], row, s[g][n]);
+      }
     }
   }
   __builtin_amdgcn_s_setprio(0);
+  float f[G][N];
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int n = 0; n < N; ++n) f[g][n] = F16 ? uniform(a.scale_log2 * unit_scale(unit)) : a.scale_log2;
+  if constexpr (F16) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int m = threadIdx.x & 31, at = t0[n] + (m & 4 ? 16 : 0) + (m >> 3) * 4 + (m & 3);  // the lane's token of the first product
+      const bool there = at < u.hi && !(absent[n] >> (m >> 2 & 1) & 1);
+      if (__builtin_expect(__any(there && !in_window<D>(c[n].ks, unit)), 0)) {
+        const int last = windows(c[n], there, q, s, n);
+#pragma unroll
+        for (int g = 0; g < G; ++g) f[g][n] = uniform(a.scale_log2 * unit_scale(last));
+      }
+    }
+  }
   Marks m[N];
   Scales p[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) m[n] = marks[n], p[n] = scales_of<D>(c[n], absent[n], t0[n], u.hi, most);
   ahead();
-  float f[G][N];
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      f[g][n] = a.scale_log2;
       const Pair pair{1.f, 0.f, absent[n], 0, 0};
       if constexpr (KIND == kMarked)
         finish_scores<KIND>(a, u.prefix, u.hi, t0[n], pair, Marked{m[n], r[g].position, r[g].by_tag}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
@@ -336,11 +410,11 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
 // A unit of G groups of 32 rows.  Every wave takes a quarter of the tokens, pairs wave, wave + 4, ...; the four meet at the end.  Two pairs at a time, so that a
 // softmax's way through its lanes is taken once for 64 tokens; with two groups and 128 dims there are registers for one.  Q's operands lie in LDS, a copy for
 // each wave (where its output goes later).
-template <int D, int PARTS, int KIND, int G>
+template <int D, bool F16, int KIND, int G>
 __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int listed, int head, float* lds) {
   constexpr bool MARKS = KIND == kMarked;
   constexpr int N = G == 1 || D == 64 ? 2 : 1;
-  static_assert(G * PARTS * (D / 16) * 64 * 16 <= kRows * kPitch<D> * 4, "Q's operands lie where the output goes");
+  static_assert(G * (D / 16) * 64 * 16 <= kRows * kPitch<D> * 4, "Q's operands lie where the output goes");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 31, half = lane >> 5;
   const int n_pairs = max((((u.hi - u.lo + 31) >> 5) - wave + 3) >> 2, 0);  // this wave's
   uint4v* q = (uint4v*)(lds + wave * kRows * kPitch<D>);
@@ -384,14 +458,18 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
     for (int g = 0; g < G; ++g) {
       if (g) k4::request_rows<D, MARKS>(a, u, head, g * kRows, r[g], raw);
       if constexpr (MARKS) r[g].by_tag = rows_by_tag(r[g].see, a.g_shift);
+      const uint32_t sign = a.negate ? 0x80008000u : 0u;
+      if (a.negate)  // (the same for all lanes)
 #pragma unroll
-      for (int y = 0; y < D / 16; ++y) {
-        uint4v x[PARTS];
-        operands<PARTS>(a.negate, raw[y], x);
+        for (int y = 0; y < D / 16; ++y) raw[y] ^= uint4v{sign, sign, sign, sign};
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) q[((g * PARTS + part) * (D / 16) + y) * 64 + lane] = x[part];
-      }
+      for (int y = 0; y < D / 16; ++y) q[(g * (D / 16) + y) * 64 + lane] = raw[y];
     }
+  }
+  int unit = 127;
+  if constexpr (F16) {
+    const int byte = __builtin_amdgcn_readfirstlane(c[0].ks) & 255;  // of the wave's first token
+    unit = (gone & 1) || byte == kNone ? 127 : min(max(byte, kEMin + 127), kEMax + 127);
   }
 #pragma unroll
   for (int g = 0; g < G; ++g) start(z[g]);
@@ -400,7 +478,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
     int t0[N], absent[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) t0[n] = token(i + n), absent[n] = absent_of(i + n);
-    k4::step<D, PARTS, KIND, G, N>(a, u, r, (const bf16x8*)q, z, c, absent, marks, t0, most,
+    k4::step<D, F16, KIND, G, N>(a, u, r, q, unit, z, c, absent, marks, t0, most,
       [&] {
         if (i + N >= n_pairs) return;
         if (((i + N) & 31) == 0) find(i + N);
@@ -420,7 +498,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
     if (i < n_pairs) {
       const int t0[1] = {token(i)}, absent[1] = {absent_of(i)};
       const Marks last[1] = {marks[0]};
-      k4::step<D, PARTS, KIND, G, 1>(a, u, r, (const bf16x8*)q, z, *(Codes<D>(*)[1]) & c, absent, last, t0, most, [] {}, [] {});
+      k4::step<D, F16, KIND, G, 1>(a, u, r, q, unit, z, *(Codes<D>(*)[1]) & c, absent, last, t0, most, [] {}, [] {});
     }
   }
   // The four waves meet, group after group.  Each gives three quarters of its output to the others and joins the fourth with theirs: quarter y of a lane's
@@ -495,11 +573,12 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
   }
 }
 
-// Two groups at a time do not fit the registers with 128 dims and scores that are capped, lowered or hidden by tags, nor LDS with two parts of Q: then a work-group (blockIdx.y) takes each.
-template <int D, int PARTS, int KIND>
-constexpr bool kApart = PARTS == 2 || (D == 128 && KIND != kPlain);
+// Two groups at a time do not fit the registers with 128 dims and scores that are capped, lowered or hidden by tags: then a work-group (blockIdx.y) takes each.
+// (2048 rows over 8k tokens, plain: 336 us in bf16, 348 in fp16, which spills a few registers in `rare`; a work-group each 390.)
+template <int D, int KIND>
+constexpr bool kApart = D == 128 && KIND != kPlain;
 
-template <int D, int PARTS, bool MANY, int KIND>
+template <int D, bool F16, bool MANY, int KIND>
 __global__ __launch_bounds__(256, 2) void k4_attend(AttendArgs a) {
   __shared__ __attribute__((aligned(16))) float lds[4 * kRows * kPitch<D> + 4 * kRows * 2];
   const int head = blockIdx.x % a.g.Hkv, unit = blockIdx.x / a.g.Hkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -507,19 +586,19 @@ __global__ __launch_bounds__(256, 2) void k4_attend(AttendArgs a) {
   // the lane's block, asked for together with the unit: pairs are dealt out to the four waves
   const int listed = a.unit_blocks[unit * kUnitBlocks + min(2 * (wave + 4 * (lane >> 1)) + (lane & 1), kUnitBlocks - 1)];
   asm volatile("" ::"s"(u.request), "s"(u.s0), "s"(u.pos0), "s"(u.lo), "s"(u.hi), "s"(u.prefix), "s"(u.part));  // (one load, ahead of the branch)
-  if constexpr (MANY && kApart<D, PARTS, KIND>) {
+  if constexpr (MANY && kApart<D, KIND>) {
     const int first = blockIdx.y * kRows;
     u.s0 += first, u.n_rows = min(u.n_rows - first, kRows), u.pos0 += first >> a.g_shift;
     if (u.part >= 0) u.part += first;
   }
   if (u.n_rows <= 0) return;
-  if constexpr (MANY && !kApart<D, PARTS, KIND>) {
+  if constexpr (MANY && !kApart<D, KIND>) {
     if (u.n_rows > kRows)
-      k4::attend_unit<D, PARTS, KIND, 2>(a, u, listed, head, lds);
+      k4::attend_unit<D, F16, KIND, 2>(a, u, listed, head, lds);
     else
-      k4::attend_unit<D, PARTS, KIND, 1>(a, u, listed, head, lds);
+      k4::attend_unit<D, F16, KIND, 1>(a, u, listed, head, lds);
   } else {
-    k4::attend_unit<D, PARTS, KIND, 1>(a, u, listed, head, lds);
+    k4::attend_unit<D, F16, KIND, 1>(a, u, listed, head, lds);
   }
 }
 

@@ -162,12 +162,12 @@ extern "C" int32_t pasta_kv4_plan(pasta_kv4* h, const pasta_kv8_plan_args* a) {
 
 namespace {
 
-template <int D, int PARTS>
+template <int D, bool F16>
 void launch_attend(const k4::AttendArgs& k, const k8::Planned& plan, hipStream_t s) {
   const int64_t groups = plan.most.units * k.g.Hkv;
   k8::by_kind(k, plan, [&](auto many, auto kind) {
-    const dim3 grid((unsigned)groups, many.value && k4::kApart<D, PARTS, kind.value> ? k8::kWideRows / k8::kRows : 1);
-    k4::k4_attend<D, PARTS, many.value, kind.value><<<grid, 256, 0, s>>>(k);
+    const dim3 grid((unsigned)groups, many.value && k4::kApart<D, kind.value> ? k8::kWideRows / k8::kRows : 1);
+    k4::k4_attend<D, F16, many.value, kind.value><<<grid, 256, 0, s>>>(k);
   });
 }
 
@@ -185,9 +185,9 @@ extern "C" int32_t pasta_kv4_attend(pasta_kv4* h, const pasta_kv8_attend_args* a
   k.k_scale = c.k_scale + at * 16 * (c.head_dim / 32), k.v_scale = c.v_scale + at * 16;
   hipStream_t s = (hipStream_t)c.hip_stream;
   if (c.dtype == PASTA_BF16)
-    c.head_dim == 128 ? launch_attend<128, 1>(k, h->plan, s) : launch_attend<64, 1>(k, h->plan, s);
+    c.head_dim == 128 ? launch_attend<128, false>(k, h->plan, s) : launch_attend<64, false>(k, h->plan, s);
   else
-    c.head_dim == 128 ? launch_attend<128, 2>(k, h->plan, s) : launch_attend<64, 2>(k, h->plan, s);
+    c.head_dim == 128 ? launch_attend<128, true>(k, h->plan, s) : launch_attend<64, true>(k, h->plan, s);
   k8::launch_merge(k, h->plan, s);
   return launched();
 }

@@ -303,6 +303,49 @@ def test_scales_of_k_far_apart(n):
     c.check()
 
 
+@pytest.mark.parametrize("n", [8, 80])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("far", [10, 12, 13, 14, 18, 24, 30, 34])
+@pytest.mark.parametrize("down", [False, True])
+def test_scales_of_k_beyond_a_window_of_fp16(n, D, far, down):
+    """Groups of dims 2^far apart, in all tokens, in some, and not a number in one; rows that see one group, the other, or both, in sizes that make scores of 1.
+    (Where only some tokens have the small scale, the rows made for it see those alone: the others' scores would be 2^far, and from 2^22 on fp32 does not tell
+    scores apart.)"""
+    for some in (False, True):
+        c = Case([n, D, far, down, some], "f16", 8, 2, D, length=[300], rows=[n], scale=2.0 ** 14, k_spread=0)
+        t = np.arange(300)
+        slots = c.table[0, t // 16] * 16 + t % 16
+        c.tag[:] = 2
+        for i, s in enumerate(slots):
+            k = c.c.ks[s // 16, :, s % 16]
+            k[:] = 127
+            if not some or i % 37 == 5 or i > 250:
+                k[:, 0 if down else 1], c.tag[s] = 127 - far, 1
+        c.c.ks[slots[280] // 16, 0, slots[280] % 16, 0] = ref.NONE
+        q = c.q.double().numpy().reshape(n, 8, -1, 32)
+        for i in range(n):
+            low = 0 if down else 1
+            q[i] *= 2.0 ** -17
+            if i % 3 == 0:
+                q[i, :, [g for g in range(D // 32) if g != low]] = 0.0
+                q[i, :, low] *= 2.0 ** min(far, 30)
+            elif i % 3 == 1:
+                q[i, :, low] = 0.0
+        c.q = torch.from_numpy(q.reshape(n, 8, D)).to(torch.float16)
+        c.check(see=np.where(np.arange(n) % 3 == 0, 1 << 1, -1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_scales_of_k_all_over_their_range(dtype):
+    """One token's scale in each window that there is; the scores of the largest ones decide."""
+    c = Case([29], dtype, length=[64], rows=[5], scale=2.0 ** -115)
+    t = np.arange(64)
+    slots = c.table[0, t // 16] * 16 + t % 16
+    for i, s in enumerate(slots):
+        c.c.ks[s // 16, :, s % 16] = 27 + (i * 29) % 220
+    c.check()
+
+
 @pytest.mark.parametrize("n", [3, 40])
 def test_pages_with_bad_numbers_are_seen_by_nobody(n):
     c = Case([n, 17], length=[200, 40], rows=[n, 4])
