@@ -10,7 +10,7 @@ threads can be captured into a graph and replayed, each replay one token further
 begun, of other requests too; the captured one keeps its own rows, for which see again().
 
 With rope, layer() turns q and k by the rows' position ids on their way.  With vocab, a step's rows may be drafts: verify() holds them to the target's
-probabilities, and the next begin() or again() takes back those that were not accepted, in a replayed graph as well.
+probabilities, and the next begin() or again() takes back those that were not accepted, in a replayed graph as well.  settle() tells the host how far it went.
 """
 from __future__ import annotations
 
@@ -43,7 +43,7 @@ class Session:
     cache = None  # the handle of the 4-bit cache; the 8-bit cache's does everything itself
     places = places_workspace = None  # configuration and workspace of the handle that gives places to the 4-bit cache's rows
     rows_cfg = rows_workspace = rows = keep = None  # of rope and drafts
-    _verified = _unsettled = False  # drafts wait to be taken back; threads do not know their positions
+    _unsettled = False  # threads do not know their positions
 
     def __init__(self, *, codes="e4m3", dtype="bf16", n_q_heads, n_kv_heads, head_dim, softmax_scale, n_layers=1, max_requests=1, max_rows=256,
                  page_tokens=16, n_phys_pages, pages_per_request, slopes=None, logit_cap=0.0, rope=None, vocab=0, device="cuda:0"):
@@ -73,6 +73,8 @@ class Session:
             self.rows_cfg = rows.make_config(max_rows=max_rows, vocab=vocab, max_sequences=max_requests if vocab else 0, **turns)
             self.rows_workspace = torch.empty(rows.query_workspace_bytes(self.rows_cfg), **u8)
         if vocab:
+            # how much of every request the next step keeps: its length, but for what verify() writes.  (Replays write it unseen by the host, so every step
+            # goes by it, and leaves it as one that is not verified would.)
             self.keep = torch.zeros(max_requests, **i32)
             self.accepted, self.next_token = torch.zeros(max_requests, **i32), torch.full((max_requests,), -1, **i32)
         self.page_table = torch.full((max_requests, pages_per_request), -1, **i32)
@@ -180,14 +182,21 @@ class Session:
             keep[request].zero_()
             self.handle.slots(self.length, torch.zeros(n + 1, dtype=torch.int32, device=self.device), 0, None, self.length, self.free_count,
                               self.free_count, keep=keep)
+            self._keep_all()
         self._on_stream(give_back)
 
     def _take_back(self):
         """Drafts that were not accepted, ahead of the next step."""
-        if self._verified:
-            self._on_stream(lambda: self.handle.slots(self.length, torch.zeros(len(self.requests) + 1, dtype=torch.int32, device=self.device), 0, None,
-                                                      self.length, self.free_count, self.free_count, keep=self.keep))
-            self._verified = False
+        def take():
+            self.handle.slots(self.length, torch.zeros(len(self.requests) + 1, dtype=torch.int32, device=self.device), 0, None, self.length,
+                              self.free_count, self.free_count, keep=self.keep)
+            self._keep_all()
+        if self.keep is not None:
+            self._on_stream(take)
+
+    def _keep_all(self):
+        if self.keep is not None:
+            self.keep.copy_(self.length)
 
     def _must_be_settled(self):
         if self._unsettled:
@@ -221,18 +230,24 @@ class Session:
         signed = [t.sees - (1 << 64) if t.sees >> 63 else t.sees for t in rows]
         times = Counter(id(t) for t in rows)
         self._on_stream(lambda: self._enter(dict(
-            n=n, most=max(count), rows=list(rows), offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8), see=dev(signed, torch.int64),
+            n=n, most=max(count), rows=list(rows), verified=False, offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8), see=dev(signed, torch.int64),
             position=dev(ids, torch.int32), stride=dev([times[id(t)] for t in rows], torch.int32))))
         for t in rows:
             t.position = after[id(t)]
 
     def _enter(self, step):
+        for c in self._captured:
+            if c is not step and any(t is u for t in c["rows"] for u in step["rows"]):
+                c["verified"] = False  # (its threads go on elsewhere, and know their positions from there)
         if torch.cuda.is_current_stream_capturing():
             self._captured.append(step)
-        drafts = dict(keep=self.keep) if self._verified else {}
+        drafts = {}
+        if self.keep is not None:
+            drafts = dict(keep=self.keep)
+            step["next"] = torch.add(step["position"], step["stride"], out=step.get("next"))
         self.handle.slots(self.length, step["offsets"], step["n"], self.slot, self.length, self.free_count, self.free_count, row_tag=step["tag"],
                           row_position=step["position"], **drafts)
-        step["kept"], self._verified = bool(drafts), False
+        self._keep_all()
         (self.cache or self.handle).plan(self.length, step["offsets"], step["n"], max_request_rows=step["most"], prefix_len=self.prefix_len, slot=self.slot)
         self._step = step
         step["refused"] = None  # (not known)
@@ -243,7 +258,9 @@ class Session:
         Captured, the step goes on with rows, tags and positions of its own for as long as the session lives.  They are those of the capture: between
         replays its threads neither fork nor join nor write rows by other calls.  What other requests do is free."""
         def go_on():
-            if not self._verified:  # (verify() has moved positions on)
+            if self.keep is not None:  # (verify() has a say in it)
+                self._step["position"].copy_(self._step["next"])
+            else:
                 self._step["position"].add_(self._step["stride"])
             self._enter(self._step)
         self._on_stream(go_on)
@@ -263,7 +280,9 @@ class Session:
                     t = s["rows"][i]
                     if t.request in s["refused"]:
                         t.position = ids[i]
-                        if not self._verified:
+                        if self.keep is not None:
+                            s["next"][i] = s["position"][i]
+                        else:
                             s["position"][i] -= s["stride"][i]  # (again() adds it)
         return s["refused"]
 
@@ -282,37 +301,40 @@ class Session:
                 q, k_new = self._q[:n], self._k[:n]
             cache.append(layer, self.slot, k_new, v_new, n_rows=s["n"])
             cache.attend(layer, q, out, lse=lse, logit_cap=self.logit_cap, slopes=self.slopes, row_see=s["see"],
-                               row_position=s["position"] if self.slopes is not None else None)
-
+                         row_position=s["position"] if self.slopes is not None else None)
 
     def verify(self, token, target, draw, last_draw, draft=None):
         """Holds the step's rows to the target's probabilities: of each request's rows, those of one thread, the first is its last token and the others drafts.
         token, draw [n]; target, draft [n, vocab]; last_draw [max_requests].  Returns (accepted, next token) of every request, on the device, until the next call.
 
         The next begin() or again() takes back what was not accepted.  again() goes on behind the accepted rows without the host; begin(), fork() and join()
-        want settle() first.  A captured step that ends with verify() begins behind a verified one."""
+        want settle() first, also behind replays of a captured step that ends with verify()."""
         s = self._step
+        if self.keep is None or s is None:
+            raise RuntimeError("verify() wants a session with vocab and a step that has begun")
         owner = {}
         for t in s["rows"]:
             if owner.setdefault(t.request, t) is not t:
                 raise ValueError(f"request {t.request}: rows of several threads are no drafts")
-        if torch.cuda.is_current_stream_capturing() and not s["kept"]:
-            raise RuntimeError("a captured step that ends with verify() has to begin behind a verified one, or its replays would keep all drafts")
         with torch.cuda.device(self.device):
             self.rows.verify(s["offsets"], token, target, draw, last_draw, self.accepted, self.next_token, draft=draft, length=self.length, keep=self.keep,
-                             row_position=s["position"], position_out=s["position"], slot=self.slot, n_sequences=len(self.requests), n_rows=s["n"])
-        self._verified = self._unsettled = True
+                             row_position=s["position"], position_out=s["next"], slot=self.slot, n_sequences=len(self.requests), n_rows=s["n"])
+        s["verified"] = self._unsettled = True
         return self.accepted, self.next_token
 
     def settle(self):
-        """Waits for the device, after verify() or replays that end with it, and tells the step's threads their positions.  Returns the requests' accepted drafts."""
-        if self._unsettled:
-            with torch.cuda.stream(self._stream):
-                ids = self._step["position"].tolist()
-            for i in reversed(range(self._step["n"])):  # (of a thread's rows the first one's)
-                self._step["rows"][i].position = ids[i]
+        """Waits for the device, after verify() or replays that end with it, and tells the threads of such steps their positions.  Returns the requests'
+        accepted drafts."""
+        if self.keep is None:
+            raise RuntimeError("settle() wants a session with vocab")
+        with torch.cuda.stream(self._stream):
+            # (the last step, which may be a copy of a captured one, ahead of those, which replays have moved on)
+            for s in [s for s in (self._step, *self._captured) if s is not None and s["verified"]]:
+                ids = s["next"].tolist()
+                for i in reversed(range(s["n"])):  # (of a thread's rows the first one's)
+                    s["rows"][i].position = ids[i]
             self._unsettled = False
-        return self.accepted.tolist()
+            return self.accepted.tolist()
 
 
 def main():

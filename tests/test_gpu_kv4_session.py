@@ -262,18 +262,95 @@ def test_what_a_session_refuses_of_drafts():
     assert s.length.tolist() == [11 + 1 + 1 + n[0], 0]
 
 
-def test_a_capture_that_would_keep_all_drafts_is_refused():
-    d = Drafted("e4m3", 7)
-    d.prompt(10, 10)
+@pytest.mark.parametrize("seed", [7, 8, 9])
+@pytest.mark.parametrize("verified", [False, True])
+def test_another_request_goes_on_between_replays(verified, seed):
+    """A captured step of one request, begun behind a verified one or not; the other request writes rows in between, and keeps them; each settle() finds the
+    threads where the replays left them."""
+    d = Drafted("e4m3", seed, rows_of=(4, 0))
+    d.prompt(20, 33)
+    one, other = d.threads
     stream = torch.cuda.Stream()
-    stream.wait_stream(torch.cuda.current_stream())
-    d.s.begin([d.threads[0]] * 4 + [d.threads[1]] * 6)
+    d.s.begin([one] * 4)
+    d.body()
+    if not verified:  # four rows more that are kept, as the program says
+        d.s.settle()
+        d.s.begin([one] * 4, list(range(one.position, one.position + 4)))
+        d.count += 1
     torch.cuda.synchronize()
+    at = one.position if not verified else None
+    stream.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(stream):
         d.s.bind(stream)
         graph = torch.cuda.CUDAGraph()
-        with pytest.raises(RuntimeError, match="behind a verified one"):
-            with torch.cuda.graph(graph, stream=stream):
-                d.s.again()
-                d.s.verify(None, None, None, None)
+        with torch.cuda.graph(graph, stream=stream):
+            d.s.again()
+            d.body()
+        rows_of_other, done = 33, 0
+        for replays, more in ((1, 3), (2, 20), (1, 0), (2, 1)):
+            for _ in range(replays):
+                graph.replay()
+            done += replays
+            acc = d.s.settle()
+            log = d.log[:int(d.count)].cpu().numpy()
+            start = 20 + 1 + log[0, 0, 0] if verified else at
+            first = 1 if verified else 2
+            assert acc[0] == log[-1, 0, 0] and one.position == start + sum(1 + log[k, 0, 0] for k in range(first, first + done))
+            assert other.position == rows_of_other
+            if more:
+                d.s.begin([other] * more)
+                for l in range(2):
+                    x = lambda h: torch.zeros(more, h, 64, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+                    d.s.layer(l, x(2), x(2), x(8), x(8))
+                rows_of_other += more
+                torch.cuda.synchronize()
+                assert d.s.length.tolist()[1] == rows_of_other
+    stream.synchronize()
+    d.s._take_back()
     torch.cuda.synchronize()
+    assert d.s.length.tolist() == [one.position, rows_of_other]
+    print("accepted:", d.log[:int(d.count), 0, 0].tolist())
+
+
+def test_a_release_between_a_verified_step_and_the_next():
+    a, b = Drafted("e2m1", 8, rows_of=(4, 0)), Drafted("e2m1", 8, rows_of=(4, 0))
+    for d in (a, b):
+        d.prompt(20, 33)
+        d.s.begin([d.threads[0]] * 4)
+        d.body()
+        if d is a:
+            d.s.release(1)
+        d.s.again()
+        d.body()
+        d.s.settle()
+    assert torch.equal(a.log[:2, :, 0], b.log[:2, :, 0]) and a.threads[0].position == b.threads[0].position
+    (la, ca), (lb, cb) = a.contents(), b.contents()
+    assert la == [lb[0], 0] and lb[1] == 33
+    for l in range(2):
+        assert torch.equal(ca[2 * l][0], cb[2 * l][0]) and torch.equal(ca[2 * l][1], cb[2 * l][1])
+
+
+def test_a_step_verified_twice_goes_by_the_second():
+    a, b = Drafted("e2m1", 9), Drafted("e2m1", 9)
+    for d in (a, b):
+        d.prompt(20, 33)
+        d.s.begin([d.threads[0]] * 4 + [d.threads[1]] * 6)
+        if d is a:
+            n = len(d.request)
+            d.s.verify(torch.full((n,), -1, dtype=torch.int32, device="cuda"), d.target[0, :n], d.draw[0], d.last[0])  # (nothing is accepted)
+        d.body()
+        d.s.again()
+        d.body()
+        d.s.settle()
+    assert torch.equal(a.log[:2], b.log[:2]) and [t.position for t in a.threads] == [t.position for t in b.threads]
+    assert a.contents()[0] == b.contents()[0]
+
+
+def test_a_session_without_a_vocabulary_verifies_nothing():
+    s = Session(codes="e2m1", **SIZES)
+    s.begin([s.open(0)])
+    for call in (lambda: s.verify(None, None, None, None), s.settle):
+        with pytest.raises(RuntimeError, match="vocab"):
+            call()
+    with pytest.raises(RuntimeError, match="begun"):
+        Session(codes="e2m1", vocab=V, **SIZES).verify(None, None, None, None)
