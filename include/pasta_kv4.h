@@ -105,8 +105,9 @@ int32_t pasta_kv4_append(pasta_kv4 *h, const pasta_kv4_append_args *a);
  * slot[] may name slots in any order and more than once (rows in neighbouring slots side
  * by side read fastest); rows whose slot is not in range are left as they were.
  * k_out or v_out may be NULL.  Alignment and strides as above.  n_rows is not bounded by
- * max_rows.
- * Needs the codes and scales that are read.  Errors: E_INVAL, E_DEVICE, E_STATE. */
+ * max_rows, but by 2^27.
+ * Needs the codes and scales that are read.
+ * Errors: E_INVAL, E_CAPACITY, E_DEVICE, E_STATE.                                */
 typedef struct {
   uint32_t struct_size, flags;    /* flags: 0 */
   int32_t layer, n_rows;

@@ -37,7 +37,7 @@ enum { PASTA_ROPE_HALF = 0, PASTA_ROPE_INTERLEAVED = 1 };
  * are then 0.                                                                     */
 typedef struct {
   uint32_t struct_size;      /* sizeof(pasta_rows_config) */
-  int32_t max_rows;          /* most rows of one call */
+  int32_t max_rows;          /* most rows of one call, < 2^24 */
   /* rotate */
   int32_t n_q_heads, n_kv_heads; /* >= 1, together <= 1024 */
   int32_t head_dim;          /* a multiple of 8, <= 256 */

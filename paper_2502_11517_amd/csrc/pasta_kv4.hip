@@ -15,6 +15,7 @@ namespace {
 using k8::aligned;
 using k8::launched;
 
+constexpr int kMaxRead = 1 << 27;  // rows, 16 to a work-group in such calls: a launch has fewer than 2^32 threads
 constexpr uint64_t kMagic = 0x3476'6b61'7473'6170ull;
 
 }  // namespace
@@ -135,6 +136,7 @@ extern "C" int32_t pasta_kv4_read(pasta_kv4* h, const pasta_kv4_read_args* a) {
   if (!a || a->struct_size != sizeof(*a) || a->flags) return PASTA_E_INVAL;
   const pasta_kv4_config& c = h->cfg;
   if (a->layer < 0 || a->layer >= c.n_layers || a->n_rows < 0 || !is_row_type(a->dtype)) return PASTA_E_INVAL;
+  if (a->n_rows > kMaxRead) return PASTA_E_CAPACITY;
   if ((a->k_out && (!c.k_codes || !c.k_scale)) || (a->v_out && (!c.v_codes || !c.v_scale))) return PASTA_E_INVAL;
   k4::RowArgs k{};
   k.k_stride = a->k_stride, k.v_stride = a->v_stride;

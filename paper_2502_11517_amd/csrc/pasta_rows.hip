@@ -13,6 +13,7 @@
 namespace {
 
 constexpr uint64_t kMagic = 0x7277'6b61'7473'6170ull;
+constexpr int kMaxRows = (1 << 24) - 1;  // of a work-group each: a launch has fewer than 2^32 threads
 constexpr int kMaxVocab = 1 << 22, kWholeVocab = 16 * 8 * 256;  // the latter: 16 waves of 8 times 256 tokens
 
 }  // namespace
@@ -37,7 +38,7 @@ uint64_t sums_of(const pasta_rows_config& c) { return (uint64_t)segments_of(c.vo
 uint64_t workspace_of(const pasta_rows_config& c) { return segments_of(c.vocab) ? sums_of(c) * sizeof(double) + c.max_sequences * sizeof(int2) : 0; }
 
 int32_t check(const pasta_rows_config* c) {
-  if (!c || c->struct_size != sizeof(*c) || c->max_rows < 1) return PASTA_E_INVAL;
+  if (!c || c->struct_size != sizeof(*c) || c->max_rows < 1 || c->max_rows > kMaxRows) return PASTA_E_INVAL;
   if (c->rope_dims == 0 && c->vocab == 0) return PASTA_E_INVAL;
   if (c->rope_dims) {
     if (c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_q_heads > 1024 || c->n_kv_heads > 1024 || c->n_q_heads + c->n_kv_heads > 1024) return PASTA_E_INVAL;

@@ -87,7 +87,7 @@ def test_read_refusals():
     h = handle()
     good = dict(layer=1, slot=FAKE, k_out=FAKE, v_out=FAKE, n_rows=400, dtype="f32")
     for kw, code in ((dict(layer=2), kv4.E_INVAL), (dict(layer=-1), kv4.E_INVAL), (dict(n_rows=-1), kv4.E_INVAL), (dict(dtype=5), kv4.E_INVAL),
-                     (dict(slot=None), kv4.E_INVAL), (dict(k_out=None, v_out=None), kv4.E_INVAL), (dict(v_out=FAKE + 4), kv4.E_INVAL),
+                     (dict(n_rows=(1 << 27) + 1), kv4.E_CAPACITY), (dict(slot=None), kv4.E_INVAL), (dict(k_out=None, v_out=None), kv4.E_INVAL), (dict(v_out=FAKE + 4), kv4.E_INVAL),
                      (dict(n_rows=0, slot=None, k_out=None, v_out=None), kv4.OK)):
         assert h.prepare_read(**{**good, **kw})() == code, kw
     assert handle(left_out=["v_scale"]).prepare_read(**good)() == kv4.E_INVAL

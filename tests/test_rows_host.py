@@ -43,7 +43,7 @@ def test_every_declared_symbol_is_exported():
     assert declared <= {l.split()[-1] for l in syms.splitlines() if " T " in l}
 
 
-@pytest.mark.parametrize("kw", [dict(max_rows=0), dict(n_q_heads=0), dict(n_kv_heads=0), dict(n_q_heads=1000, n_kv_heads=25), dict(head_dim=0), dict(head_dim=12),
+@pytest.mark.parametrize("kw", [dict(max_rows=0), dict(max_rows=1 << 24), dict(n_q_heads=0), dict(n_kv_heads=0), dict(n_q_heads=1000, n_kv_heads=25), dict(head_dim=0), dict(head_dim=12),
                                 dict(head_dim=264, rope_dims=8), dict(rope_dims=130), dict(rope_dims=7), dict(rope_dims=-2), dict(rope_layout=2),
                                 dict(rope_magnitude=float("nan")), dict(rope_magnitude=float("inf")), dict(max_sequences=4)])
 def test_configurations_of_rotate_that_are_refused(kw):
@@ -52,7 +52,7 @@ def test_configurations_of_rotate_that_are_refused(kw):
     assert e.value.code == rows.E_INVAL
 
 
-@pytest.mark.parametrize("kw", [dict(max_rows=0), dict(vocab=-1), dict(vocab=(1 << 22) + 1), dict(max_sequences=0), dict(max_sequences=65536), dict(vocab=0),
+@pytest.mark.parametrize("kw", [dict(max_rows=0), dict(max_rows=1 << 24), dict(vocab=-1), dict(vocab=(1 << 22) + 1), dict(max_sequences=0), dict(max_sequences=65536), dict(vocab=0),
                                 dict(head_dim=64), dict(n_q_heads=1)])
 def test_configurations_of_verify_that_are_refused(kw):
     with pytest.raises(rows.PastaError) as e:
