@@ -288,7 +288,7 @@ __device__ inline int windows(const Codes<D>& c, bool there, const uint4v* q, fl
   const int half = (threadIdx.x >> 5) & 1;
   int byte[D / 64], unit = -1;
 #pragma unroll
-  for (int x = 0; x < D / 64; ++x) byte[x] = there ? (int)(c.ks >> (8 * (2 * x + half)) & 255u) : 127;
+  for (int x = 0; x < D / 64; ++x) byte[x] = there ? (int)(c.ks >> (8 * (2 * x + half)) & 255u) : kNone;  // (those have no window)
 #pragma unroll
   for (int g = 0; g < G; ++g)
 #pragma unroll
@@ -469,7 +469,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
   int unit = 127;
   if constexpr (F16) {
     const int byte = __builtin_amdgcn_readfirstlane(c[0].ks) & 255;  // of the wave's first token
-    unit = (gone & 1) || byte == kNone ? 127 : min(max(byte, kEMin + 127), kEMax + 127);
+    unit = (gone & 1) || byte == kNone ? 127 : min(max(byte, kEMin + 127), kNone - 1 - kAside);  // (kNone lies in no window)
   }
 #pragma unroll
   for (int g = 0; g < G; ++g) start(z[g]);

@@ -336,6 +336,34 @@ def test_scales_of_k_beyond_a_window_of_fp16(n, D, far, down):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", [8, 80])
+@pytest.mark.parametrize("byte", [233, 241, 242, 246])
+def test_the_largest_scales_of_k_with_one_that_is_not_a_number(n, byte, dtype):
+    c = Case([31, n, byte], dtype, 8, 2, 64, length=[300], rows=[n], scale=2.0 ** (126 - byte), k_spread=0)
+    t = np.arange(300)
+    slots = c.table[0, t // 16] * 16 + t % 16
+    for s in slots:
+        c.c.ks[s // 16, :, s % 16] = byte
+    c.tag[:], c.tag[slots[40]] = 2, 1
+    c.c.ks[slots[40] // 16, 0, slots[40] % 16, 0] = ref.NONE
+    c.check(see=np.where(np.arange(n) % 2 == 0, 3, 1 << 2))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("length", [1, 30, 300])
+def test_the_smallest_scales_of_k_beyond_a_window(length, dtype):
+    """Tokens behind the last one are in no window, whatever their bytes."""
+    n = min(length, 5)
+    c = Case([32, length], dtype, 8, 2, 64, length=[length], rows=[n], scale=2.0 ** 80, k_spread=0)
+    c.c.ks[:] = 127
+    t = np.arange(length)
+    slots = c.table[0, t // 16] * 16 + t % 16
+    for i, s in enumerate(slots):
+        c.c.ks[s // 16, :, s % 16] = 47 if i % 3 else 27
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_scales_of_k_all_over_their_range(dtype):
     """One token's scale in each window that there is; the scores of the largest ones decide."""
     c = Case([29], dtype, length=[64], rows=[5], scale=2.0 ** -115)
