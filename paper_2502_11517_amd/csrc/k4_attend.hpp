@@ -33,15 +33,16 @@ constexpr int kNear = 8;      // powers of two between a block's V scales that i
 constexpr float kLift = 7.f;  // The base of the scores is set 2^7 below their maximum and follows when that is 2^15 ahead, which fp16 still holds: so its
                               // smallest normal number is 2^-21 of the largest weight or less, times 2^kNear where that is one of a small V scale
 
-// A wave's rows of Q, as pieces of 8 dims: lane n and n + 32 hold row n, group 2x + half of the dims at 4x .. 4x + 3.
-template <int D, bool MARKS>
-__device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head, int first, Rows<D>& r, uint4v (&raw)[D / 16]) {
-  const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
+// A wave's rows of Q, as pieces of 8 dims: lane n and n + 32 hold row n, group 2x + half of the dims at 4x .. 4x + 3.  With 16 rows, lanes n, n + 16, ..
+// each a quarter of the dims.
+template <int D, bool MARKS, int ROWS = kRows>
+__device__ inline void request_rows(const AttendArgs& a, const Unit& u, int head, int first, Rows<D>& r, uint4v (&raw)[D * ROWS / 512]) {
+  const int lane = threadIdx.x & 63, n = lane & (ROWS - 1), part = lane / ROWS;
   r.real = first + n < u.n_rows;
   const int s = u.s0 + (r.real ? first + n : 0);  // (a lane without a row computes the first one's, and nobody looks)
   const uint4v* p = (const uint4v*)((const uint16_t*)a.q + row_address(a, s, head) * D);
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) raw[k] = p[(2 * (k >> 2) + half) * 4 + (k & 3)];
+  for (int k = 0; k < D * ROWS / 512; ++k) raw[k] = p[ROWS == kRows ? (2 * (k >> 2) + part) * 4 + (k & 3) : part * (D / 32) + k];
   r.token = u.pos0 + ((first + n) >> a.g_shift);
   r.first_token = u.pos0 + (first >> a.g_shift);
   r.slope = a.slopes[head * a.g.G + (s & (a.g.G - 1))] * kLog2e;
@@ -155,27 +156,34 @@ __device__ inline int row_largest(int x) {  // of a row of 16 lanes, of which i 
   return max(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xf, 0xf, false));
 }
 
-template <int D>
-__device__ inline Scales scales_of(const Codes<D>& c, int absent, int t0, int hi, int& most) {
+template <int BLOCKS>
+__device__ inline int largest_block(int x) {  // of what is the same in a block's lanes
+  const auto halves = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+  x = max((int)halves[0], (int)halves[1]);
+  if constexpr (BLOCKS == 2) return x;
+  const auto rows = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+  return max((int)rows[0], (int)rows[1]);
+}
+
+template <int BLOCKS>
+__device__ inline Scales scales_of(uint32_t vs, int absent, int t0, int hi, int& most) {
   Scales s;
-  int b0 = c.vs & 255, b1 = c.vs >> 8;
+  int b0 = vs & 255, b1 = vs >> 8;
   bool some = true, nan = false;
   int up = row_largest(max(b0, b1));
-  const bool cut = t0 + 32 > hi || absent, all = !__any(up == kNone) && !cut;  // (the same for the whole wave)
+  const bool cut = t0 + BLOCKS * kBlock > hi || absent, all = !__any(up == kNone) && !cut;  // (the same for the whole wave)
   if (__builtin_expect(!all, 0)) {  // tokens that there are not, or whose V is not a number, are left out: they get the largest of the others
-    const int left = of_half(absent) ? 0 : min(max(hi - (t0 + 16 * (int)(threadIdx.x >> 5 & 1) + 2 * (int)(threadIdx.x & 7)), 0), 2);
+    const int block = lanes_block<BLOCKS>(), left = (absent >> block) & 1 ? 0 : min(max(hi - (t0 + 16 * block + 2 * (int)(threadIdx.x & 7)), 0), 2);
     const bool n0 = left > 0 && b0 == kNone, n1 = left > 1 && b1 == kNone;
     up = row_largest(max(left > 0 && !n0 ? b0 : 0, left > 1 && !n1 ? b1 : 0));
     some = up > 0, nan = n0 || n1;
-    const auto both = __builtin_amdgcn_permlane32_swap((uint32_t)up, (uint32_t)up, false, false);
-    most = max(most, (int)max(both[0], both[1]));
+    most = max(most, largest_block<BLOCKS>(up));
     up = some ? up : most;
     s.vs = (uint32_t)(n0 || left < 1 ? (n0 ? kNone : up) : b0) | (uint32_t)(n1 || left < 2 ? (n1 ? kNone : up) : b1) << 8;
     b0 = left < 1 || n0 ? up : b0, b1 = left < 2 || n1 ? up : b1;
   } else {
-    const auto both = __builtin_amdgcn_permlane32_swap((uint32_t)up, (uint32_t)up, false, false);
-    most = max(most, (int)max(both[0], both[1]));
-    s.vs = c.vs;
+    most = max(most, largest_block<BLOCKS>(up));
+    s.vs = vs;
   }
   s.ev = (float)(up - 127);
   s.low = 0x3c003c00u - ((uint32_t)(up - b0) << 10) - ((uint32_t)(up - b1) << 26);
@@ -183,9 +191,17 @@ __device__ inline Scales scales_of(const Codes<D>& c, int absent, int t0, int hi
   return s;
 }
 
-// N pairs of blocks and G groups of 32 rows: their scores (times f) become the second product's operands.
-template <int D, int G, int N>
-__device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[G][N], Scales (&p)[N], half8 (&w)[G][N][2]) {
+template <int D>
+__device__ inline void times(State<D>& z, float x) {
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int k = 0; k < 16; ++k) z.o[i][k] *= x;
+}
+
+// N pairs (of BLOCKS blocks) and G groups of rows: their scores (times f) become the second product's operands.
+template <int BLOCKS, class Z, int G, int N>
+__device__ inline void soften(Z (&z)[G], float16v (&s)[G][N], float (&f)[G][N], Scales (&p)[N], half8 (&w)[G][N][2]) {
   bool rare = false;
 #pragma unroll
   for (int n = 0; n < N; ++n) rare |= p[n].rare;
@@ -234,6 +250,10 @@ __device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[
       m[g] = fmaxf(m[g], fmaf(most, f[g][n], p[n].ev));
     }
     m[g] = fmaxf(m[g], other_half(m[g]));
+    if constexpr (BLOCKS == 4) {
+      const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(m[g]), __float_as_uint(m[g]), false, false);
+      m[g] = fmaxf(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+    }
     ahead |= m[g] > z[g].m + (kSlack + kLift);
   }
   if (__builtin_expect(__any(ahead), 0)) {
@@ -243,11 +263,7 @@ __device__ inline void soften(State<D> (&z)[G], float16v (&s)[G][N], float (&f)[
       const bool fresh = z[g].m == -FLT_MAX;  // (nothing so far)
       z[g].m = to;
       z[g].l = z[g].l * h * h;
-      if (__all(fresh)) continue;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) z[g].o[i][k] *= alpha;
+      if (!__all(fresh)) times(z[g], alpha);
     }
   }
   if (__builtin_expect(rare, 0)) {
@@ -377,7 +393,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
   Marks m[N];
   Scales p[N];
 #pragma unroll
-  for (int n = 0; n < N; ++n) m[n] = marks[n], p[n] = scales_of<D>(c[n], absent[n], t0[n], u.hi, most);
+  for (int n = 0; n < N; ++n) m[n] = marks[n], p[n] = scales_of<2>(c[n].vs, absent[n], t0[n], u.hi, most);
   ahead();
 #pragma unroll
   for (int g = 0; g < G; ++g)
@@ -390,7 +406,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
         finish_scores<KIND>(a, u.prefix, u.hi, t0[n], pair, Unmarked{}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
     }
   half8 w[G][N][2];
-  k4::soften<D, G, N>(z, s, f, p, w);
+  k4::soften<2>(z, s, f, p, w);
   __builtin_amdgcn_s_setprio(1);
   __builtin_amdgcn_sched_barrier(0);  // (V's codes are turned as they are needed: all at once they take 64 registers more)
 #pragma unroll
@@ -578,6 +594,12 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
 template <int D, int KIND>
 constexpr bool kApart = D == 128 && KIND != kPlain;
 
+}  // namespace k4
+
+#include "k4_few.hpp"
+
+namespace k4 {
+
 template <int D, bool F16, bool MANY, int KIND>
 __global__ __launch_bounds__(256, 2) void k4_attend(AttendArgs a) {
   __shared__ __attribute__((aligned(16))) float lds[4 * kRows * kPitch<D> + 4 * kRows * 2];
@@ -585,6 +607,7 @@ __global__ __launch_bounds__(256, 2) void k4_attend(AttendArgs a) {
   Unit u = a.units[unit];
   // the lane's block, asked for together with the unit: pairs are dealt out to the four waves
   const int listed = a.unit_blocks[unit * kUnitBlocks + min(2 * (wave + 4 * (lane >> 1)) + (lane & 1), kUnitBlocks - 1)];
+  const int few = MANY ? 0 : a.unit_blocks[unit * kUnitBlocks + min(4 * (wave + 4 * (lane >> 2)) + (lane & 3), kUnitBlocks - 1)];  // (fours, in attend_few)
   asm volatile("" ::"s"(u.request), "s"(u.s0), "s"(u.pos0), "s"(u.lo), "s"(u.hi), "s"(u.prefix), "s"(u.part));  // (one load, ahead of the branch)
   if constexpr (MANY && kApart<D, KIND>) {
     const int first = blockIdx.y * kRows;
@@ -597,6 +620,8 @@ __global__ __launch_bounds__(256, 2) void k4_attend(AttendArgs a) {
       k4::attend_unit<D, F16, KIND, 2>(a, u, listed, head, lds);
     else
       k4::attend_unit<D, F16, KIND, 1>(a, u, listed, head, lds);
+  } else if (!MANY && u.n_rows <= kFewRows) {
+    k4::attend_few<D, F16, KIND>(a, u, few, head, lds);
   } else {
     k4::attend_unit<D, F16, KIND, 1>(a, u, listed, head, lds);
   }

@@ -230,6 +230,12 @@ __device__ inline Pair pair_of(const Blocks& b, int k) {  // blocks 2k and 2k + 
 
 __device__ inline bool of_half(int bits) { return (bits >> ((threadIdx.x >> 5) & 1)) & 1; }
 
+// Which of BLOCKS blocks side by side the lane holds scores of: two, a half of the wave each, or four.
+template <int BLOCKS>
+__device__ inline int lanes_block() {
+  return BLOCKS == 2 ? (threadIdx.x >> 5) & 1 : (threadIdx.x >> 4) & 3;
+}
+
 // The codes of a pair, as this lane's pieces.  Row m = 8a + 4h + b of the first product is token 4a + b of block h.
 __device__ inline const uint8_t* k_piece(const AttendArgs& a, int at0, int at1, int D) {
   const int lane = threadIdx.x & 63, m = lane & 31, half = lane >> 5;
@@ -314,14 +320,15 @@ __device__ inline float shown(float s, int seen) {  // where seen is -1, else -i
   return __uint_as_float((__float_as_uint(s) & seen) | (0xff800000u & ~seen));
 }
 
-// Scores of a pair, tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
+// Scores of a pair (of BLOCKS blocks), tokens t0 .. t0 + 31: capped, lowered, hidden.  They come as the first product gives them (times f: log2 units) and are
 // left so where nothing has to be done; else they come out in log2 units and f is 1.
-template <int KIND, class Source>
+template <int KIND, int BLOCKS = 2, class Source>
 __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, const Pair& p, const Source& source, float slope, int token,
                                      int first_token, float& f, float16v& s) {
-  const int half = (threadIdx.x >> 5) & 1, base = t0 + 16 * half;
-  const bool ordered = t0 + 31 > first_token, cut = t0 + 32 > hi || p.absent;
-  const bool masked = cut || (t0 + 32 > prefix && ((KIND == kMarked && a.tagged) || ordered));
+  constexpr int kTokens = BLOCKS * kBlock;
+  const int block = lanes_block<BLOCKS>(), base = t0 + 16 * block;
+  const bool ordered = t0 + kTokens - 1 > first_token, cut = t0 + kTokens > hi || p.absent;
+  const bool masked = cut || (t0 + kTokens > prefix && ((KIND == kMarked && a.tagged) || ordered));
   const bool shaped = KIND != kPlain && (a.cap_log2 > 0.f || a.lowered);
   if (KIND == kPlain ? __builtin_expect(!masked, 1) : !masked && !shaped) return;
   if (KIND != kPlain && a.cap_log2 > 0.f) {
@@ -383,7 +390,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     bits &= tagged;
   }
   bits |= below(prefix - base);
-  bits = of_half(p.absent) ? 0u : bits & below(hi - base);
+  bits = (p.absent >> block) & 1 ? 0u : bits & below(hi - base);
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = shown(s[i], __builtin_amdgcn_sbfe((int)bits, i, 1));
 }
