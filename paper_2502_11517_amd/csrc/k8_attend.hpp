@@ -326,8 +326,8 @@ template <int KIND, int BLOCKS = 2, class Source>
 __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, int t0, const Pair& p, const Source& source, float slope, int token,
                                      int first_token, float& f, float16v& s) {
   constexpr int kTokens = BLOCKS * kBlock;
-  const int block = lanes_block<BLOCKS>(), base = t0 + 16 * block;
-  const bool ordered = t0 + kTokens - 1 > first_token, cut = t0 + kTokens > hi || p.absent;
+  const int half = (threadIdx.x >> 5) & 1, block = BLOCKS == 2 ? half : lanes_block<BLOCKS>(), base = t0 + 16 * block;
+  const bool ordered = t0 + (kTokens - 1) > first_token, cut = t0 + kTokens > hi || p.absent;
   const bool masked = cut || (t0 + kTokens > prefix && ((KIND == kMarked && a.tagged) || ordered));
   const bool shaped = KIND != kPlain && (a.cap_log2 > 0.f || a.lowered);
   if (KIND == kPlain ? __builtin_expect(!masked, 1) : !masked && !shaped) return;
@@ -390,7 +390,7 @@ __device__ inline void finish_scores(const AttendArgs& a, int prefix, int hi, in
     bits &= tagged;
   }
   bits |= below(prefix - base);
-  bits = (p.absent >> block) & 1 ? 0u : bits & below(hi - base);
+  bits = (BLOCKS == 2 ? of_half(p.absent) : p.absent >> block & 1) ? 0u : bits & below(hi - base);
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = shown(s[i], __builtin_amdgcn_sbfe((int)bits, i, 1));
 }
