@@ -18,7 +18,17 @@
 //
 // Products are transposed, S^T = K Q^T and O^T = V^T P^T, in 32x32x16 steps over 32 tokens x 32 stacked rows.  A lane's piece of K is 16 bytes, the 32 dims of
 // one token under one scale; its piece of V 16 bytes, two neighbouring dims of a block's 16 tokens, which go to two products' rows: the dims of a product are
-// every second of 64.  The scores that a lane gets (16 tokens of one block, one row) are its operand of the second product, as in the 8-bit cache.
+// every second of 64.  The scores that a lane gets (16 tokens of one block, one row) are its operand of the second product, as in the 8-bit cache.  Units with at
+// most 16 rows go in steps of another shape (k4_few.hpp).
+//
+// What bounds it (8 kv heads of 128; a layer):
+//   8 streams over 8k tokens, 11 MB        9.5 us: the ramp, as in the 8-bit cache (11.1): a work-group has 1.3 steps' worth to each wave; 2.5 of launch
+//   16 ragged requests, capped, 50 MB      21.1 us: vector instructions, 23 a score, half of the time; ramp and end 4
+//   2048 x 4 rows over 8k tokens, 309 GF   325 to 365 us by the card, 850 to 950 TFLOP/s against 1190 of a large library product: vector instructions busy 68% of the
+//                                          time, matrix instructions 42%
+// Tried and not taken: the scaled matrix instruction on the codes themselves with q split into e4m3 parts (its sums are off by 1.5e-4 of their terms' magnitudes,
+// a hundred times as much as a sum in fp32), eight waves to a work-group (8 streams over 8k 109 -> 110 us a pass, the prompt 389 -> 415), the first blocks in scalar
+// registers (no change), Q's rows loaded whole and turned in LDS (the prompt 333 -> 338).
 #pragma once
 #include "k4_dev.hpp"
 #include "k8_attend.hpp"

