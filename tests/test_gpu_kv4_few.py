@@ -119,3 +119,62 @@ def test_units_longer_than_a_waves_list_of_blocks(dtype, D):
         bound = torch.finfo(td).eps / 2 * want.abs() + (2.0 ** -11 + 2 * ds[:, None]) * mean + T * 2.0 ** -25 * vv.abs().max() * w.amax(-1, keepdim=True)
         assert ((out[:, head].double() - want).abs() <= bound * (1 + 2.0 ** -6)).all()
         assert ((lse[:, head].double() - want_lse).abs() <= ds + 2.0 ** -20 * want_lse.abs()).all()
+
+
+def test_pages_and_requests_that_are_not_there():
+    c = Case(47, length=[200, 40, 90], rows=[3, 4, 2], pad=4)
+    c.table[0, 2], c.table[0, 3], c.table[0, 9], c.table[1, 2] = -1, 1 << 29, c.pages, -(1 << 31)
+    c.check()
+    c.check(see=c.rng.integers(-2 ** 63, 2 ** 63, c.n), prefix=[50, 0, 90])
+    c.table[1, :] = -1
+    slot = np.zeros(c.n, int)
+    slot[7:9] = -1  # request 2 was refused
+    out, lse = c.check(slot=slot, refused=(2,), see=np.full(c.n, -1))
+    assert (out[3:] == 0).all() and np.isneginf(lse[3:]).all()
+    c.length, c.offs = np.array([1 << 30, -9, 90]), np.array([-5, 4, 2, 1 << 20])
+    c.run()
+
+
+def test_the_same_bits_every_time():
+    for kw in (dict(dtype="bf16", length=[5000], rows=[3]), dict(dtype="f16", D=64, length=[700, 40], rows=[4, 1])):
+        c = Case(48, **kw)
+        a = c.run()
+        for _ in range(3):
+            b = c.run()
+            assert all(np.array_equal(x, y) for x, y in zip(a, b))
+
+
+def test_two_captured_steps_at_a_time():
+    """Each with a handle and a workspace of its own over one cache, replayed side by side on two streams: what they read they share, what they write they do not."""
+    cases = [Case(49, length=[3000], rows=[n]) for n in (4, 20)]
+    a = cases[0]
+    cases[1].c, cases[1].table, cases[1].pages = a.c, a.table, a.pages
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    bufs = [torch.from_numpy(np.ascontiguousarray(b)).to("cuda", torch.uint8).reshape(s) for b, s in zip(a.c.pack(), kv4.cache_shapes(a.config()))]
+    table = i32(a.table)
+    steps = []
+    for c in cases:
+        cfg, stream = c.config(), torch.cuda.Stream()
+        ws = torch.empty(kv4.query_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        q = c.q.cuda()
+        out, lse = torch.zeros_like(q), torch.zeros(c.n, c.Hq, device="cuda")
+        h = kv4.PastaKv4(cfg, ws, page_table=table, k_codes=bufs[0], v_codes=bufs[1], k_scale=bufs[2], v_scale=bufs[3], stream=stream.cuda_stream)
+        length, offs = i32(c.length), i32(c.offs)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            h.plan(length, offs, c.n)
+            for _ in range(4):
+                h.attend(0, q, out, lse=lse)
+        steps.append((c, stream, graph, out, lse, (h, ws, q, length, offs)))
+    want = [c.run() for c in cases]
+    for i in range(5):
+        for c, stream, graph, out, lse, _ in steps:
+            with torch.cuda.stream(stream):
+                out.zero_(), lse.zero_()
+                graph.replay()
+        if i % 2:
+            (torch.ones(100, device="cuda") * i).sum().item()
+        torch.cuda.synchronize()
+        for (c, _, _, out, lse, _), (o, l) in zip(steps, want):
+            assert np.array_equal(out.double().cpu().numpy(), o) and np.array_equal(lse.double().cpu().numpy(), l)

@@ -208,3 +208,53 @@ def test_layers_are_apart():
     c.check()
     got, want = c.read([5, 6, 17, 18, 19], "bf16", layer=2)
     assert same(got[0], want[0]) and same(got[1], want[1])
+
+
+def test_rows_behind_four_gibibytes_of_codes_and_of_rows():
+    H, D, P = 8, 128, 64
+    pages = (5 << 30) // (H * D * P // 2)
+    cfg = kv4.make_config("bf16", H, H, D, 1.0, max_rows=64, page_tokens=P, n_phys_pages=pages)
+    bufs = [torch.zeros(s, dtype=torch.uint8, device="cuda") for s in kv4.cache_shapes(cfg)]
+    h = kv4.PastaKv4(cfg, k_codes=bufs[0], v_codes=bufs[1], k_scale=bufs[2], v_scale=bufs[3], stream=torch.cuda.current_stream().cuda_stream)
+    n, far = 40, 1 << 26  # 40 rows 2^26 values apart
+    slots = [pages * P - 40 + i for i in range(n)]
+    slot = torch.tensor(slots, dtype=torch.int32, device="cuda")
+    apart = torch.empty((n - 1) * far + H * D, dtype=torch.bfloat16, device="cuda").as_strided((n, H, D), (far, D, 1))
+    k, v = rows(40, n, H, D, "bf16"), rows(41, n, H, D, "bf16")
+    apart.copy_(k)
+    h.append(0, slot, apart, v)
+    small = Cache(H, D, P, 1)
+    small.append([P - 40 + i for i in range(n)], k, v)
+    (wk, wv), _ = small.read([P - 40 + i for i in range(n)], "bf16")
+    apart.zero_()
+    got = torch.zeros(n, H, D, dtype=torch.bfloat16, device="cuda")
+    h.read(0, slot, apart, got)
+    torch.cuda.synchronize()
+    assert torch.equal(apart.cpu(), wk) and torch.equal(got.cpu(), wv)
+    assert not bufs[0][0, :-1].any() and not bufs[3][0, :-1].any()
+
+
+def test_captured_and_replayed():
+    c = Cache(3, 64, 16, 4, max_rows=64)
+    k, v, k2, v2 = (rows(i, 21, 3, 64, "bf16") for i in (50, 51, 52, 53))
+    slots = list(range(7, 28))
+    slot = torch.tensor(slots, dtype=torch.int32, device="cuda")
+    ko, vo = torch.zeros(2, 21, 3, 64, device="cuda")
+    stream = torch.cuda.Stream()
+    h = kv4.PastaKv4(c.cfg, k_codes=c.bufs[0], v_codes=c.bufs[1], k_scale=c.bufs[2], v_scale=c.bufs[3], stream=stream.cuda_stream)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        h.append(0, slot, k, v)
+        h.read(0, slot, ko, vo)
+    for i in range(4):
+        if i == 2:
+            k.copy_(k2), v.copy_(v2)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graph.replay()
+        torch.cuda.synchronize()
+        c.want[0].append(slots, k.double().cpu().numpy(), v.double().cpu().numpy())
+        c.check()
+        for got, full in zip((ko, vo), c.want[0].natural()):
+            assert torch.equal(got.double().cpu(), torch.from_numpy(np.ascontiguousarray(full[slots])))

@@ -180,3 +180,18 @@ def test_the_cpu_reference_is_a_rotation():
     x = torch.randn(2, 1, 8)
     y, _ = turned(x, torch.tensor([3, 5]), [1.0, 0.5], 4, "half", 1.0, False)
     assert np.isclose(float(y[0, 0, 0]), float(x[0, 0, 0] * np.cos(3.0) - x[0, 0, 2] * np.sin(3.0)), atol=1e-6)
+
+
+def test_rows_that_lie_far_apart():
+    """Offsets beyond 2^31 values, in place, beside rows that lie side by side."""
+    f, _ = rows.rope_frequencies(64)
+    q, k, position = make(10, 40, 4, 2, 64, "bf16")
+    far = 1 << 26
+    apart = torch.empty(39 * far + 4 * 64, dtype=torch.bfloat16, device="cuda").as_strided((40, 4, 64), (far, 64, 1))
+    apart.copy_(q)
+    h = handle(4, 2, 64, 64, "half", f, max_rows=40)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    h.rotate(position, q, qo, k, ko)
+    h.rotate(position, apart, apart, k, ko)
+    torch.cuda.synchronize()
+    assert torch.equal(apart.cpu(), qo.cpu())
