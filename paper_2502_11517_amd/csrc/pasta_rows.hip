@@ -22,7 +22,7 @@ struct pasta_rows {
   uint64_t magic = kMagic;
   pasta_rows_config cfg{};
   double* sums = nullptr;
-  int2* verdicts = nullptr;
+  int2* outcomes = nullptr;
 };
 
 namespace {
@@ -92,7 +92,7 @@ extern "C" int32_t pasta_rows_create(pasta_rows_config* cfg, pasta_rows** out) {
   pasta_rows* h = new (std::nothrow) pasta_rows();
   if (!h) return PASTA_E_NOMEM;
   h->cfg = *cfg;
-  h->sums = (double*)cfg->workspace, h->verdicts = (int2*)(h->sums + sums_of(*cfg));
+  h->sums = (double*)cfg->workspace, h->outcomes = (int2*)(h->sums + sums_of(*cfg));
   *out = h;
   return PASTA_OK;
 }
@@ -162,7 +162,7 @@ extern "C" int32_t pasta_rows_verify(pasta_rows* h, const pasta_rows_verify_args
   k.n_sequences = a->n_sequences, k.n_rows = a->n_rows, k.vocab = c.vocab;
   k.row_offsets = a->row_offsets, k.token = a->token, k.slot = a->slot, k.target = a->target, k.draft = a->draft, k.draw = a->draw, k.last_draw = a->last_draw;
   k.length = a->length, k.row_position = a->row_position, k.accepted = a->accepted, k.next_token = a->next_token, k.keep = a->keep;
-  k.position_out = a->position_out, k.sums = h->sums, k.verdicts = h->verdicts;
+  k.position_out = a->position_out, k.sums = h->sums, k.outcomes = h->outcomes;
   hipStream_t s = (hipStream_t)c.hip_stream;
   by_type(a->dtype, [&](auto type) {
     if (k.segments) {

@@ -5,7 +5,7 @@
 // ones a launch of as many waves as there are segments, which leave their sums, and one in which a work-group a sequence finds the segment that the draw falls
 // into and reads that once more.
 //
-// One sequence of 32000 tokens takes 7.3 us: positions, drafts and the verdict are reads behind one another, then one CU reads 256 KB.  64 sequences of 131072
+// One sequence of 32000 tokens takes 7.3 us: positions, drafts and what becomes of them are reads behind one another, then one CU reads 256 KB.  64 sequences of 131072
 // tokens, 67 MB, take 11.3 (sums, 5.9 TB/s: what is that small stays in the last-level cache) and 4.4 (the pick, a chain of reads).  Weights kept as fp64 took twice the
 // registers and spilled (11.3 -> 7.6 for the one sequence, with its sums added once and the search by 256 tokens).
 #pragma once
@@ -25,7 +25,7 @@ struct VerifyArgs {
   const int *length, *row_position;
   int *accepted, *next_token, *keep, *position_out;
   double* sums;     // workspace: [sequence][segment]
-  int2* verdicts;   // workspace: [sequence] accepted, rejected
+  int2* outcomes;   // workspace: [sequence] accepted, rejected
 };
 
 
@@ -78,16 +78,16 @@ __device__ inline void four(const void* base, int64_t row, int at, int n, float 
 __device__ inline double weight(float p, float q) { return fmax((double)p - (double)q, 0.0); }
 
 // What becomes of a sequence's drafts; every lane of the wave knows.
-struct Verdict {
+struct Outcome {
   int first, rows, accepted;
   int refused;   // rows of a sequence that has no place for them, whose `rows` are then 0
   int rejected;  // the token that was, -1: none
   __device__ bool left() const { return accepted + 1 < rows; }  // a draft was rejected: what the target has beyond the draft's distribution is left
 };
 
-__device__ inline Verdict rows_of(const VerifyArgs& a, int s) {
+__device__ inline Outcome rows_of(const VerifyArgs& a, int s) {
   const int end = min(max(a.row_offsets[a.n_sequences], 0), a.n_rows);
-  Verdict v;
+  Outcome v;
   v.first = min(max(a.row_offsets[s], 0), end);
   v.rows = min(max(a.row_offsets[s + 1], v.first), end) - v.first;
   v.refused = a.slot && v.rows && a.slot[v.first] < 0 ? v.rows : 0;
@@ -97,9 +97,9 @@ __device__ inline Verdict rows_of(const VerifyArgs& a, int s) {
 }
 
 template <int TYPE>
-__device__ inline Verdict judge(const VerifyArgs& a, int s) {
+__device__ inline Outcome decide(const VerifyArgs& a, int s) {
   const int lane = threadIdx.x & 63;
-  Verdict v = rows_of(a, s);
+  Outcome v = rows_of(a, s);
   for (int i0 = 1; i0 < v.rows; i0 += 64) {
     const int i = i0 + lane, row = v.first + min(i, v.rows - 1);
     const int t = a.token[row];
@@ -123,7 +123,7 @@ template <int TYPE, int LOADS>
 struct Segment {
   float p[LOADS][4], q[LOADS][4];  // q: 0 where the target alone counts, +inf where nothing is to count
 
-  __device__ void load(const VerifyArgs& a, const Verdict& v, int from) {
+  __device__ void load(const VerifyArgs& a, const Outcome& v, int from) {
     const int lane = threadIdx.x & 63;
     const int64_t row = v.first + v.accepted;
 #pragma unroll
@@ -218,7 +218,7 @@ struct Segment {
 };
 
 // Everything but next_token; the threads of a work-group.
-__device__ inline void put_down(const VerifyArgs& a, int s, const Verdict& v) {
+__device__ inline void put_down(const VerifyArgs& a, int s, const Outcome& v) {
   if (threadIdx.x == 0) {
     a.accepted[s] = v.accepted;
     if (a.keep) a.keep[s] = v.rows ? max(a.length[s] - v.rows + 1 + v.accepted, 0) : a.length[s];
@@ -238,7 +238,7 @@ template <int TYPE, int LOADS>
 __global__ __launch_bounds__(1024) void rows_verify_whole(VerifyArgs a) {
   __shared__ double s_sum[2][16];
   const int s = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), from = wave * LOADS * 256;
-  const Verdict v = judge<TYPE>(a, s);
+  const Outcome v = decide<TYPE>(a, s);
   if (v.rows == 0) return put_down(a, s, v);
   Segment<TYPE, LOADS> g;
   g.load(a, v, from);
@@ -269,13 +269,13 @@ __global__ __launch_bounds__(1024) void rows_verify_whole(VerifyArgs a) {
   }
 }
 
-// Sums of the segments; four of a sequence to a work-group.  What is judged goes to the next launch.
+// Sums of the segments; four of a sequence to a work-group.  What becomes of the drafts goes to the next launch.
 template <int TYPE>
 __global__ __launch_bounds__(256) void rows_verify_sums(VerifyArgs a) {
   const int s = blockIdx.y, segment = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (segment >= a.segments) return;
-  const Verdict v = judge<TYPE>(a, s);
-  if (segment == 0 && (threadIdx.x & 63) == 0) a.verdicts[s] = int2{v.accepted, v.rejected};
+  const Outcome v = decide<TYPE>(a, s);
+  if (segment == 0 && (threadIdx.x & 63) == 0) a.outcomes[s] = int2{v.accepted, v.rejected};
   if (v.rows == 0) return;
   Segment<TYPE, kSegment / 256> g;
   g.load(a, v, segment * kSegment);
@@ -292,8 +292,8 @@ __global__ __launch_bounds__(256) void rows_verify_pick(VerifyArgs a) {
   double* sums = a.sums + (int64_t)s * a.segments;
   const int each = (a.segments + 255) / 256, from = min((int)threadIdx.x * each, a.segments), to = min(from + each, a.segments);  // this thread's
   const double first = from < to ? sums[from] : 0.0;  // (asked for at once; of a sequence without rows it is nothing)
-  const int2 known = a.verdicts[s];
-  Verdict v = rows_of(a, s);
+  const int2 known = a.outcomes[s];
+  Outcome v = rows_of(a, s);
   v.accepted = known.x, v.rejected = known.y;
   put_down(a, s, v);
   if (v.rows == 0) return;
