@@ -74,6 +74,7 @@ Bounds bounds(const Config& c, int64_t n_rows, int64_t n_requests, bool wide, bo
 // What a plan keeps in the workspace.
 struct PlanSpace {
   int least_alone = kLeastAlone;  // (of the cache: the least length of pieces where a CU has one)
+  int few_rows = 0;               // (of the cache: rows of a tile that costs less, k8_plan.hpp)
   int* tiles_upto = nullptr;
   Unit* units = nullptr;
   int* unit_blocks = nullptr;
@@ -116,7 +117,7 @@ bool launch_plan(const Config& c, const Geometry& g, const PlanSpace& space, con
   plan.whole = (int64_t)c.pages_per_request * c.page_tokens <= (plan.wide ? kWholeWide : kWholeTokens);
   plan.most = bounds(c, a.n_rows, a.n_requests, plan.wide, plan.whole, space.least_alone);
   PlanArgs k{};
-  k.g = g, k.n_requests = a.n_requests, k.n_rows = a.n_rows, k.wide = plan.wide, k.whole = plan.whole, k.capacity = (int)plan.most.capacity, k.least_alone = space.least_alone;
+  k.g = g, k.n_requests = a.n_requests, k.n_rows = a.n_rows, k.wide = plan.wide, k.whole = plan.whole, k.capacity = (int)plan.most.capacity, k.least_alone = space.least_alone, k.few_rows = space.few_rows;
   k.max_units = (int)plan.most.units, k.max_tiles = (int)plan.most.tiles, k.max_part_rows = (int)plan.most.part_rows;
   k.length = a.n_requests ? a.length : a.row_offsets;  // (read, not used, without a request)
   k.row_offsets = a.row_offsets, k.prefix_len = a.prefix_len, k.slot = a.slot;

@@ -24,7 +24,7 @@ struct pasta_kv4 {
   uint64_t magic = kMagic;
   pasta_kv4_config cfg{};
   k8::Geometry g{};
-  k8::PlanSpace space{k8::kLeastAlone4};
+  k8::PlanSpace space{k8::kLeastAlone4, k4::kFewRows};
   k8::Planned plan;  // the last one
 };
 

@@ -71,3 +71,16 @@ def test_positions_in_order_and_out_of_it(dtype, D, Hq, Hkv, n, cap):
     row[0], row[1] = 2000, 40 + 15
     c.check(slopes=c.rng.uniform(-0.002, 0.02, Hq).astype(np.float32), row_position=row, cap=cap)
     c.check(slopes=np.full(Hq, 0.01, np.float32), row_position=np.full(n, 3000), cap=cap)
+
+
+@pytest.mark.parametrize("R", [2, 3, 5, 16, 40, 100, 200])
+@pytest.mark.parametrize("Hkv", [1, 8])
+def test_requests_with_few_rows_beside_others_with_many(R, Hkv):
+    """Their units weigh differently; none is lost whatever the weights make of the split."""
+    rng = np.random.default_rng([R, Hkv, 50])
+    length = rng.integers(1, 400 if R > 16 else 1500 if Hkv > 1 else 6000, R)
+    rows = np.minimum(length, rng.integers(0, 9, R))
+    rows[0], rows[1] = min(length[0], 1), min(length[1], 8)
+    c = Case([R, Hkv, 51], "bf16", 4 * Hkv, Hkv, 64, 16, length, rows, width=400)
+    c.check(prefix=np.where(rng.random(R) < 0.5, length // 2, 0))
+    c.check(see=rng.integers(-2 ** 63, 2 ** 63, c.n), prefix=length // 3)
