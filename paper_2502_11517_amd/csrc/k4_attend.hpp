@@ -23,7 +23,8 @@
 //
 // What bounds it (8 kv heads of 128; a layer):
 //   8 streams over 8k tokens, 11 MB        9.5 us: the ramp, as in the 8-bit cache (11.1): a work-group has 1.3 steps' worth to each wave; 2.5 of launch
-//   16 ragged requests, capped, 50 MB      21.1 us: vector instructions, 23 a score, half of the time; ramp and end 4
+//   16 ragged requests, capped, 50 MB      20.3 us: units with more than 16 rows, 15 of these us and more in a wave's chain from step to step, ramp and end 4; vector
+//                                          instructions, 23 a score, are busy half of the time, and ten percent fewer (the cap by a series) changed nothing
 //   2048 x 4 rows over 8k tokens, 309 GF   325 to 365 us by the card, 850 to 950 TFLOP/s against 1190 of a large library product: vector instructions busy 68% of the
 //                                          time, matrix instructions 42%
 // Tried and not taken: the scaled matrix instruction on the codes themselves with q split into e4m3 parts (its sums are off by 1.5e-4 of their terms' magnitudes,
