@@ -105,6 +105,8 @@ int32_t pasta_kv8_destroy(pasta_kv8 *h);
  *   A request is REFUSED, and nothing of it changes, if it would outgrow its row of
  *   the page table, or if it needs pages and the needs of the requests up to and
  *   including it (those that would outgrow their table not counted) exceed the stack.
+ *   (What it was not to keep stays, too: a call without rows ahead, which refuses nobody,
+ *   takes it back in any case.)
  *
  * Writes page_table (entries of taken pages; an entry past a request's pages keeps
  * its old value), free_pages, length_out[r] (kept + n; of a refused request,

@@ -7,9 +7,11 @@
  * by position ids that need not be consecutive.  And pasta_kv8_slots takes drafts back
  * by keep[]: pasta_rows_verify writes it.  So a captured step
  *
- *   slots (keep) -> plan -> per layer: rotate, append, attend -> verify
+ *   slots (keep, no rows) -> slots -> plan -> per layer: rotate, append, attend -> verify
  *
- * goes on by as many tokens as were accepted, without the host.
+ * goes on by as many tokens as were accepted, without the host.  Drafts are taken back by
+ * a call of their own, ahead of the one that places the step's rows: a request that this one
+ * refuses stays as it is, so that with keep[] its rejected drafts would stay in the cache.
  *
  * Conventions are those of pasta_kv8.h: status codes, nothing throws or aborts, DEVICE
  * pointers are the caller's, all work is enqueued on the handle's stream, whose device
@@ -104,8 +106,8 @@ int32_t pasta_rows_rotate(pasta_rows *h, const pasta_rows_rotate_args *a);
  *   the next step.  It may be row_position.
  *
  * slot (optional): the rows' places, as pasta_kv8_slots gave them.  A sequence whose first
- * row has none was refused: a is 0, next_token -1, keep[s] = length[s], and its
- * positions stay.
+ * row has none was refused: a is 0, next_token -1, keep[s] = length[s] (what of it was to be
+ * taken back has been, ahead of the step), and its positions stay.
  *
  * Rows behind row_offsets[n_sequences] are left alone.  Strides are at least vocab, in values.
  * Needs the workspace.  Errors: E_INVAL, E_CAPACITY, E_DEVICE, E_STATE.          */

@@ -75,7 +75,7 @@ class Session:
         if vocab:
             # how much of every request the next step keeps: its length, but for what verify() writes.  (Replays write it unseen by the host, so every step
             # goes by it, and leaves it as one that is not verified would.)
-            self.keep = torch.zeros(max_requests, **i32)
+            self.keep, self._no_rows = torch.zeros(max_requests, **i32), torch.zeros(max_requests + 1, **i32)
             self.accepted, self.next_token = torch.zeros(max_requests, **i32), torch.full((max_requests,), -1, **i32)
         self.page_table = torch.full((max_requests, pages_per_request), -1, **i32)
         self.free_pages = torch.arange(n_phys_pages - 1, -1, -1, **i32)
@@ -186,10 +186,10 @@ class Session:
         self._on_stream(give_back)
 
     def _take_back(self):
-        """Drafts that were not accepted, ahead of the next step."""
+        """Drafts that were not accepted, ahead of the next step.  In a call of its own: of a request that slots refuses nothing changes, its rejected drafts
+        would stay, and what it keeps would become all of them."""
         def take():
-            self.handle.slots(self.length, torch.zeros(len(self.requests) + 1, dtype=torch.int32, device=self.device), 0, None, self.length,
-                              self.free_count, self.free_count, keep=self.keep)
+            self.handle.slots(self.length, self._no_rows, 0, None, self.length, self.free_count, self.free_count, keep=self.keep)
             self._keep_all()
         if self.keep is not None:
             self._on_stream(take)
@@ -241,12 +241,11 @@ class Session:
                 c["verified"] = False  # (its threads go on elsewhere, and know their positions from there)
         if torch.cuda.is_current_stream_capturing():
             self._captured.append(step)
-        drafts = {}
         if self.keep is not None:
-            drafts = dict(keep=self.keep)
+            self.handle.slots(self.length, self._no_rows, 0, None, self.length, self.free_count, self.free_count, keep=self.keep)  # (_take_back)
             step["next"] = torch.add(step["position"], step["stride"], out=step.get("next"))
         self.handle.slots(self.length, step["offsets"], step["n"], self.slot, self.length, self.free_count, self.free_count, row_tag=step["tag"],
-                          row_position=step["position"], **drafts)
+                          row_position=step["position"])
         self._keep_all()
         (self.cache or self.handle).plan(self.length, step["offsets"], step["n"], max_request_rows=step["most"], prefix_len=self.prefix_len, slot=self.slot)
         self._step = step
