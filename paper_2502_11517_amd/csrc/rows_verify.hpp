@@ -139,7 +139,7 @@ struct Segment {
     }
   }
 
-  // Infinite weights count as 0: they are taken out here, and the sums need not look for them.
+  // Infinite weights count as 0: they are taken out here, and the sums need not look for them.  (p - q is that of an infinite p whatever a finite q, one below 0, too.)
   __device__ void hold() {
     float most = 0.f, least = 0.f;
 #pragma unroll
@@ -150,7 +150,7 @@ struct Segment {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[j][i] = p[j][i] == __builtin_inff() ? 0.f : p[j][i], q[j][i] = q[j][i] == -__builtin_inff() ? __builtin_inff() : q[j][i];
+      for (int i = 0; i < 4; ++i) p[j][i] = p[j][i] == __builtin_inff() ? -__builtin_inff() : p[j][i], q[j][i] = q[j][i] == -__builtin_inff() ? __builtin_inff() : q[j][i];
   }
 
   __device__ void target_alone() {

@@ -209,6 +209,23 @@ def test_infinite_weights_beside_finite_ones(V):
     assert (c.check()[0] == 0).all()
 
 
+@pytest.mark.parametrize("drafted", [True, False])
+@pytest.mark.parametrize("V", [300, 20000, 40000])
+def test_infinite_weights_where_the_draft_is_below_zero(V, drafted):
+    """An infinite p less a negative q is infinite, too, and does not count, whatever the q."""
+    c = Case(28, V, [2] * 8, drafted=drafted)
+    t = c.token[1::2].long()
+    c.target[:] = 0.0
+    c.target[::2, 11] = 0.25
+    c.target[::2, 7], c.target[::2, V - 1] = float("inf"), float("inf")
+    c.token[1::2] = torch.where((t == 7) | (t == 11) | (t == V - 1), 8, t).int()  # (rejected: p is 0 there)
+    if drafted:
+        c.draft[:] = 0.0
+        c.draft[1::2, 7], c.draft[1::2, V - 1] = -1000.0, -3.0e38
+    got = c.check()
+    assert (got[0] == 0).all() and (got[1] == 11).all()
+
+
 @pytest.mark.parametrize("V", [300, 40000])
 def test_draws_outside_of_their_range(V):
     c = Case(19, V, [1] * 6 + [2] * 3)
