@@ -79,8 +79,10 @@ int32_t pasta_kv4_destroy(pasta_kv4 *h);
 /* New rows of one layer into the cache: k_new, v_new [n_rows][Hkv][D], row i at
  * i * k_stride, i * v_stride values (0: rows side by side).  A row goes to slot[i];
  * rows whose slot is not in [0, n_phys_pages * page_tokens) are skipped.  Rows of one
- * block have to be neighbours with ascending slots, as pasta_kv8_slots gives them out,
- * and no slot may stand in a call twice.  What no row is written to keeps its bytes.
+ * block have to be neighbours (no skipped row between them, either) with ascending slots,
+ * which may leave some out (those of pasta_kv8_slots do not), and no slot may stand in a
+ * call twice: bytes that two tokens share are put back by who writes one of them.  What no
+ * row is written to keeps its bytes.
  *
  * Per row, kv head and, of K, 32 dims: e = the least whole number with
  * max|x| <= 7 * 2^e, held within [-100, 119]; code = the nearest to x * 2^-e, ties to the

@@ -1,6 +1,6 @@
 // New rows of one layer into the 4-bit cache, and rows back out of it.
 //
-// A wave takes a run, at most 16 neighbouring rows that lie in neighbouring slots of one block, of one kv head, K or V.  A row's scales depend on that row
+// A wave takes a run, at most 16 neighbouring rows that lie in one block, ascending, of one kv head, K or V.  A row's scales depend on that row
 // alone, so nothing that was written before is rounded again.
 //   K  a lane has 8 dims of a token, four neighbouring ones those under one scale
 //   V  a lane has D / 64 neighbouring dims of all 16 tokens, whose codes lie together; a token's magnitudes are compared across the wave.  Codes of two
@@ -26,26 +26,47 @@ struct RowArgs {
   uint8_t *k, *v, *ks, *vs;
 };
 
-// f(first row, rows, token of the first, block) for every run that begins within the work-group's rows.
-template <class F>
+// Neighbouring rows that lie in one block, ascending.
+struct Run {
+  int row, n;       // the first, how many
+  int offset;       // token of the first
+  uint32_t tokens;  // theirs, a bit each
+  int64_t block;
+  int mine, lane;   // slots of the rows, from this lane on
+  __device__ bool gaps() const { return (tokens >> offset) + 1 != 1u << n; }
+  __device__ int token(int i) const { return gaps() ? __builtin_amdgcn_ds_bpermute(4 * (lane + min(i, n - 1)), mine) & 15 : offset + i; }  // of row i < n; for all lanes
+  __device__ int rank(int t) const { return min(__builtin_popcount(tokens & ((1u << t) - 1u)), n - 1); }  // of token t's row; without one, of a near one's
+};
+
+// f(run) for every run that begins within the work-group's rows.  With GAPS it may leave slots out: what a wave puts back of a block's V codes has to be
+// nobody else's to write.  Without, its slots are neighbours.
+template <bool GAPS, class F>
 __device__ inline void each_run(const RowArgs& a, int head, F f) {
   const int lane = threadIdx.x & 63, n_slots = a.g.n_pages << a.g.page_shift;
   const int first = blockIdx.x * a.group, last = min(first + a.group, a.n_rows);
-  // lane k: the slot of row first + k - 1; a run that begins within the group ends within 16 more rows
+  // lane k: the slot of row first + k - 1, and of the row ahead of it (read again, which is sooner than from lane to lane: a step's sixteen calls 49.9 / 50.7 us);
+  // a run that begins within the group ends within 16 more rows
   const int row = first + lane - 1;
-  const int mine = lane <= a.group + kBlock && row >= 0 && row < a.n_rows ? a.slot[row] : -1;
+  const bool there = lane <= a.group + kBlock && row < a.n_rows;
+  const int mine = there && row >= 0 ? a.slot[row] : -1, ahead = there && row > 0 ? a.slot[row - 1] : -1;
+  const bool goes_on = ahead >= 0 && mine < n_slots && (GAPS ? mine > ahead : mine == ahead + 1) && (mine >> 4) == (ahead >> 4);
+  const uint64_t joined = __ballot(goes_on);
   int i = first;
   while (i < last) {
-    const int at = i - first + 1, prev = __builtin_amdgcn_readlane(mine, at - 1), slot = __builtin_amdgcn_readlane(mine, at);
+    const int at = i - first + 1, slot = __builtin_amdgcn_readlane(mine, at);
     if (slot < 0 || slot >= n_slots) {
       ++i;
       continue;
     }
-    const bool goes_on = lane >= at && mine == slot + lane - at && (mine >> 4) == (slot >> 4);
-    const int n = __builtin_ctzll(~(__ballot(goes_on) >> at));
-    if (!(prev >= 0 && slot == prev + 1 && (slot & 15))) {  // the run begins here
+    const int n = 1 + __builtin_ctzll(~(joined >> (at + 1)));
+    if (!(joined >> at & 1)) {  // the run begins here
       const int page = slot >> a.g.page_shift, b = (slot & (a.g.page_tokens - 1)) >> 4;
-      f(i, n, slot & 15, ((int64_t)page * a.g.Hkv + head) * a.g.blocks_per_page + b);
+      uint32_t tokens = ((1u << n) - 1u) << (slot & 15);
+      if (GAPS && __builtin_amdgcn_readlane(mine, at + n - 1) != slot + n - 1) {
+        tokens = 0;
+        for (int k = 0; k < n; ++k) tokens |= 1u << (__builtin_amdgcn_readlane(mine, at + k) & 15);
+      }
+      f(Run{i, n, slot & 15, tokens, ((int64_t)page * a.g.Hkv + head) * a.g.blocks_per_page + b, mine, at});
     }
     i += n;
   }
@@ -62,9 +83,10 @@ struct KLane {
 };
 
 template <int D, int IN>
-__device__ inline void append_k(const RowArgs& a, int row, int n, int offset, int head, int64_t block) {
+__device__ inline void append_k(const RowArgs& a, const Run& run, int head) {
   using L = KLane<D>;
   const L l;
+  const int row = run.row, n = run.n;
   float x[L::kTurns][8];
   // Places without a row get the nearest one's and are dropped below: loads under branches wait for one another.
 #pragma unroll
@@ -80,45 +102,51 @@ __device__ inline void append_k(const RowArgs& a, int row, int n, int offset, in
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[j][k] = byte == kNone ? 0.f : x[j][k] * inverse;
     const uint32_t w = encode8(x[j]);
+    const int t = run.token(i);
     if (i >= n) continue;
-    *(uint32_t*)(a.k + l.codes(block, offset + i)) = w;
-    if (l.dim % kGroup == 0) a.ks[l.scale(block, offset + i)] = (uint8_t)byte;
+    *(uint32_t*)(a.k + l.codes(run.block, t)) = w;
+    if (l.dim % kGroup == 0) a.ks[l.scale(run.block, t)] = (uint8_t)byte;
   }
 }
 
-// Bytes 0 .. 7 of a dim's codes, whose tokens lie in [from, from + n): 255 in each half of them.
-__device__ inline uint2v tokens_mask(int from, int n) {
-  const uint64_t all = ~0ull;
-  const uint64_t m = (all >> (64 - 4 * n)) << (4 * from);  // 1 <= n, from + n <= 16
+// 15 in the half byte of every token in `tokens`, of a dim's bytes 0 .. 7.
+__device__ inline uint2v tokens_mask(uint32_t tokens) {
+  uint64_t m = tokens & 0xffffu;
+  m = (m | m << 24) & 0x000000ff000000ffull;
+  m = (m | m << 12) & 0x000f000f000f000full;
+  m = (m | m << 6) & 0x0303030303030303ull;
+  m = (m | m << 3) & 0x1111111111111111ull;
+  m *= 15;
   return uint2v{(uint32_t)m, (uint32_t)(m >> 32)};
 }
 
 template <int D, int IN>
-__device__ inline void append_v(const RowArgs& a, int row, int n, int offset, int head, int64_t block) {
+__device__ inline void append_v(const RowArgs& a, const Run& run, int head) {
   constexpr int N = D / 64;
   const int lane = threadIdx.x & 63;
+  const int64_t block = run.block;
   uint2v* codes = (uint2v*)(a.v + block * kCodeBytes(D)) + lane * N;
   float x[kBlock][N];
   // Places without a row get the nearest one's and are dropped below: loads under branches wait for one another.
 #pragma unroll
-  for (int t = 0; t < kBlock; ++t) load_row<IN, N>(a.v_new, (int64_t)(row + min(max(t - offset, 0), n - 1)) * a.v_stride + head * D + lane * N, x[t]);
+  for (int t = 0; t < kBlock; ++t) load_row<IN, N>(a.v_new, (int64_t)(run.row + run.rank(t)) * a.v_stride + head * D + lane * N, x[t]);
   uint2v old[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) old[j] = uint2v{0, 0};
-  if (n < kBlock)
+  if (run.n < kBlock)
 #pragma unroll
     for (int j = 0; j < N; ++j) old[j] = codes[j];
   int byte = 0;  // lane t: of token t
 #pragma unroll
   for (int t = 0; t < kBlock; ++t) {
-    if (t < offset || t >= offset + n) continue;  // (the same for the whole wave)
+    if (!(run.tokens >> t & 1)) continue;  // (the same for the whole wave)
     const int b = scale_byte(wave_max(magnitude(x[t], 0)));
     const float inverse = inverse_scale(b);
 #pragma unroll
     for (int j = 0; j < N; ++j) x[t][j] = b == kNone ? 0.f : x[t][j] * inverse;
     byte = lane == t ? b : byte;
   }
-  const uint2v mine = tokens_mask(offset, n);
+  const uint2v mine = tokens_mask(run.tokens);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     uint2v w;
@@ -131,18 +159,18 @@ __device__ inline void append_v(const RowArgs& a, int row, int n, int offset, in
     }
     codes[j] = w;
   }
-  if (lane >= offset && lane < offset + n) a.vs[block * kBlock + lane] = (uint8_t)byte;
+  if (lane < kBlock && (run.tokens >> lane & 1)) a.vs[block * kBlock + lane] = (uint8_t)byte;
 }
 
 template <int D, int IN>
 __global__ __launch_bounds__(256) void k4_append(RowArgs a) {
   const int task = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = task >> 1;
   if (head >= a.g.Hkv) return;
-  each_run(a, head, [&](int row, int n, int offset, int64_t block) {
+  each_run<true>(a, head, [&](const Run& run) {
     if (task & 1)
-      append_v<D, IN>(a, row, n, offset, head, block);
+      append_v<D, IN>(a, run, head);
     else
-      append_k<D, IN>(a, row, n, offset, head, block);
+      append_k<D, IN>(a, run, head);
   });
 }
 
@@ -267,11 +295,11 @@ __global__ __launch_bounds__(256) void k4_read(RowArgs a) {
   const bool both = a.k_out && a.v_out;
   const int task = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = both ? task >> 1 : task;
   if (head >= a.g.Hkv) return;
-  each_run(a, head, [&](int row, int n, int offset, int64_t block) {
+  each_run<false>(a, head, [&](const Run& run) {
     if (both ? task & 1 : !a.k_out)
-      read_v<D, OUT>(a, row, n, offset, head, block, lds);
+      read_v<D, OUT>(a, run.row, run.n, run.offset, head, run.block, lds);
     else
-      read_k<D, OUT>(a, row, n, offset, head, block, lds);
+      read_k<D, OUT>(a, run.row, run.n, run.offset, head, run.block, lds);
   });
 }
 
