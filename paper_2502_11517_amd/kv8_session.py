@@ -230,14 +230,14 @@ class Session:
         signed = [t.sees - (1 << 64) if t.sees >> 63 else t.sees for t in rows]
         times = Counter(id(t) for t in rows)
         self._on_stream(lambda: self._enter(dict(
-            n=n, most=max(count), rows=list(rows), verified=False, offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8), see=dev(signed, torch.int64),
+            n=n, most=max(count), rows=list(rows), threads=set(times), verified=False, offsets=dev(offsets, torch.int32), tag=dev([t.tag for t in rows], torch.uint8), see=dev(signed, torch.int64),
             position=dev(ids, torch.int32), stride=dev([times[id(t)] for t in rows], torch.int32))))
         for t in rows:
             t.position = after[id(t)]
 
     def _enter(self, step):
         for c in self._captured:
-            if c is not step and any(t is u for t in c["rows"] for u in step["rows"]):
+            if c["verified"] and c is not step and not c["threads"].isdisjoint(step["threads"]):
                 c["verified"] = False  # (its threads go on elsewhere, and know their positions from there)
         if torch.cuda.is_current_stream_capturing():
             self._captured.append(step)

@@ -140,3 +140,22 @@ def test_a_page_of_rejected_drafts_goes_back_ahead_of_the_step(session):
     assert s.length.tolist() == [16, 20] and int(s.free_count) == 0 and other.position == 16
     s.begin([one, other])
     assert s.length.tolist() == [17, 16] and s.refused() == [1] and other.position == 16
+
+
+def test_settle_goes_by_captured_steps_whose_threads_went_on_nowhere_else(session, monkeypatch):
+    s = session(60)
+    one, other = s.threads
+    for t in (one, other):
+        s.begin([t] * 4)
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+        s.again()
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+        verify(s, 1, 1)
+        s.settle()
+    assert [c["verified"] for c in s._captured] == [True, True] and (one.position, other.position) == (6, 6)
+    s.begin([one])
+    assert [c["verified"] for c in s._captured] == [False, True]
+    s.settle()
+    assert (one.position, other.position) == (7, 6)
+    s.again()
+    assert [c["verified"] for c in s._captured] == [False, True]

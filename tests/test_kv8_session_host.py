@@ -156,3 +156,31 @@ def test_threads_that_have_ended_neither_join_nor_fork(session):
     session.release(0)
     with pytest.raises(ValueError):
         session.fork(root)
+
+
+@pytest.mark.parametrize("captured", [1, 3])
+def test_a_step_costs_the_host_no_more_behind_captured_ones(session, monkeypatch, captured):
+    """Python's own steps of a begin() of many rows: no row is held against every row of the captured steps."""
+    import sys
+
+    session.slot = torch.full((4096,), -1, dtype=torch.int32)
+    one, other = session.open(0), session.open(1)
+
+    def steps_of(f):
+        seen = [0]
+        sys.setprofile(lambda *event: seen.__setitem__(0, seen[0] + 1))
+        try:
+            f()
+        finally:
+            sys.setprofile(None)
+        return seen[0]
+
+    alone = steps_of(lambda: session.begin([other] * 2000))
+    for _ in range(captured):
+        session.begin([one] * 64)
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+        session.again()
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    assert len(session._captured) == captured
+    behind = steps_of(lambda: session.begin([other] * 2000))
+    assert behind <= alone + 200 * captured, (alone, behind)
