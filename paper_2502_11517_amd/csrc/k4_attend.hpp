@@ -210,9 +210,14 @@ __device__ inline void times(State<D>& z, float x) {
     for (int k = 0; k < 16; ++k) z.o[i][k] *= x;
 }
 
+// How far a maximum may be ahead of the scores' base before that follows.  Where a base is beyond kFar, nothing: there fp32's steps are half a unit and more, so
+// that t_j + ev - m, rounded, and what it is compared with, rounded on its own way, may be any number of units apart; t_j + ev is rounded first there, and then
+// no weight is above 2^8.  (Kept out of the way of all other steps: a prompt's pass 337 -> 338 us, the smallest call 14.7 -> 15.2, batches within 1%.)
+constexpr float kAhead = kSlack + kLift, kFar = 0x1p22f;
+
 // N pairs (of BLOCKS blocks) and G groups of rows: their scores (times f) become the second product's operands.
 template <int BLOCKS, class Z, int G, int N>
-__device__ inline void soften(Z (&z)[G], float16v (&s)[G][N], float (&f)[G][N], Scales (&p)[N], half8 (&w)[G][N][2]) {
+__device__ inline void soften(Z (&z)[G], float& slack, float16v (&s)[G][N], float (&f)[G][N], Scales (&p)[N], half8 (&w)[G][N][2]) {
   bool rare = false;
 #pragma unroll
   for (int n = 0; n < N; ++n) rare |= p[n].rare;
@@ -265,9 +270,10 @@ __device__ inline void soften(Z (&z)[G], float16v (&s)[G][N], float (&f)[G][N], 
       const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(m[g]), __float_as_uint(m[g]), false, false);
       m[g] = fmaxf(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
     }
-    ahead |= m[g] > z[g].m + (kSlack + kLift);
+    ahead |= m[g] > z[g].m + slack;
   }
   if (__builtin_expect(__any(ahead), 0)) {
+    bool far = false;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const float to = fmaxf(m[g] - kLift, z[g].m), h = root_exp2(z[g].m - to), alpha = h * h;
@@ -275,6 +281,25 @@ __device__ inline void soften(Z (&z)[G], float16v (&s)[G][N], float (&f)[G][N], 
       z[g].m = to;
       z[g].l = z[g].l * h * h;
       if (!__all(fresh)) times(z[g], alpha);
+      far |= fabsf(to) >= kFar && to != -FLT_MAX;
+    }
+    slack = __any(far) ? 0.f : kAhead;
+  }
+  if (__builtin_expect(slack == 0.f, 0)) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        float to = f[g][n];
+        asm volatile("" : "+v"(to));  // (or else this is done ahead of the branch)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[g][n][i] = fmaf(s[g][n][i], to, p[n].ev);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        f[g][n] = 1.f;
+      }
+      p[n].ev = 0.f;
     }
   }
   if (__builtin_expect(rare, 0)) {
@@ -351,7 +376,7 @@ __device__ inline int windows(const Codes<D>& c, bool there, const uint4v* q, fl
 // One step of a wave: N pairs whose codes are in c, against G groups of 32 rows.  `ahead` is called when K may be overwritten, `behind` when V may.
 template <int D, bool F16, int KIND, int G, int N, class Ahead, class Behind>
 __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&r)[G], const uint4v* q, int unit, State<D> (&z)[G], Codes<D> (&c)[N],
-                            const int (&absent)[N], const Marks (&marks)[N], const int (&t0)[N], int& most, Ahead ahead, Behind behind) {
+                            const int (&absent)[N], const Marks (&marks)[N], const int (&t0)[N], int& most, float& slack, Ahead ahead, Behind behind) {
   float16v s[G][N];
 #pragma unroll
   for (int g = 0; g < G; ++g)
@@ -417,7 +442,7 @@ __device__ inline void step(const AttendArgs& a, const Unit& u, const Rows<D> (&
         finish_scores<KIND>(a, u.prefix, u.hi, t0[n], pair, Unmarked{}, r[g].slope, r[g].token, r[g].first_token, f[g][n], s[g][n]);
     }
   half8 w[G][N][2];
-  k4::soften<2>(z, s, f, p, w);
+  k4::soften<2>(z, slack, s, f, p, w);
   __builtin_amdgcn_s_setprio(1);
   __builtin_amdgcn_sched_barrier(0);  // (V's codes are turned as they are needed: all at once they take 64 registers more)
 #pragma unroll
@@ -450,6 +475,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
   Blocks b;
   uint64_t gone;
   int most = kEMin + 127;  // largest byte of V's scales so far
+  float slack = kAhead;
   Codes<D> c[N];
   Marks marks[N] = {};
   auto token = [&](int i) { return u.lo + (wave + 4 * i) * 32; };  // first of the wave's i-th pair
@@ -505,7 +531,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
     int t0[N], absent[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) t0[n] = token(i + n), absent[n] = absent_of(i + n);
-    k4::step<D, F16, KIND, G, N>(a, u, r, q, unit, z, c, absent, marks, t0, most,
+    k4::step<D, F16, KIND, G, N>(a, u, r, q, unit, z, c, absent, marks, t0, most, slack,
       [&] {
         if (i + N >= n_pairs) return;
         if (((i + N) & 31) == 0) find(i + N);
@@ -525,7 +551,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
     if (i < n_pairs) {
       const int t0[1] = {token(i)}, absent[1] = {absent_of(i)};
       const Marks last[1] = {marks[0]};
-      k4::step<D, F16, KIND, G, 1>(a, u, r, q, unit, z, *(Codes<D>(*)[1]) & c, absent, last, t0, most, [] {}, [] {});
+      k4::step<D, F16, KIND, G, 1>(a, u, r, q, unit, z, *(Codes<D>(*)[1]) & c, absent, last, t0, most, slack, [] {}, [] {});
     }
   }
   // The four waves meet, group after group.  Each gives three quarters of its output to the others and joins the fourth with theirs: quarter y of a lane's

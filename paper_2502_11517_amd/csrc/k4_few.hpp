@@ -113,7 +113,7 @@ __device__ inline int few_windows(const FewCodes<D>& c, const int (&byte)[4], co
 // One step of a wave.  `ahead` is called when K may be overwritten, `behind` when V may.
 template <int D, bool F16, int KIND, class Ahead, class Behind>
 __device__ inline void few_step(const AttendArgs& a, const Unit& u, const Rows<D>& r, const uint4v (&q)[D / 32], int unit, FewState<D> (&z)[1], FewCodes<D>& c,
-                                int absent, const Marks& marks, int t0, int& most, Ahead ahead, Behind behind) {
+                                int absent, const Marks& marks, int t0, int& most, float& slack, Ahead ahead, Behind behind) {
   float4v p[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) p[t] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -151,7 +151,7 @@ __device__ inline void few_step(const AttendArgs& a, const Unit& u, const Rows<D
   else
     finish_scores<KIND, 4>(a, u.prefix, u.hi, t0, pair, Unmarked{}, r.slope, r.token, r.first_token, f[0][0], s[0][0]);
   half8 w[1][1][2];
-  k4::soften<4>(z, s, f, scales, w);
+  k4::soften<4>(z, slack, s, f, scales, w);
   __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int y = 0; y < 2; ++y)
@@ -181,6 +181,7 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
   Blocks b;
   uint64_t gone;
   int most = kEMin + 127;  // largest byte of V's scales so far
+  float slack = kAhead;
   FewCodes<D> c;
   Marks marks{};
   auto token = [&](int i) { return u.lo + (wave + 4 * i) * kFour; };  // first of the wave's i-th step
@@ -211,7 +212,7 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
   for (int i = 0; i < D / 16; ++i) z[0].o[i] = float4v{0.f, 0.f, 0.f, 0.f};
   z[0].m = -FLT_MAX, z[0].l = 0.f, z[0].bad = 0.f;
   for (int i = 0; i < n_steps; ++i)
-    few_step<D, F16, KIND>(a, u, r, q, unit, z, c, (int)(gone >> first_of(i)) & 15, marks, token(i), most,
+    few_step<D, F16, KIND>(a, u, r, q, unit, z, c, (int)(gone >> first_of(i)) & 15, marks, token(i), most, slack,
       [&] {
         if (i + 1 >= n_steps) return;
         if (((i + 1) & 15) == 0) find(i + 1);
