@@ -44,6 +44,12 @@ constexpr int kNear = 8;      // powers of two between a block's V scales that i
 constexpr float kLift = 7.f;  // The base of the scores is set 2^7 below their maximum and follows when that is 2^15 ahead, which fp16 still holds: so its
                               // smallest normal number is 2^-21 of the largest weight or less, times 2^kNear where that is one of a small V scale
 
+// The sums l are held 2^-kRoom times: a token's term is between 2^-112 (V's scale 2^119, the weight 2^7) and 2^115 (2^-100, as of a V of zeros, and 2^15), of which
+// 2^13 are no fp32 number, but 2^25 times 2^-12 are.  (A multiplication a step: prompts within 1.5% of what they took, the rest within what two runs differ by.)
+constexpr float kRoom = 12.f, kLess = 0x1p-12f;
+
+__device__ inline float lse_of(float m, float l) { return l == 0.f ? -INFINITY : kLn2 * (m + (__builtin_amdgcn_logf(l) + kRoom)); }
+
 // A wave's rows of Q, as pieces of 8 dims: lane n and n + 32 hold row n, group 2x + half of the dims at 4x .. 4x + 3.  With 16 rows, lanes n, n + 16, ..
 // each a quarter of the dims.
 template <int D, bool MARKS, int ROWS = kRows>
@@ -307,7 +313,7 @@ __device__ inline void soften(Z (&z)[G], float& slack, float16v (&s)[G][N], floa
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        const float h = root_exp2(own_m[g][n] - z[g].m);
+        const float h = root_exp2(own_m[g][n] - z[g].m - kRoom);
         z[g].l = fmaf(own_l[g][n] * h, h, z[g].l);
       }
   }
@@ -328,7 +334,7 @@ __device__ inline void soften(Z (&z)[G], float& slack, float16v (&s)[G][N], floa
       }
     });
 #pragma unroll
-    for (int g = 0; g < G; ++g) z[g].l = fmaf(sum[g], back[n], z[g].l);
+    for (int g = 0; g < G; ++g) z[g].l = fmaf(sum[g] * kLess, back[n], z[g].l);
   }
 }
 
@@ -601,7 +607,7 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
     if (!r[g].real) continue;
     const int s = u.s0 + g * kRows + row, first = 16 * wave + 8 * half;
     const int64_t to = u.part < 0 ? row_address(a, s, head) : (int64_t)(u.part + g * kRows + row) * a.g.Hkv + head;
-    const float inverse = inverse_of(all);
+    const float inverse = inverse_of(all) * kLess;
 #pragma unroll
     for (int x = 0; x < D / 64; ++x) {
       float4v o[2];
@@ -616,12 +622,12 @@ __device__ inline void attend_unit(const AttendArgs& a, const Unit& u, int liste
         store_out(a, to * D + 64 * x + first + 4, o[1] * inverse);
       } else {
         float4v* p = (float4v*)(a.part_acc + to * D + 64 * x + first);
-        p[0] = o[0], p[1] = o[1];
+        p[0] = o[0] * kLess, p[1] = o[1] * kLess;
       }
     }
     if (wave == 0 && half == 0) {
-      if (u.part >= 0) a.part_ml[to] = float2v{m, all};
-      else if (a.lse) a.lse[to] = lse_of(m, all);
+      if (u.part >= 0) a.part_ml[to] = float2v{m + kRoom, all};
+      else if (a.lse) a.lse[to] = k4::lse_of(m, all);
     }
   }
 }

@@ -261,7 +261,7 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
   const float mine = wave < 2 ? (wave == 0 ? factor[0] : factor[1]) : (wave == 2 ? factor[2] : factor[3]);
   if (!r.real) return;
   const int64_t to = u.part < 0 ? row_address(a, u.s0 + row, head) : (int64_t)(u.part + row) * a.g.Hkv + head;
-  const float inverse = inverse_of(all);
+  const float inverse = inverse_of(all) * kLess;
 #pragma unroll
   for (int k = 0; k < kOwn; ++k) {
     float4v o = own[k] * mine;
@@ -270,11 +270,11 @@ __device__ inline void attend_few(const AttendArgs& a, const Unit& u, int listed
     const int at = wave * kOwn + k;
     const int64_t dims = to * D + 32 * (at / 2) + 8 * part + 4 * (at % 2);
     if (u.part < 0) store_out(a, dims, o * inverse);
-    else *(float4v*)(a.part_acc + dims) = o;
+    else *(float4v*)(a.part_acc + dims) = o * kLess;
   }
   if (wave == 0 && part == 0) {
-    if (u.part >= 0) a.part_ml[to] = float2v{m, all};
-    else if (a.lse) a.lse[to] = lse_of(m, all);
+    if (u.part >= 0) a.part_ml[to] = float2v{m + kRoom, all};
+    else if (a.lse) a.lse[to] = k4::lse_of(m, all);
   }
 }
 
