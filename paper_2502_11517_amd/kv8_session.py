@@ -56,7 +56,8 @@ class Session:
         if codes == "e2m1":
             self.cfg = cfg = kv4.make_config(dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale, **sizes)
             self.k_codes, self.v_codes, self.k_scale, self.v_scale = (torch.empty(s, **u8) for s in kv4.cache_shapes(cfg))
-            self.places = kv8.make_config("e4m3", dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale, **{**sizes, "n_layers": 1})
+            # (places go by none of an attention's sizes: the least there are, since the workspace holds a plan's partial rows, too, which nobody asks for)
+            self.places = kv8.make_config("e4m3", dtype, 1, 1, 64, 1.0, **{**sizes, "n_layers": 1})
             self.places_workspace = torch.empty(kv8.query_workspace_bytes(self.places), **u8)
         else:
             self.cfg = cfg = kv8.make_config(codes, dtype, n_q_heads, n_kv_heads, head_dim, softmax_scale, **sizes)
