@@ -35,8 +35,10 @@ typedef struct pasta_kv4 pasta_kv4; /* opaque */
  *
  * A code is a sign, two bits of exponent and one of mantissa: 0, 1/2, 1, 3/2, 2, 3, 4, 6
  * are the codes 0 .. 7, their negatives 8 .. 15.  Every row of K has a scale per kv head
- * and 32 dims, every row of V one per kv head: a power of two 2^e, held as the byte
- * e + 127, or the byte 255, under which the values read as NaN.
+ * and 32 dims, every row of V one per kv head: a power of two 2^e, -100 <= e <= 119, held
+ * as the byte e + 127, or the byte 255, under which the values read as NaN.  (Of bytes that
+ * are none of these pasta_kv4_read makes 2^(byte - 127); what pasta_kv4_attend makes of them
+ * is not said.)
  *
  * Slots and blocks are those of pasta_kv8.h.  A block of 16 tokens of page p, kv head g is
  *
@@ -124,7 +126,7 @@ int32_t pasta_kv4_read(pasta_kv4 *h, const pasta_kv4_read_args *a);
  * is said there: a token whose K reads as NaN for a head gives NaN to the rows that see it,
  * one whose V does, too (out, not lse).  K enters the products exactly; q does, too; the
  * softmax weights, each times its token's V scale and in units of the row's largest such product,
- * enter the product with V as fp16: what is 2^-25 of the largest or less adds to the sums,
+ * enter the product with V as fp16: what is 2^-24 of the largest or less adds to the sums,
  * but nothing to out.  Scores are held in fp32, which tells those beyond 2^22 in magnitude
  * no longer apart by what matters: there out is still a mean of the values of tokens whose
  * scores are the largest within 2^-18 of that magnitude, and out and lse are finite as long

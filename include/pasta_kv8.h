@@ -133,7 +133,7 @@ typedef struct {
 int32_t pasta_kv8_slots(pasta_kv8 *h, const pasta_kv8_slots_args *a);
 
 /* New rows of one layer into the cache, k_new and v_new [n_rows][Hkv][D].  Rows of
- * one block have to be neighbours with ascending slots, as pasta_kv8_slots gives
+ * one block have to be neighbours with consecutive slots, as pasta_kv8_slots gives
  * them out; rows whose slot is not in [0, n_phys_pages * page_tokens) are skipped.
  *
  * Scales.  Q = 448 (E4M3) or 127 (INT8).  For the rows that a call brings into a
@@ -200,7 +200,9 @@ int32_t pasta_kv8_plan(pasta_kv8 *h, const pasta_kv8_plan_args *a);
  * its block's V scale and in units of the row's largest such product, enter the
  * product with V as fp16: what is 2^-25 of the largest or less adds to the sums, but
  * nothing to out.  Rows that no request has (behind row_offsets[n_requests]) get
- * out = 0, lse = -inf.
+ * out = 0, lse = -inf.  Scores are held in fp32, too: where a row's largest is beyond
+ * 2^22 in magnitude, those near it are no longer told apart, and beyond 2^27 out and
+ * lse can be anything, NaN included.
  * Needs everything but free_pages; slot_tag with row_see, slot_position with
  * row_position.  n_rows is that of the last plan (E_STATE otherwise, or without one).
  * Errors: E_INVAL, E_DEVICE, E_STATE.                                            */

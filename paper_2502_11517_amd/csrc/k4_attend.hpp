@@ -14,7 +14,8 @@
 //           the weight, rounded to fp16 before that, stays as exact.  Where a block's scales are further apart, or one of them is further below the largest so
 //           far, or not a number, the step takes scores t_j + ev_j instead, token by token, and sums l from t_j apart (rare: V's rows of a model differ by
 //           a few powers of two).
-// Weights rounded to fp16, at most 2^-11 of each, are the only rounding that fp32 does not see.
+// Weights rounded to fp16, each by at most 2^-11 of itself or 2^-25 (which is 2^-24 of the row's largest product of weight and scale, or less), are the only rounding
+// that fp32 does not see.
 //
 // Products are transposed, S^T = K Q^T and O^T = V^T P^T, in 32x32x16 steps over 32 tokens x 32 stacked rows.  A lane's piece of K is 16 bytes, the 32 dims of
 // one token under one scale; its piece of V 16 bytes, two neighbouring dims of a block's 16 tokens, which go to two products' rows: the dims of a product are
@@ -22,11 +23,12 @@
 // most 16 rows go in steps of another shape (k4_few.hpp).
 //
 // What bounds it (8 kv heads of 128; a layer):
-//   8 streams over 8k tokens, 11 MB        9.5 us: the ramp, as in the 8-bit cache (11.1): a work-group has 1.3 steps' worth to each wave; 2.5 of launch
-//   16 ragged requests, capped, 50 MB      20.3 us: units with more than 16 rows, 15 of these us and more in a wave's chain from step to step, ramp and end 4; vector
+//   8 streams over 8k tokens, 11 MB        9.6 us: the ramp, as in the 8-bit cache (11.1): a work-group has 1.3 steps' worth to each wave; 2.5 of launch
+//   16 ragged requests, capped, 50 MB      20.0 us: units with more than 16 rows, 15 of these us and more in a wave's chain from step to step, ramp and end 4; vector
 //                                          instructions, 23 a score, are busy half of the time, and ten percent fewer (the cap by a series) changed nothing
-//   2048 x 4 rows over 8k tokens, 309 GF   325 to 365 us by the card, 850 to 950 TFLOP/s against 1190 of a large library product: vector instructions busy 68% of the
-//                                          time, matrix instructions 42%
+//   2048 x 4 rows over 8k tokens, 309 GF   329 us once the card's clocks have settled (325 to 350 by the card; 360 to 416 in the first thirty launches), 880 to 950
+//                                          TFLOP/s (740 to 860) against 1190 of a large library product: vector instructions busy 68% of the time, matrix
+//                                          instructions 42%.  2048 rows that end 8k tokens: plain 264 us, with tags 340, capped 370; of 64 dims 178, with tags 235
 // Tried and not taken: the scaled matrix instruction on the codes themselves with q split into e4m3 parts (its sums are off by 1.5e-4 of their terms' magnitudes,
 // a hundred times as much as a sum in fp32), eight waves to a work-group (8 streams over 8k 109 -> 110 us a pass, the prompt 389 -> 415), the first blocks in scalar
 // registers (no change), Q's rows loaded whole and turned in LDS (the prompt 333 -> 338).

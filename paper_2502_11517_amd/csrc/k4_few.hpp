@@ -1,6 +1,7 @@
 // Attention over the 4-bit cache of units with at most 16 stacked rows: one or a few threads, where half of a tile of 32 rows and more would be empty.
 //
-// As k4_attend.hpp, in 16x16x32 steps over 64 tokens (four blocks) x 16 rows: half the scores, and so half the softmax, per lane and token.
+// As k4_attend.hpp, in 16x16x32 steps over 64 tokens (four blocks) x 16 rows: half the scores, and so half the softmax, per lane and token.  Only in launches without
+// tiles of 64 rows: beside those the registers do not hold both forms, and such units go in steps of 32 rows there.
 //   S^T = K Q^T    four tiles of 16 tokens: row m of tile t is token 4t + m % 4 of block m / 4, so that lane row + 16 g gets the 16 scores of block g, its operand of
 //                  the second product; a lane's piece of K is a quarter of a token's dims
 //   O^T = V^T P^T  a lane's piece of V is two neighbouring dims of a block's 16 tokens, which go to two products: the dims of a product are every second of 32

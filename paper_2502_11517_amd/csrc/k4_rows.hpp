@@ -7,7 +7,7 @@
 //      tokens share a byte, so those of the block's other tokens are read and put back.
 //
 // Long calls are bound by memory: 8192 rows of 8 heads of 128, bf16, 42 MB, in 11.9 us into the cache (3.6 TB/s) and in 9.6 out of it (4.4; a large copy 5.2);
-// 32768 rows out of it, 169 MB, in 36.8 (4.6).  A step of eight rows takes 3.1 and 2.6 us, a launch and its two dependent reads (slots, then rows or codes).
+// 32768 rows out of it, 169 MB, in 37 (4.6).  A step of eight rows takes 3.2 and 2.7 us, a launch and its two dependent reads (slots, then rows or codes).
 // Tried and not taken for steps: rows asked for together with their slots, and V's codes set by atomics instead of read and put back (a step of eight rows, 8
 // layers in and out, 51.4 -> 52.5 us; 128 single rows of as many requests 27 -> 35).
 #pragma once

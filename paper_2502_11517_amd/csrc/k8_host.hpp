@@ -35,8 +35,8 @@ bool sizes_hold(const Config& c) {
   return true;
 }
 
-// Work-groups of the attention: two per CU.  (256 / 384 / 768: eight streams over 8k tokens of the 4-bit cache, 8 layers, 118 / 110 / 124 us for 105, 16 ragged
-// requests, 4 layers, 131 / 120 / 124 for 107.)
+// Work-groups of the attention: two per CU.  (256 / 384 / 768: eight streams over 8k tokens of the 4-bit cache, 8 layers, 118 / 110 / 124 us where these take 105, 16 ragged
+// requests, 4 layers, 131 / 120 / 124 where they took 107, ahead of the weights in k8_plan.hpp.)
 constexpr int kUnitsAtOnce = 512;
 
 struct Bounds {

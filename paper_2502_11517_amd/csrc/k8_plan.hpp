@@ -20,7 +20,10 @@ namespace k8 {
 
 // Tiles of at most few_rows rows take less time for a token, half (the softmax, the matrix instructions) to all of it (memory): they weigh three for four in a
 // step that has both kinds.  16 requests of 1 to 8 threads, 32 / 8 heads: ragged and capped, 4 layers, 104 -> 99.5 us, 90 -> 87.5 without caps, over 16k to 32k tokens, 2
-// layers, 203 -> 197 (two for three: 99.8, 86.5, 212); 12 with 64 dims 84 -> 75; 40 over up to 4k 168 -> 153.
+// layers, 203 -> 197 (two for three: 99.8, 86.5, 212); 12 with 64 dims 84 -> 75; 40 over up to 4k 168 -> 153.  In steps with tiles of 64 rows, where units with few rows
+// have no steps of their own, it stands for what the tiles of 64 take more than others, and is as often worse as better (alike -> three for four: 512 rows beside 15 of one
+// over 8k, with tags 677 -> 575, plain 455 -> 482; 300 beside 7 of four 212 -> 202 and 174 -> 159; 2048 beside 31 of one 690 -> 724 and 592 -> 620).  k8_plan_long weighs all
+// alike.
 constexpr int kFew = 3, kMany = 4;
 
 struct PlanArgs {
@@ -164,7 +167,7 @@ __global__ __launch_bounds__(NT) void k8_plan(PlanArgs a) {
   // the second half of what runs at once stands in reverse
   const int here = blockIdx.x, half = a.capacity / 2;
   const int unit = n_units <= a.capacity && here >= half && here < n_units ? half + n_units - 1 - here : here;
-  const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;  // (the host's bounds hold: see pasta_kv8.hip)
+  const bool fits = at + parts <= a.max_units && row_at + rows <= a.max_part_rows;  // (the host's bounds hold: see k8_host.hpp)
   if (unit >= at && unit < at + parts && fits) s_unit = part_of(u, cost, unit - at, parts, row_at);
   if (blockIdx.x == 0 && tid < a.max_tiles) a.tiles[tid] = Tile{u.s0, u.n_rows, row_at, tid < n_tiles && fits ? parts : 0};
   __syncthreads();

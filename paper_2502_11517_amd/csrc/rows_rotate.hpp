@@ -85,6 +85,8 @@ __device__ inline void turn_of(double revolutions, float& c, float& s) {
 
 // WIDE: every piece of a head is 16 bytes, of one kind: half-split planes (then the piece is two, half the turned dims apart), interleaved ones, or dims that
 // stay.  Else a piece is one plane or one dim that stays: rope_dims that are not whole 16-byte pieces.  A work-group turns ROWS rows.
+// The narrow form is bound by its instructions and work-groups, two to four bytes to each: 8192 rows of 32 + 8 heads of 128 dims, of which 34 or 50 are turned, take 188 us,
+// 100 128, against 35 of the wide one; a work-group has one row's two or three heads, and each finds the row's sines anew.
 template <int TYPE, bool WIDE, int ROWS>
 __global__ __launch_bounds__(256) void rows_rotate(RotateArgs a) {
   __shared__ float s_cos[ROWS][kMaxDim / 2], s_sin[ROWS][kMaxDim / 2];

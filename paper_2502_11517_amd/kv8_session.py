@@ -304,7 +304,8 @@ class Session:
                          row_position=s["position"] if self.slopes is not None else None)
 
     def verify(self, token, target, draw, last_draw, draft=None):
-        """Holds the step's rows to the target's probabilities: of each request's rows, those of one thread, the first is its last token and the others drafts.
+        """Holds the step's rows to the target's probabilities: of each request's rows, those of one thread (what is not accepted goes from the request's end, where
+        the rows of several threads would lie in turn), the first is its last token and the others drafts.
         token, draw [n]; target, draft [n, vocab]; last_draw [max_requests].  Returns (accepted, next token) of every request, on the device, until the next call.
 
         The next begin() or again() takes back what was not accepted.  again() goes on behind the accepted rows without the host; begin(), fork() and join()

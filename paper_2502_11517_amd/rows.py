@@ -107,7 +107,7 @@ def rope_frequencies(dims, theta=10000.0, *, scaling="none", factor=1.0, trained
 
 def make_config(*, max_rows=1, n_q_heads=0, n_kv_heads=0, head_dim=0, rope_dims=0, rope_layout="half", rope_frequency=None, rope_magnitude=1.0, vocab=0,
                 max_sequences=0) -> Config:
-    """`rope_frequency`: radians a position, rope_dims / 2 numbers (rope_frequencies) or a float64 tensor of them on the GPU."""
+    """`rope_frequency`: radians a position, rope_dims / 2 numbers (rope_frequencies) or a float64 tensor of them on the GPU, which saves every handle a copy."""
     c = Config()
     c.struct_size = C.sizeof(Config)
     c.max_rows, c.n_q_heads, c.n_kv_heads, c.head_dim = max_rows, n_q_heads, n_kv_heads, head_dim

@@ -7,7 +7,6 @@ import torch
 
 import kv8_ref as ref
 from paper_2502_11517_amd import kv8
-from paper_2502_11517_amd.kv8_session import Session
 from test_gpu_kv4_session import SIZES, Drafted
 
 pytestmark = pytest.mark.gpu
