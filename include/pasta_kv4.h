@@ -130,8 +130,8 @@ int32_t pasta_kv4_read(pasta_kv4 *h, const pasta_kv4_read_args *a);
  * but nothing to out.  Scores are held in fp32, which tells those beyond 2^22 in magnitude
  * no longer apart by what matters: there out is still a mean of the values of tokens whose
  * scores are the largest within 2^-18 of that magnitude, and out and lse are finite as long
- * as the scores are (but where a block's V scales are more than 2^8 apart they can be
- * anything).                                                                             */
+ * as the scores are (but where a block's V scales are more than 2^8 apart, or beyond 2^100,
+ * they can be anything).                                                                 */
 int32_t pasta_kv4_plan(pasta_kv4 *h, const pasta_kv8_plan_args *a);
 int32_t pasta_kv4_attend(pasta_kv4 *h, const pasta_kv8_attend_args *a);
 
